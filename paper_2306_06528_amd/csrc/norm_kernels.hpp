@@ -1,0 +1,219 @@
+// Layer norm of n x rows rows of `width` values and its backward pass.  A row is held in registers by a team of
+// L threads, E values each, from its one load to its one store: the mean is known before the squares of the distances from
+// it are summed, so a row far from zero loses nothing.  Memory bounds both passes.
+#pragma once
+#include "layer_common.hpp"
+
+namespace svgd {
+
+// Sum over a team of L threads, in all of them.  Teams of more than a wave are workgroups (64 .. 1024 threads): `slots` is
+// LDS of 2 * 16 floats, used by turns, so that one barrier per sum is enough.
+template <int L> struct TeamSum {
+    float *slots;
+    int turn = 0;
+    __device__ __forceinline__ float operator()(float v)
+    {
+        if constexpr (L <= 16) {
+            return row_sum<L>(v);
+        } else if constexpr (L == 32) {
+            const unsigned u = __float_as_uint(row_sum(v));
+            const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+            return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        } else if constexpr (L == 64) {
+            return wave_sum(v);
+        } else {
+            float *const s = slots + 16 * turn;
+            turn ^= 1;
+            v = wave_sum(v);
+            if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = 0.f;
+#pragma unroll
+            for (int w = 0; w < L / 64; ++w) v += s[w];
+            return v;
+        }
+    }
+};
+
+template <int L> constexpr int kTeamBlock = L > 256 ? L : 256; // threads per workgroup
+template <int L> constexpr int kTeams = kTeamBlock<L> / L;     // rows at a time
+
+struct NormShape {
+    int64_t rows;
+    int width;
+    int blocks;       // workgroups per particle
+    int64_t per;      // rows of each
+};
+template <class T> struct ActRows {
+    T *p;
+    int64_t particle, row;
+};
+
+template <class T, int L, int E>
+__global__ __launch_bounds__(kTeamBlock<L>) void norm_forward_kernel(NormShape s, ActRows<const T> x, Params weight, Params bias, float eps, ActRows<T> y,
+                                                                     float *mean_out, float *rstd_out)
+{
+    constexpr int VEC = 16 / sizeof(T), C = E / VEC;
+    __shared__ float slots[32];
+    TeamSum<L> sum{slots};
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t particle = blockIdx.x / s.blocks;
+    const int64_t first = (blockIdx.x % s.blocks) * s.per, last = first + s.per < s.rows ? first + s.per : s.rows;
+    float w[E], b[E];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * L + lane) * VEC;
+        float v[VEC];
+        load_pack<float, VEC>(weight.p + particle * weight.stride + col, s.width - col, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[c * VEC + e] = v[e];
+        load_pack<float, VEC>(bias.p + particle * bias.stride + col, bias.p ? s.width - col : 0, v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) b[c * VEC + e] = v[e];
+    }
+    const float inv = 1.f / (float)s.width;
+    for (int64_t r0 = first; r0 < last; r0 += kTeams<L>) {
+        const int64_t r = r0 + team;
+        const bool live = r < last;
+        float v[C][VEC], total = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * VEC;
+            load_pack<T, VEC>(x.p + particle * x.particle + r * x.row + col, live ? s.width - col : 0, v[c]);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) total += v[c][e];
+        }
+        const float mean = sum(total) * inv;
+        float square = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                v[c][e] -= mean;
+                if ((c * L + lane) * VEC + e < s.width) square += v[c][e] * v[c][e];
+            }
+        const float rstd = 1.f / sqrtf(sum(square) * inv + eps);
+        if (!live) continue;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * VEC;
+            float out[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) out[e] = v[c][e] * rstd * w[c * VEC + e] + b[c * VEC + e];
+            store_pack<T, VEC>(y.p + particle * y.particle + r * y.row + col, s.width - col, out);
+        }
+        if (lane == 0) {
+            if (mean_out) mean_out[particle * s.rows + r] = mean;
+            if (rstd_out) rstd_out[particle * s.rows + r] = rstd;
+        }
+    }
+}
+
+// dx row by row; every thread adds up dy xhat and dy of its columns over the workgroup's rows, the teams' sums are added
+// in LDS and go to partials[workgroup][2][width].  norm_reduce_kernel adds those: no atomics, the same bits every time.
+template <class T, int L, int E>
+__global__ __launch_bounds__(kTeamBlock<L>) void norm_backward_kernel(NormShape s, ActRows<const T> dy, ActRows<const T> x, Params weight,
+                                                                      const float *mean_in, const float *rstd_in, ActRows<T> dx, float *partials)
+{
+    constexpr int VEC = 16 / sizeof(T), C = E / VEC;
+    __shared__ float slots[32];
+    __shared__ float sums[kTeams<L> > 1 ? 2 * E * kTeamBlock<L> : 1];
+    TeamSum<L> sum{slots};
+    const int lane = threadIdx.x % L, team = threadIdx.x / L;
+    const int64_t particle = blockIdx.x / s.blocks;
+    const int64_t first = (blockIdx.x % s.blocks) * s.per, last = first + s.per < s.rows ? first + s.per : s.rows;
+    float w[C][VEC], dw[C][VEC], db[C][VEC];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * L + lane) * VEC;
+        load_pack<float, VEC>(weight.p + particle * weight.stride + col, s.width - col, w[c]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
+    }
+    const float inv = 1.f / (float)s.width;
+    for (int64_t r0 = first; r0 < last; r0 += kTeams<L>) {
+        const int64_t r = r0 + team;
+        const bool live = r < last;
+        const float mean = live ? mean_in[particle * s.rows + r] : 0.f, rstd = live ? rstd_in[particle * s.rows + r] : 0.f;
+        float v[C][VEC], d[C][VEC], sa = 0.f, sax = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * VEC, left = live ? s.width - col : 0;
+            load_pack<T, VEC>(x.p + particle * x.particle + r * x.row + col, left, v[c]);
+            load_pack<T, VEC>(dy.p + particle * dy.particle + r * dy.row + col, left, d[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) { // (beyond the width dy and weight are 0; x is not to count either: -mean * rstd may be infinite)
+                v[c][e] = (c * L + lane) * VEC + e < s.width ? (v[c][e] - mean) * rstd : 0.f;
+                dw[c][e] += d[c][e] * v[c][e];
+                db[c][e] += d[c][e];
+                d[c][e] *= w[c][e];
+                sa += d[c][e];
+                sax += d[c][e] * v[c][e];
+            }
+        if (!dx.p) continue;
+        const float ma = sum(sa) * inv, max = sum(sax) * inv;
+        if (!live) continue;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * VEC;
+            float out[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) out[e] = rstd * (d[c][e] - ma - v[c][e] * max);
+            store_pack<T, VEC>(dx.p + particle * dx.particle + r * dx.row + col, s.width - col, out);
+        }
+    }
+    if (!partials) return;
+    float *const mine = partials + (int64_t)blockIdx.x * 2 * s.width;
+    if constexpr (kTeams<L> == 1) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * VEC;
+            store_pack<float, VEC>(mine + col, s.width - col, dw[c]);
+            store_pack<float, VEC>(mine + s.width + col, s.width - col, db[c]);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                sums[(c * VEC + e) * kTeamBlock<L> + threadIdx.x] = dw[c][e];
+                sums[(E + c * VEC + e) * kTeamBlock<L> + threadIdx.x] = db[c][e];
+            }
+        __syncthreads();
+        for (int k = threadIdx.x; k < 2 * E * L; k += kTeamBlock<L>) {
+            const int which = k / (E * L), e = k / L % E, l = k % L;
+            float total = 0.f;
+#pragma unroll
+            for (int t = 0; t < kTeams<L>; ++t) total += sums[(which * E + e) * kTeamBlock<L> + t * L + l];
+            const int col = (e / VEC * L + l) * VEC + e % VEC;
+            if (col < s.width) mine[which * s.width + col] = total;
+        }
+    }
+}
+
+// Sums of a particle's partials, in the same order every time: 64 columns per workgroup, its four waves take every fourth
+// partial and their sums are added in order.
+__global__ __launch_bounds__(256) void norm_reduce_kernel(const float *partials, int blocks, int width, int column_groups, Params dweight, Params dbias,
+                                                          bool accumulate)
+{
+    __shared__ double sums[4][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t particle = blockIdx.x / column_groups;
+    const int col = (blockIdx.x % column_groups) * 64 + lane; // of 2 * width
+    double total = 0.0;
+    if (col < 2 * width)
+        for (int b = wave; b < blocks; b += 4) total += (double)partials[((particle * blocks + b) * 2) * (int64_t)width + col];
+    sums[wave][lane] = total;
+    __syncthreads();
+    if (wave != 0 || col >= 2 * width) return;
+    const Params &out = col < width ? dweight : dbias;
+    if (!out.p) return;
+    float *const p = const_cast<float *>(out.p) + particle * out.stride + (col < width ? col : col - width);
+    const double v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    *p = (float)(accumulate ? v + (double)*p : v);
+}
+
+} // namespace svgd
