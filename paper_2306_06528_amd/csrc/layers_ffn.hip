@@ -1,5 +1,5 @@
 // Host side of the gated feed-forward block (include/svgd_layers.h): checks and launches.
-#include "ffn_kernels.hpp"
+#include "ffn_thin_kernels.hpp"
 
 using namespace svgd;
 
@@ -26,10 +26,37 @@ template <class T> Rows<const T> in(const svgd_rows &r) { return {(const T *)r.d
 template <class T> Rows<T> out(const svgd_rows &r) { return {(T *)r.data, r.particle_stride, r.row_stride}; }
 int launched() { return hipGetLastError() == hipSuccess ? SVGD_OK : SVGD_ERR_DEVICE; }
 
+// Up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp).
+constexpr int64_t kThinRows = 32;
+
+template <class T, int ACT, int JB> int thin_forward(const Call &c, const svgd_rows &x, const svgd_rows &y, float *h, float *g, float *u, bool save)
+{
+    const ThinGrid first(c.s.hidden, 16), second(c.s.width, 16);
+    const int blocks = c.n * first.per_particle;
+    if (save) thin_gate_up_kernel<T, ACT, true, JB><<<blocks, kThinBlock, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, g, u);
+    else thin_gate_up_kernel<T, ACT, false, JB><<<blocks, kThinBlock, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
+    if (const int rc = launched()) return rc;
+    thin_down_kernel<T, JB><<<c.n * second.per_particle, kThinBlock, 0, c.stream>>>(c.s, second, h, c.down, out<T>(y));
+    return launched();
+}
+
+template <class T, int ACT, int JB>
+int thin_backward(const Call &c, const svgd_rows &dy, const float *g, const float *u, const svgd_rows &dx, float *dg, float *du)
+{
+    const ThinGrid hidden(c.s.hidden, 32), input(c.s.width, 32);
+    thin_hidden_grad_kernel<T, ACT, JB><<<c.n * hidden.per_particle, kThinBlock, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
+    const int rc = launched();
+    if (rc || !dx.data) return rc;
+    thin_input_grad_kernel<T, JB><<<c.n * input.per_particle, kThinBlock, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
+    return launched();
+}
+
 template <class T, int ACT> int forward(const Call &c, const svgd_rows &x, const svgd_rows &y, float *buffer, bool save)
 {
     const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
     float *const h = buffer, *const g = buffer + plane, *const u = buffer + 2 * plane;
+    if (c.s.rows <= kThinRows)
+        return c.s.rows <= 16 ? thin_forward<T, ACT, 1>(c, x, y, h, g, u, save) : thin_forward<T, ACT, 2>(c, x, y, h, g, u, save);
     const TileGrid first(c.n, tiles(c.s.hidden, kTile / 2), tiles(c.s.rows, kTile)), second(c.n, tiles(c.s.width, kTile), tiles(c.s.rows, kTile));
     if (first.total < 0 || second.total < 0) return SVGD_ERR_TOO_LARGE;
     if (save) gate_up_kernel<T, ACT, true><<<first.blocks(), 256, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, g, u);
@@ -50,11 +77,15 @@ int backward(const Call &c, const svgd_rows &dy, const svgd_rows &x, const float
     const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0), high = (int)tiles(c.s.hidden, kTile);
     const TileGrid gate_up(c.n, tiles(c.s.width, kTile), (int64_t)high * gates), down(c.n, tiles(c.s.hidden, kTile), tiles(c.s.width, kTile));
     if (hidden.total < 0 || input.total < 0 || gate_up.total < 0 || down.total < 0) return SVGD_ERR_TOO_LARGE;
-    if (c.s.rows > 0 && (dx.data || gates)) {
+    const bool thin = c.s.rows <= kThinRows;
+    if (thin && c.s.rows > 0 && (dx.data || gates)) {
+        if (const int rc = c.s.rows <= 16 ? thin_backward<T, ACT, 1>(c, dy, g, u, dx, dg, du) : thin_backward<T, ACT, 2>(c, dy, g, u, dx, dg, du)) return rc;
+    }
+    if (!thin && (dx.data || gates)) {
         hidden_grad_kernel<T, ACT><<<hidden.blocks(), 256, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
         if (const int rc = launched()) return rc;
     }
-    if (c.s.rows > 0 && dx.data) {
+    if (!thin && dx.data) {
         input_grad_kernel<T><<<input.blocks(), 256, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
         if (const int rc = launched()) return rc;
     }
