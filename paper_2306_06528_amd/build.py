@@ -1,5 +1,5 @@
 """Build the C-ABI library (csrc/*.hip -> libsvgd.so) for gfx950 with hipcc, and what Python calls it through
-(csrc/binding.cpp -> _binding.<ABI of this Python>.so, host code against torch's C++ interface)."""
+(csrc/*binding.cpp -> _binding.<ABI of this Python>.so, host code against torch's C++ interface)."""
 import glob
 import os
 import subprocess
@@ -9,6 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SOURCES = sorted(glob.glob(os.path.join(HERE, "csrc", "*.hip")))
+HOST_SOURCES = sorted(glob.glob(os.path.join(HERE, "csrc", "*.cpp")))
 LIB = os.path.join(HERE, "libsvgd.so")
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))  # (another Python does not take it for its own)
 
@@ -40,14 +41,14 @@ def build(verbose: bool = False) -> str:
     """Compile unconditionally, the sources side by side; returns the path of the library."""
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
-        with ThreadPoolExecutor(max_workers=min(len(SOURCES) + 1, os.cpu_count() or 1, 8)) as pool:
+        with ThreadPoolExecutor(max_workers=min(len(SOURCES) + len(HOST_SOURCES), os.cpu_count() or 1, 8)) as pool:
             compile_flags, link_flags = _binding_flags()
-            binding = os.path.join(tmp, "binding.o")
-            host = pool.submit(_run, ["g++", *compile_flags, "-c", "-o", binding, os.path.join(HERE, "csrc", "binding.cpp")])
+            binding = [os.path.join(tmp, os.path.basename(s) + ".o") for s in HOST_SOURCES]
+            host = [pool.submit(_run, ["g++", *compile_flags, "-c", "-o", o, s]) for s, o in zip(HOST_SOURCES, binding)]
             outs = list(pool.map(lambda so: _run(["hipcc", *HIPCC_FLAGS, "-c", "-o", so[1], so[0]]), zip(SOURCES, objects)))
-            outs.append(host.result())
+            outs += [h.result() for h in host]
         outs.append(_run(["hipcc", *HIPCC_FLAGS, "-shared", "-o", LIB, *objects]))
-        outs.append(_run(["g++", "-shared", "-o", BINDING, binding, *link_flags]))
+        outs.append(_run(["g++", "-shared", "-o", BINDING, *binding, *link_flags]))
     if verbose:
         for out in outs:
             if out.strip():

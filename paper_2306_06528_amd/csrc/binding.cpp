@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/svgd.h"
+#include "layers_binding.hpp"
 
 namespace {
 
@@ -255,7 +256,8 @@ PyObject *step_rows(PyObject *, PyObject *const *a, Py_ssize_t na)
 }
 
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(step), METHOD(phi), METHOD(step_static), METHOD(step_rows), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {METHOD(step), METHOD(phi), METHOD(step_static), METHOD(step_rows), METHOD(layer_norm_forward), METHOD(layer_norm_backward),
+                         METHOD(gated_ffn_forward), METHOD(gated_ffn_backward), METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
