@@ -47,7 +47,7 @@ template <class F> int for_type(int dtype, F f)
 }
 
 // The rows of a particle in at most about `most` / n workgroups, each a multiple of the rows that it has at a time.
-NormShape split_rows(int n, int64_t rows, int64_t width, int most)
+NormShape split_rows(int n, int64_t rows, int64_t width, int64_t most)
 {
     const Team t = team_for(width);
     const int64_t at_a_time = (t.threads > 256 ? t.threads : 256) / t.threads;
@@ -57,7 +57,28 @@ NormShape split_rows(int n, int64_t rows, int64_t width, int most)
     if (per < 1) per = 1;
     return {rows, (int)width, (int)((rows + per - 1) / per), per};
 }
-constexpr int kForwardBlocks = 256 * 8, kBackwardBlocks = 256 * 4;
+
+// Forward: up to 4,096 workgroups, but beyond 512 two turns for each, so that the second row's load hides behind the first's
+// sums (16 x 200 x 64 fp32, 100 turns: 3.0 us one by one, 4.1 two by two).  us at 1,024 / 2,048 / 4,096: 16 x 8,192 x 1,024 bf16 110 / 110 / 104, 8 x 1,576 x 384 bf16 (3,152 turns) 9.1 / 8.2 / 8.8, 5 x 1,003 x 1,001 fp32
+// (1,255 turns) 10.0 / 11.9 / 11.8.
+NormShape forward_split(int n, int64_t rows, int64_t width)
+{
+    const Team t = team_for(width);
+    const int64_t turns = n * rows * t.threads / (t.threads > 256 ? t.threads : 256);
+    return split_rows(n, rows, width, turns / 2 > 4096 ? 4096 : turns / 2 > 512 ? turns / 2 : 512);
+}
+
+// Backward: as many workgroups as run at a time, by their registers: four per CU, two with 16 values per thread, one of 1,024
+// threads; fewer partial sums are left then.  Activations that the memory-side cache does not hold like one per CU better.
+// us at 256 / 512 / 1,024: 8 x 1,576 x 384 bf16 24 / 18 / 15, 5 x 1,003 x 1,001 fp32 19 / 17.5 / 21, 16 x 8,192 x 1,024 bf16 (805 MB)
+// 157 / 163 / 171, 8 x 16,384 x 256 bf16 (201 MB) 40 / 34 / 35.  (At four bytes
+// per value: their type is not known where scratch memory is asked for.)
+NormShape backward_split(int n, int64_t rows, int64_t width)
+{
+    const Team t = team_for(width);
+    const bool big = n * rows * width * 4 > (int64_t)256 << 20;
+    return split_rows(n, rows, width, big || t.threads > 256 ? 256 : t.values > 8 ? 512 : 1024);
+}
 
 template <class T> ActRows<const T> in(const svgd_rows &r) { return {(const T *)r.data, r.particle_stride, r.row_stride}; }
 template <class T> ActRows<T> out(const svgd_rows &r) { return {(T *)r.data, r.particle_stride, r.row_stride}; }
@@ -94,7 +115,7 @@ int svgd_layer_norm_forward(int dtype, int n, int64_t rows, int64_t width, svgd_
         for (int o = 0; o < a; ++o)
             if (written[a].meets(written[o])) return SVGD_ERR_INVALID_ARG;
     }
-    const NormShape s = split_rows(n, rows, width, kForwardBlocks);
+    const NormShape s = forward_split(n, rows, width);
     return for_type(dtype, [&](auto t) {
         return for_team(width, [&](auto l, auto e) {
             using T = decltype(t);
@@ -108,7 +129,7 @@ int svgd_layer_norm_forward(int dtype, int n, int64_t rows, int64_t width, svgd_
 size_t svgd_layer_norm_scratch(int n, int64_t rows, int64_t width)
 {
     if (check_sizes(SVGD_F32, n, rows, width, SVGD_LAYER_MAX_NORM)) return 0;
-    return (size_t)n * split_rows(n, rows, width, kBackwardBlocks).blocks * 2 * (size_t)width * 4;
+    return (size_t)n * backward_split(n, rows, width).blocks * 2 * (size_t)width * 4;
 }
 
 int svgd_layer_norm_backward(int dtype, int n, int64_t rows, int64_t width, svgd_rows dy, svgd_rows x, const float *weight, int64_t weight_stride,
@@ -121,7 +142,7 @@ int svgd_layer_norm_backward(int dtype, int n, int64_t rows, int64_t width, svgd
     for (const Params *g : {&dw, &db})
         if (g->p && (!valid_params(*g, n, true) || params_meet(*g, w, n))) return SVGD_ERR_INVALID_ARG;
     if (dw.p && db.p && params_meet(dw, db, n)) return SVGD_ERR_INVALID_ARG;
-    const NormShape s = split_rows(n, rows, width, kBackwardBlocks);
+    const NormShape s = backward_split(n, rows, width);
     const bool params = dw.p || db.p;
     if (rows > 0) {
         const size_t need = params ? svgd_layer_norm_scratch(n, rows, width) : 0, stats = (size_t)n * rows * 4;
@@ -153,7 +174,7 @@ int svgd_layer_norm_backward(int dtype, int n, int64_t rows, int64_t width, svgd
     }
     if (!params || (rows == 0 && accumulate)) return SVGD_OK;
     const int groups = (int)((2 * width + 63) / 64);
-    norm_reduce_kernel<<<n * groups, 256, 0, (hipStream_t)stream>>>((const float *)scratch, rows > 0 ? s.blocks : 0, (int)width, groups, dw, db,
+    norm_reduce_kernel<<<n * groups, 64 * kReduceWaves, 0, (hipStream_t)stream>>>((const float *)scratch, rows > 0 ? s.blocks : 0, (int)width, groups, dw, db,
                                                                     accumulate != 0);
     return launched();
 }

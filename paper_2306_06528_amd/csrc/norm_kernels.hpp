@@ -49,6 +49,29 @@ template <class T> struct ActRows {
     int64_t particle, row;
 };
 
+// A thread's part of a row, as it comes from memory; packs beyond the width (`left` of the first pack on) count as 0.
+template <class T, int L, int E> struct RowPart {
+    static constexpr int VEC = 16 / sizeof(T), C = E / VEC;
+    typename Pack<T, VEC>::raw v[C];
+    __device__ __forceinline__ void load(const T *row, int lane, int width)
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * L + lane) * VEC;
+            if (col + VEC <= width) {
+                v[c] = *reinterpret_cast<const typename Pack<T, VEC>::type *>(row + col);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    v[c][e] = (T)0.f;
+                    if (col + e < width) v[c][e] = row[col + e];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float operator()(int c, int e) const { return (float)v[c][e]; }
+};
+
 template <class T, int L, int E>
 __global__ __launch_bounds__(kTeamBlock<L>) void norm_forward_kernel(NormShape s, ActRows<const T> x, Params weight, Params bias, float eps, ActRows<T> y,
                                                                      float *mean_out, float *rstd_out)
@@ -72,17 +95,21 @@ __global__ __launch_bounds__(kTeamBlock<L>) void norm_forward_kernel(NormShape s
         for (int e = 0; e < VEC; ++e) b[c * VEC + e] = v[e];
     }
     const float inv = 1.f / (float)s.width;
+    RowPart<T, L, E> next; // the next row is on its way while one is worked on
+    const T *const rows = x.p + particle * x.particle;
+    next.load(rows + (first + team) * x.row, lane, first + team < last ? s.width : 0);
     for (int64_t r0 = first; r0 < last; r0 += kTeams<L>) {
         const int64_t r = r0 + team;
         const bool live = r < last;
         float v[C][VEC], total = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * L + lane) * VEC;
-            load_pack<T, VEC>(x.p + particle * x.particle + r * x.row + col, live ? s.width - col : 0, v[c]);
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) total += v[c][e];
-        }
+            for (int e = 0; e < VEC; ++e) {
+                v[c][e] = next(c, e);
+                total += v[c][e];
+            }
+        if (r0 + kTeams<L> < last) next.load(rows + (r + kTeams<L>) * x.row, lane, r + kTeams<L> < last ? s.width : 0);
         const float mean = sum(total) * inv;
         float square = 0.f;
 #pragma unroll
@@ -131,17 +158,29 @@ __global__ __launch_bounds__(kTeamBlock<L>) void norm_backward_kernel(NormShape 
         for (int e = 0; e < VEC; ++e) dw[c][e] = db[c][e] = 0.f;
     }
     const float inv = 1.f / (float)s.width;
+    RowPart<T, L, E> next_x, next_d; // the next row is on its way while one is worked on
+    float next_mean, next_rstd;
+    const auto fetch = [&](int64_t r) {
+        const bool live = r < last;
+        next_x.load(x.p + particle * x.particle + r * x.row, lane, live ? s.width : 0);
+        next_d.load(dy.p + particle * dy.particle + r * dy.row, lane, live ? s.width : 0);
+        next_mean = live ? mean_in[particle * s.rows + r] : 0.f;
+        next_rstd = live ? rstd_in[particle * s.rows + r] : 0.f;
+    };
+    fetch(first + team);
     for (int64_t r0 = first; r0 < last; r0 += kTeams<L>) {
         const int64_t r = r0 + team;
         const bool live = r < last;
-        const float mean = live ? mean_in[particle * s.rows + r] : 0.f, rstd = live ? rstd_in[particle * s.rows + r] : 0.f;
+        const float mean = next_mean, rstd = next_rstd;
         float v[C][VEC], d[C][VEC], sa = 0.f, sax = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * L + lane) * VEC, left = live ? s.width - col : 0;
-            load_pack<T, VEC>(x.p + particle * x.particle + r * x.row + col, left, v[c]);
-            load_pack<T, VEC>(dy.p + particle * dy.particle + r * dy.row + col, left, d[c]);
-        }
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                v[c][e] = next_x(c, e);
+                d[c][e] = next_d(c, e);
+            }
+        if (r0 + kTeams<L> < last) fetch(r + kTeams<L>);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -194,25 +233,38 @@ __global__ __launch_bounds__(kTeamBlock<L>) void norm_backward_kernel(NormShape 
     }
 }
 
-// Sums of a particle's partials, in the same order every time: 64 columns per workgroup, its four waves take every fourth
-// partial and their sums are added in order.
-__global__ __launch_bounds__(256) void norm_reduce_kernel(const float *partials, int blocks, int width, int column_groups, Params dweight, Params dbias,
-                                                          bool accumulate)
+// Sums of a particle's partials, in the same order every time: 64 columns per workgroup, its sixteen waves take every
+// sixteenth partial, four of them in flight, and their sums are added in order.
+constexpr int kReduceWaves = 16;
+__global__ __launch_bounds__(64 * kReduceWaves) void norm_reduce_kernel(const float *partials, int blocks, int width, int column_groups, Params dweight,
+                                                                        Params dbias, bool accumulate)
 {
-    __shared__ double sums[4][64];
+    __shared__ double sums[kReduceWaves][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t particle = blockIdx.x / column_groups;
     const int col = (blockIdx.x % column_groups) * 64 + lane; // of 2 * width
     double total = 0.0;
-    if (col < 2 * width)
-        for (int b = wave; b < blocks; b += 4) total += (double)partials[((particle * blocks + b) * 2) * (int64_t)width + col];
+    if (col < 2 * width) {
+        const float *const p = partials + particle * blocks * 2 * (int64_t)width + col;
+        int b = wave;
+        for (; b + 3 * kReduceWaves < blocks; b += 4 * kReduceWaves) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = p[(int64_t)(b + k * kReduceWaves) * 2 * width];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) total += (double)v[k];
+        }
+        for (; b < blocks; b += kReduceWaves) total += (double)p[(int64_t)b * 2 * width];
+    }
     sums[wave][lane] = total;
     __syncthreads();
     if (wave != 0 || col >= 2 * width) return;
     const Params &out = col < width ? dweight : dbias;
     if (!out.p) return;
     float *const p = const_cast<float *>(out.p) + particle * out.stride + (col < width ? col : col - width);
-    const double v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    double v = 0.0;
+#pragma unroll
+    for (int w = 0; w < kReduceWaves; ++w) v += sums[w][lane];
     *p = (float)(accumulate ? v + (double)*p : v);
 }
 
