@@ -17,20 +17,29 @@
 
 namespace svgd {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr int kTileK = 32; // columns of both operands per step
 
-constexpr int kTile = 128;  // rows of A and of B per workgroup
-constexpr int kTileK = 32;  // columns of both per step
+// A workgroup of W waves computes 64 W values of i and 16 NJ of j, each wave 64 of i and all of j.
+template <int W, int NJ> struct Tile {
+    static constexpr int kWaves = W, kBlocksJ = NJ, kThreads = 64 * W, kI = 64 * W, kJ = 16 * NJ;
+    static constexpr int kPlane = kJ * 4; // 16-byte units of one part of B's rows
+};
 
 template <class T> constexpr int kParts = 3;
 template <> constexpr int kParts<f16_t> = 2;
 template <> constexpr int kParts<bf16_t> = 1;
 
-// An operand's tile in LDS: one plane per part, each kTile rows of four 16-byte units (8 values of k).  Two rows share 128
-// bytes; which half a row takes and where its units lie in it is permuted so that neither 8 rows in succession nor 8
-// every-second rows (what eight lanes read or write at a time) meet in a bank.
-constexpr int kPlane = kTile * 4; // units
+// B's rows in LDS, one plane per part, each row four 16-byte units (8 values of k).  Two rows share 128 bytes; which half a row takes
+// and where its units lie in it is permuted so that neither 8 rows in succession nor 8 every-second rows (what eight
+// lanes write at a time) meet in a bank.
 __device__ __forceinline__ int unit_of(int row, int kg) { return (row >> 1) * 8 + (((row ^ (row >> 3)) & 1) << 2) + (kg ^ ((row >> 1) & 3)); }
+
+// The order of k within a step: group g of 8 values that one lane hands to a matrix instruction has 4 g .. 4 g + 3 and 16 more than
+// these, in A as in B.  Four lanes then read 64 bytes of an fp32 row side by side.
+__device__ __forceinline__ constexpr int k_of(int g, int e) { return 4 * g + (e & 3) + 16 * (e >> 2); }
+
+// The wave's number, known to be the same in all its lanes.
+__device__ __forceinline__ int wave_of_block() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 template <int P>
 __device__ __forceinline__ void split_parts(f32x4 a, f32x4 b, const SplitConst &sc, bf16x8 (&out)[P])
@@ -70,156 +79,354 @@ __device__ __forceinline__ void to_parts(const T (&v)[8], const SplitConst &sc, 
     }
 }
 
-// An operand whose k is contiguous in memory: each thread brings 8 values of k of rows tid / 4 and tid / 4 + 64.
-template <class T, int P> struct AlongK {
-    const T *row[2];
-    T v[2][8];
-    template <class F> __device__ __forceinline__ AlongK(F row_start)
+// A, whose rows no other wave of the workgroup needs, goes from memory to the registers of the matrix instructions without LDS.
+// Instruction block ib (of four) has rows 4 quad(m) + ib of the wave's 64, m = 0 .. 15; lane l holds m = l % 16, k of group l / 16.  Since a
+// lane's results are those of m = 4 (l / 16) + r, r = 0 .. 3, their quads are l / 16 + 4 r: four lanes have 16 results side by side, 64 bytes.
+// `fetch` brings a whole step and has no branch, so that it can lie among the matrix instructions; `fetch_any` brings
+// any step, value by value, columns from K on as 0 and unread.
+
+__device__ __forceinline__ int quad_of_lane() { return ((threadIdx.x & 15) >> 2) + 4 * (threadIdx.x & 3); }
+
+// K contiguous in memory, fp32.  The vector memory unit joins what 16 lanes in a row read, and those of the matrix instructions'
+// layout read 16 rows: 64 accesses for each load, which kept it busy 86 % of the time.  So eight lanes read 128 bytes of a row, and
+// the values change lanes in the wave's own part of LDS, kScratch floats, as they are.
+template <int P, int STEP> struct RowsOfA { // STEP: 2 where the groups of 8 rows are of gate and up by turns
+    const float *from[2]; // of even and of odd groups of 8 rows: the wave's first row there
+    int last;             // rows beyond this one: this one again
+    uint32_t row_bytes;   // below 2^24
+    f32x4 v[8];
+    static constexpr bool narrow = false;
+    __device__ __forceinline__ RowsOfA(const float *even, const float *odd, int64_t rows_left, int64_t width)
+        : last(rows_left < 64 ? (int)rows_left - 1 : 63), row_bytes((uint32_t)width * 4)
     {
-        row[0] = row_start(threadIdx.x >> 2);
-        row[1] = row_start((threadIdx.x >> 2) + 64);
+        from[0] = even;
+        from[1] = odd;
     }
-    // Columns k0 .. k0 + 31; those from K on count as 0 and are not read.
-    __device__ __forceinline__ void fetch(int64_t k0, int64_t K)
+    static __device__ __forceinline__ int row_of(int n) { return 8 * n + ((threadIdx.x & 63) >> 3); }
+    static __device__ __forceinline__ int place(int row, int piece) { return row * 8 + (piece ^ (((row >> 4) & 3) | (row & 4))); } // in 16 bytes
+    // Two instructions each time rather than eight registers: `row` is the lane's, hidden from the compiler.
+    __device__ __forceinline__ uint32_t offset(int n, int row) const
     {
-        const int64_t k = k0 + (threadIdx.x & 3) * 8;
-        if (k0 + kTileK <= K) {
+        const int r = 8 * (n / STEP) + row;
+        return __umul24(r < last ? r : last, row_bytes) + 16 * (threadIdx.x & 7);
+    }
+    __device__ __forceinline__ void fetch(int64_t k0)
+    {
+        int row = (threadIdx.x & 63) >> 3;
+        asm volatile("" : "+v"(row));
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                constexpr int W = 16 / sizeof(T);
-#pragma unroll
-                for (int q = 0; q < 8; q += W) {
-                    const typename Pack<T, W>::raw r = *reinterpret_cast<const typename Pack<T, W>::type *>(row[t] + k + q);
-#pragma unroll
-                    for (int e = 0; e < W; ++e) v[t][q + e] = r[e];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const T x = row[t][k + e < K ? k + e : K - 1];
-                    v[t][e] = k + e < K ? x : (T)0.f;
-                }
+        for (int n = 0; n < 8; ++n) {
+            const char *const p = reinterpret_cast<const char *>(from[n & (STEP - 1)] + k0);
+            v[n] = *reinterpret_cast<const f32x4u *>(p + offset(n, row));
         }
+    }
+    __device__ __forceinline__ void fetch_any(int64_t k0, int64_t K)
+    {
+        const int64_t k = k0 + 4 * (threadIdx.x & 7);
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const float *const row = reinterpret_cast<const float *>(reinterpret_cast<const char *>(from[n & (STEP - 1)]) + offset(n, (threadIdx.x & 63) >> 3)) - 4 * (threadIdx.x & 7);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = row[k + e < K ? k + e : K - 1];
+                v[n][e] = k + e < K ? x : 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ void stage(float *scratch) const
+    {
+        f32x4 *const s = reinterpret_cast<f32x4 *>(scratch);
+        wave_sync(); // (the step before has been read)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) s[place(row_of(n), threadIdx.x & 7)] = v[n];
+        wave_sync();
+    }
+    __device__ __forceinline__ void parts(int ib, const SplitConst &sc, bf16x8 (&out)[P], const float *scratch) const
+    {
+        const f32x4 *const s = reinterpret_cast<const f32x4 *>(scratch);
+        const int row = 4 * quad_of_lane() + ib, g = (threadIdx.x & 63) >> 4;
+        split_parts<P>(s[place(row, g)], s[place(row, g + 4)], sc, out);
+    }
+};
+
+// The rows contiguous in memory, `count` of them, k after k `stride` apart: a lane's four rows are one load.  Where
+// these end beyond the last row they are the last four instead (quad_of says which).
+constexpr int64_t kFarStride = (int64_t)1 << 22;
+__device__ __forceinline__ int64_t quad_of(int64_t i, int64_t count) { return i + 4 <= count ? i : count - 4; }
+
+template <class T, int P> struct ColumnsOfA {
+    const T *base;   // row 0
+    int64_t stride;  // beyond kFarStride every step goes the slow way: a lane's offset is to fit 32 bits
+    uint32_t column; // the lane's first row (fewer than four rows: the first one)
+    int rows;        // of them, if they are fewer than four; otherwise 4
+    bool narrow;
+    typename Pack<T, 4>::raw v[8];
+    __device__ __forceinline__ ColumnsOfA(const T *b, int64_t s, int64_t first, int64_t count)
+        : base(b), stride(s), column(count < 4 ? 0 : (uint32_t)quad_of(first + 4 * quad_of_lane(), count)), rows(count < 4 ? (int)count : 4),
+          narrow(count < 4 || s > kFarStride)
+    {
+    }
+    __device__ __forceinline__ void fetch(int64_t k0)
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+        const uint32_t offset = (column + 4 * g * (uint32_t)stride) * (uint32_t)sizeof(T);
+        const char *const from = reinterpret_cast<const char *>(base + k0 * stride);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = *reinterpret_cast<const typename Pack<T, 4>::type *>(from + k_of(0, e) * stride * (int64_t)sizeof(T) + offset);
+    }
+    __device__ __forceinline__ void fetch_any(int64_t k0, int64_t K)
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t k = k0 + k_of(g, e);
+            const T *const line = base + (k < K ? k : K - 1) * stride + column;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const T x = line[t < rows ? t : rows - 1];
+                v[e][t] = k < K ? x : (T)0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ void stage(float *) const {}
+    __device__ __forceinline__ void parts(int ib, const SplitConst &sc, bf16x8 (&out)[P], const float *) const
+    {
+        T x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = v[e][ib];
+        to_parts<T, P>(x, sc, out);
+    }
+};
+
+// B goes through LDS, each thread bringing 8 values of k of some rows.  K contiguous in memory: rows tid / 4 + 16 W t, again from the
+// first one on where there are not so many (twice the same values to the same place, but no branch).
+template <class TL, class T, int P> struct RowsOfB {
+    static constexpr int N = (TL::kBlocksJ + TL::kWaves - 1) / TL::kWaves;
+    static __device__ __forceinline__ int row_of(int t)
+    {
+        const int r = (threadIdx.x >> 2) + 16 * TL::kWaves * t;
+        return N * TL::kWaves == TL::kBlocksJ || r < TL::kJ ? r : r - TL::kJ;
+    }
+    const T *base;  // the tile's first row
+    int64_t stride; // beyond kFarStride the slow way, as above
+    int last;       // rows beyond this one: this one again
+    bool narrow;
+    T v[N][8];
+    __device__ __forceinline__ RowsOfB(const T *b, int64_t s, int64_t rows_left)
+        : base(b), stride(s), last(rows_left < TL::kJ ? (int)rows_left - 1 : TL::kJ - 1), narrow(s > kFarStride)
+    {
+    }
+    __device__ __forceinline__ int source(int t) const { return row_of(t) < last ? row_of(t) : last; }
+    __device__ __forceinline__ void fetch(int64_t k0)
+    {
+        const int g = threadIdx.x & 3;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const uint32_t offset = ((uint32_t)source(t) * (uint32_t)stride + k_of(g, 0)) * (uint32_t)sizeof(T);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const char *const from = reinterpret_cast<const char *>(base + k0 + k_of(0, 4 * q));
+                const typename Pack<T, 4>::raw r = *reinterpret_cast<const typename Pack<T, 4>::type *>(from + offset);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[t][4 * q + e] = r[e];
+            }
+        }
+    }
+    __device__ __forceinline__ void fetch_any(int64_t k0, int64_t K)
+    {
+        const int g = threadIdx.x & 3;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t k = k0 + k_of(g, e);
+                const T x = base[source(t) * stride + (k < K ? k : K - 1)];
+                v[t][e] = k < K ? x : (T)0.f;
+            }
     }
     __device__ __forceinline__ void store(bf16x8 *lds, const SplitConst &sc) const
     {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < N; ++t) {
             bf16x8 parts[P];
             to_parts<T, P>(v[t], sc, parts);
-            const int u = unit_of((threadIdx.x >> 2) + 64 * t, threadIdx.x & 3);
+            const int u = unit_of(row_of(t), threadIdx.x & 3);
 #pragma unroll
-            for (int p = 0; p < P; ++p) lds[p * kPlane + u] = parts[p];
+            for (int p = 0; p < P; ++p) lds[p * TL::kPlane + u] = parts[p];
         }
     }
 };
 
-// An operand whose rows are contiguous in memory, k after k `stride` apart: each thread brings rows 2 l and 2 l + 1, l its
-// lane, of 8 values of k, one such group per wave.  `count`: how many of the tile's rows there are.
-template <class T, int P> struct AcrossK {
-    const T *base;
-    int64_t stride;
-    int count;
-    T v[2][8];
-    __device__ __forceinline__ AcrossK(const T *b, int64_t s, int64_t left) : base(b), stride(s), count(left < kTile ? (int)left : kTile) {}
-    __device__ __forceinline__ void fetch(int64_t k0, int64_t K)
+// Rows contiguous, `count` of them, k after k `stride` apart: two rows, the tile's 2 l and 2 l + 1, and one group of 8 values of k at a
+// time.  A pair that ends beyond the last row is loaded one row earlier; its first row is then the second one loaded.
+template <class TL, class T, int P> struct ColumnsOfB {
+    static constexpr int kPairs = TL::kJ / 2, kAtATime = TL::kThreads / kPairs, N = (4 + kAtATime - 1) / kAtATime;
+    static_assert(kAtATime >= 1, "a thread for every pair");
+    const T *base;   // row 0
+    int64_t stride;  // beyond kFarStride the slow way, as above
+    uint32_t column; // the first row of the thread's pair
+    bool late, single, narrow;
+    T v[N][2][8];
+    __device__ __forceinline__ ColumnsOfB(const T *b, int64_t s, int64_t first, int64_t count)
+        : base(b), stride(s), single(count < 2), narrow(count < 2 || s > kFarStride)
     {
-        const int r = 2 * (threadIdx.x & 63);
-        const int64_t k = k0 + (threadIdx.x >> 6) * 8;
-        if (k0 + kTileK <= K && count == kTile) {
+        const int64_t j = first + row();
+        late = j + 2 > count && !single;
+        column = single ? 0 : (uint32_t)(late ? count - 2 : j);
+    }
+    static __device__ __forceinline__ int row() { return 2 * (threadIdx.x % kPairs); }
+    static __device__ __forceinline__ int group(int t) { return (threadIdx.x / kPairs + t * kAtATime) & 3; } // (beyond the fourth: again)
+    __device__ __forceinline__ void fetch(int64_t k0)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const uint32_t offset = (column + 4 * group(t) * (uint32_t)stride) * (uint32_t)sizeof(T);
+            const char *const from = reinterpret_cast<const char *>(base + k0 * stride);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const typename Pack<T, 2>::raw x = *reinterpret_cast<const typename Pack<T, 2>::type *>(base + (k + e) * stride + r);
-                v[0][e] = x[0];
-                v[1][e] = x[1];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const T *line = base + (k + e < K ? k + e : K - 1) * stride;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const T x = line[r + t < count ? r + t : count - 1];
-                    v[t][e] = k + e < K ? x : (T)0.f;
-                }
+                const typename Pack<T, 2>::raw x =
+                    *reinterpret_cast<const typename Pack<T, 2>::type *>(from + k_of(0, e) * stride * (int64_t)sizeof(T) + offset);
+                v[t][0][e] = x[0];
+                v[t][1][e] = x[1];
             }
         }
+    }
+    __device__ __forceinline__ void fetch_any(int64_t k0, int64_t K)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t k = k0 + k_of(group(t), e);
+                const T *const line = base + (k < K ? k : K - 1) * stride + column;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const T x = line[single ? 0 : q];
+                    v[t][q][e] = k < K ? x : (T)0.f;
+                }
+            }
     }
     __device__ __forceinline__ void store(bf16x8 *lds, const SplitConst &sc) const
     {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bf16x8 parts[P];
-            to_parts<T, P>(v[t], sc, parts);
-            const int u = unit_of(2 * (threadIdx.x & 63) + t, threadIdx.x >> 6);
+        for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int p = 0; p < P; ++p) lds[p * kPlane + u] = parts[p];
-        }
+            for (int q = 0; q < 2; ++q) {
+                T x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = q == 0 && late ? v[t][1][e] : v[t][q][e];
+                bf16x8 parts[P];
+                to_parts<T, P>(x, sc, parts);
+                const int u = unit_of(row() + q, group(t));
+#pragma unroll
+                for (int p = 0; p < P; ++p) lds[p * TL::kPlane + u] = parts[p];
+            }
     }
 };
 
-// The wave's 64 x 64 values of C: block (ib, jb) of 32 x 32, in it value r of a lane is
-// i = 8 (r / 4) + 4 (lane / 32) + r % 4, j = lane % 32.
-struct Acc {
-    f32x16 c[2][2];
+// The wave's 64 x 16 NJ values of C: in block (ib, jb) value r of lane l is i = 4 (l / 16) + 16 r + ib, j = 16 jb + l % 16.
+template <int NJ> struct Acc {
+    f32x4 c[4][NJ];
     __device__ __forceinline__ Acc()
     {
 #pragma unroll
-        for (int a = 0; a < 2; ++a)
+        for (int a = 0; a < 4; ++a)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) c[a][b] = f32x16{};
+            for (int b = 0; b < NJ; ++b) c[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 };
 
 // Adds the product over K columns to acc.  Products of parts pa, pb with pa + pb beyond the last part are below 2^-24
-// (three parts; 2^-16 with two) of the whole and left out.
-template <int PA, int PB, class LA, class LB>
-__device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t K, Acc &acc, bf16x8 *lds)
+// (three parts; 2^-16 with two) of the whole and left out.  While the matrix cores work on a step, the next one's rows are
+// on their way, those of B then go to the other half of LDS, and those of A are split into the registers of the last
+// columns' blocks as these get free: one barrier per step, and nothing but it between one step's products and the next one's.
+// lds: 2 * PB * kPlane units; scratch: the wave's own kScratch floats.
+constexpr int kScratch = 64 * kTileK; // 64 rows of a step of A; 16 rows of 68 values of C
+template <class TL, int PA, int PB, class LA, class LB>
+__device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t K, Acc<TL::kBlocksJ> &acc, bf16x8 *lds, float *scratch)
 {
-    constexpr int kOrder = (PA > PB ? PA : PB) - 1;
+    constexpr int kOrder = (PA > PB ? PA : PB) - 1, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
+    constexpr int kLast = PB == 1 ? 2 : 1;
+    static_assert(NJ / 2 <= NJ - kLast, "every column once");
     const SplitConst sc = split_const();
-    bf16x8 *const lds_b = lds + PA * kPlane;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wi = wave & 1, wj = wave >> 1;
-    const int frag[2] = {unit_of(lane & 31, lane >> 5), unit_of(lane & 31, 2 + (lane >> 5))};
-    if (K > 0) {
-        a.fetch(0, K);
-        b.fetch(0, K);
-    }
-    for (int64_t k0 = 0; k0 < K; k0 += kTileK) {
-        __syncthreads(); // the step before has been read
-        a.store(lds, sc);
-        b.store(lds_b, sc);
-        __syncthreads();
-        if (k0 + kTileK < K) {
-            a.fetch(k0 + kTileK, K);
-            b.fetch(k0 + kTileK, K);
-        }
+    const int lane = threadIdx.x & 63;
+    const int frag = unit_of(lane & 15, lane >> 4);
+    bf16x8 fa[4][PA];
+    int stage = 0;
+    const auto columns = [&](int first, int last) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            bf16x8 fa[2][PA], fb[2][PB];
+        for (int jb = first; jb < last; ++jb) {
+            bf16x8 fb[PB];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                for (int p = 0; p < PA; ++p) fa[q][p] = lds[p * kPlane + (wi * 64 + q * 32) * 4 + frag[s]];
-#pragma unroll
-                for (int p = 0; p < PB; ++p) fb[q][p] = lds_b[p * kPlane + (wj * 64 + q * 32) * 4 + frag[s]];
-            }
+            for (int p = 0; p < PB; ++p) fb[p] = lds[stage + p * TL::kPlane + jb * 64 + frag];
 #pragma unroll
             for (int pa = 0; pa < PA; ++pa)
 #pragma unroll
                 for (int pb = 0; pb < PB; ++pb)
                     if (pa + pb <= kOrder) {
 #pragma unroll
-                        for (int ib = 0; ib < 2; ++ib)
-#pragma unroll
-                            for (int jb = 0; jb < 2; ++jb)
-                                acc.c[ib][jb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[ib][pa], fb[jb][pb], acc.c[ib][jb], 0, 0, 0);
+                        for (int ib = 0; ib < 4; ++ib)
+                            acc.c[ib][jb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[ib][pa], fb[pb], acc.c[ib][jb], 0, 0, 0);
                     }
         }
+    };
+    const int64_t whole = a.narrow || b.narrow ? 0 : K / kTileK * kTileK;
+    if (whole > 0) {
+        b.fetch(0);
+        a.fetch(0);
+        __syncthreads(); // (an earlier product's last step has been read)
+        b.store(lds, sc);
+        a.stage(scratch);
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) a.parts(ib, sc, fa[ib], scratch);
+        __syncthreads();
+        for (int64_t k0 = kTileK; k0 < whole; k0 += kTileK) {
+            b.fetch(k0);
+            __builtin_amdgcn_sched_barrier(0); // (the compiler would move the loads down to where their values are needed)
+            columns(0, NJ / 2 - 1);
+            b.store(lds + (kStage - stage), sc);
+            __builtin_amdgcn_sched_barrier(0);
+            a.fetch(k0);
+            __builtin_amdgcn_sched_barrier(0);
+            columns(NJ / 2 - 1, NJ - kLast);
+            __builtin_amdgcn_sched_barrier(0); // (and up to here what waits for A's)
+            a.stage(scratch);
+            bf16x8 fb[kLast][PB];
+#pragma unroll
+            for (int q = 0; q < kLast; ++q)
+#pragma unroll
+                for (int p = 0; p < PB; ++p) fb[q][p] = lds[stage + p * TL::kPlane + (NJ - kLast + q) * 64 + frag];
+#pragma unroll
+            for (int ib = 0; ib < 4; ++ib) {
+#pragma unroll
+                for (int pa = 0; pa < PA; ++pa)
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+                        if (pa + pb <= kOrder) {
+#pragma unroll
+                            for (int q = 0; q < kLast; ++q)
+                                acc.c[ib][NJ - kLast + q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[ib][pa], fb[q][pb], acc.c[ib][NJ - kLast + q], 0, 0, 0);
+                        }
+                a.parts(ib, sc, fa[ib], scratch);
+            }
+            stage = kStage - stage;
+            __syncthreads();
+        }
+        columns(0, NJ);
+    }
+#pragma unroll 1
+    for (int64_t k0 = whole; k0 < K; k0 += kTileK) {
+        b.fetch_any(k0, K);
+        a.fetch_any(k0, K);
+        __syncthreads();
+        stage = 0;
+        b.store(lds, sc);
+        a.stage(scratch);
+#pragma unroll
+        for (int ib = 0; ib < 4; ++ib) a.parts(ib, sc, fa[ib], scratch);
+        __syncthreads();
+        columns(0, NJ);
     }
 }
 
@@ -271,65 +478,94 @@ template <class T> struct Rows {
     int64_t particle, row; // strides
 };
 
-// calls f(i, j, quad) for every four values of C that a lane holds side by side: C[j][i .. i + 3] of the tile
-template <class F> __device__ __forceinline__ void each_quad(const Acc &acc, F f)
+// 16 columns j of the wave's C at a time go through its part of LDS, so that 16 lanes have 64 values of i of one j side by side.
+constexpr int kScratchRow = 68; // floats from one j to the next: eight of them meet in no bank
+template <int NJ> __device__ __forceinline__ void spread(const Acc<NJ> &acc, int jb, float *scratch)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int i0 = (wave & 1) * 64 + 4 * (lane >> 5), j0 = (wave >> 1) * 64 + (lane & 31);
+    const int lane = threadIdx.x & 63;
+    wave_sync();
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
-#pragma unroll
-        for (int jb = 0; jb < 2; ++jb)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x16 &c = acc.c[ib][jb];
-                f(i0 + ib * 32 + q * 8, j0 + jb * 32, f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]});
-            }
+    for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4 *>(scratch + (lane & 15) * kScratchRow + 4 * (lane >> 4) + 16 * r) =
+            f32x4{acc.c[0][jb][r], acc.c[1][jb][r], acc.c[2][jb][r], acc.c[3][jb][r]};
+    wave_sync();
 }
 
-// Of the tile's 128 rows of A every wave's 64 are 32 of gate and the same 32 of up, so that a lane has g and u of
-// the same values.
-template <class T, int ACT, bool SAVE>
-__global__ __launch_bounds__(256, 2) void gate_up_kernel(FfnShape s, TileGrid grid, Rows<const T> x, Params gate, Params up, float *h, float *g_out,
-                                                         float *u_out)
+// calls f(i, j, quad, first) for every four values of C that lie side by side: C[j][i .. i + 3], of which those before `first`
+// are another lane's (COLUMNS, A's columns were loaded: at the end of the `count` values of i, see quad_of) and those from count on are not there.
+template <class TL, bool COLUMNS, class F>
+__device__ __forceinline__ void each_quad(const Acc<TL::kBlocksJ> &acc, int64_t i0, int64_t count, int64_t j0, float *scratch, F f)
 {
-    __shared__ bf16x8 lds[(3 + kParts<T>)*kPlane];
-    int particle, ti, tj;
-    if (!grid.at(particle, ti, tj)) return;
-    const float *const wg = gate.p + particle * gate.stride, *const wu = up.p + particle * up.stride;
-    const T *const xs = x.p + particle * x.particle;
-    const int64_t i0 = (int64_t)ti * (kTile / 2), j0 = (int64_t)tj * kTile;
-    AlongK<float, 3> a([&](int r) {
-        int64_t i = i0 + (r >> 6) * 32 + (r & 31);
-        if (i >= s.hidden) i = s.hidden - 1;
-        return ((r >> 5) & 1 ? wu : wg) + i * s.width;
-    });
-    AlongK<T, kParts<T>> b([&](int r) { return xs + (j0 + r < s.rows ? j0 + r : s.rows - 1) * x.row; });
-    Acc acc;
-    tile_product<3, kParts<T>>(a, b, s.width, acc, lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i = i0 + (wave & 1) * 32 + 4 * (lane >> 5);
+    const int lane = threadIdx.x & 63;
+    const int64_t i = i0 + 4 * (lane & 15);
 #pragma unroll
-    for (int jb = 0; jb < 2; ++jb) {
-        const int64_t j = j0 + (wave >> 1) * 64 + jb * 32 + (lane & 31);
-        if (j >= s.rows) continue;
-        const int64_t at = (particle * s.rows + j) * s.hidden_ld + i;
+    for (int jb = 0; jb < TL::kBlocksJ; ++jb) {
+        spread(acc, jb, scratch);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (i + 8 * q >= s.hidden_ld) continue; // (the columns from hidden to hidden_ld are never used)
-            f32x4 g, u, v;
+            const int j = 4 * q + (lane >> 4);
+            const f32x4 c = *reinterpret_cast<const f32x4 *>(scratch + j * kScratchRow + 4 * (lane & 15));
+            if (i < count) f(COLUMNS && count >= 4 ? quad_of(i, count) : i, j0 + 16 * jb + j, c, i);
+        }
+    }
+}
+
+// Values c[0 .. 3] to p[0 .. 3], those before `skip` and from `left` on left out.
+template <class T> __device__ __forceinline__ void store_quad(T *p, f32x4 c, int skip, int64_t left)
+{
+    if (skip == 0 && left >= 4) {
+        const float v[4] = {c[0], c[1], c[2], c[3]};
+        store_pack<T, 4>(p, 4, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e >= skip && e < left) p[e] = (T)c[e];
+    }
+}
+
+#define SVGD_TILE_KERNEL __global__ __launch_bounds__(TL::kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+
+// Of a wave's 64 rows of A every other 8 are of gate and the next 8 of up, the same 32 of both, so that the wave has g and u of the same
+// values.
+template <class TL, class T, int ACT, bool SAVE>
+SVGD_TILE_KERNEL void gate_up_kernel(FfnShape s, TileGrid grid, Rows<const T> x, Params gate, Params up, float *h, float *g_out, float *u_out)
+{
+    __shared__ bf16x8 lds[2 * kParts<T> * TL::kPlane];
+    __shared__ float scratches[TL::kWaves][kScratch];
+    float *const scratch = scratches[wave_of_block()];
+    int particle, ti, tj;
+    if (!grid.at(particle, ti, tj)) return;
+    const T *const xs = x.p + particle * x.particle;
+    const int lane = threadIdx.x & 63;
+    const int64_t i0 = (int64_t)ti * (TL::kI / 2) + wave_of_block() * 32, j0 = (int64_t)tj * TL::kJ;
+    const int64_t first = i0 < s.hidden ? i0 : s.hidden - 1;
+    RowsOfA<3, 2> a(gate.p + particle * gate.stride + first * s.width, up.p + particle * up.stride + first * s.width, s.hidden - first, s.width);
+    RowsOfB<TL, T, kParts<T>> b(xs + j0 * x.row, x.row, s.rows - j0);
+    Acc<TL::kBlocksJ> acc;
+    tile_product<TL, 3, kParts<T>>(a, b, s.width, acc, lds, scratch);
+    const int piece = lane & 7; // four values: in the wave's rows of C those of gate are 16 (piece / 2) + 4 (piece % 2) on, those of up 8 behind
+    const int64_t i = i0 + 4 * piece;
+#pragma unroll
+    for (int jb = 0; jb < TL::kBlocksJ; ++jb) {
+        spread(acc, jb, scratch);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int64_t j = j0 + 16 * jb + 8 * q + (lane >> 3);
+            const float *const c = scratch + (8 * q + (lane >> 3)) * kScratchRow + 16 * (piece >> 1) + 4 * (piece & 1);
+            const f32x4 g = *reinterpret_cast<const f32x4 *>(c), u = *reinterpret_cast<const f32x4 *>(c + 8);
+            if (j >= s.rows || i >= s.hidden_ld) continue; // (the columns from hidden to hidden_ld are never used)
+            const int64_t at = (particle * s.rows + j) * s.hidden_ld + i;
+            f32x4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                g[e] = acc.c[0][jb][4 * q + e];
-                u[e] = acc.c[1][jb][4 * q + e];
                 float act, slope;
                 activate<ACT>(g[e], act, slope);
                 v[e] = act * u[e];
             }
-            *reinterpret_cast<f32x4 *>(h + at + 8 * q) = v;
+            *reinterpret_cast<f32x4 *>(h + at) = v;
             if constexpr (SAVE) {
-                *reinterpret_cast<f32x4 *>(g_out + at + 8 * q) = g;
-                *reinterpret_cast<f32x4 *>(u_out + at + 8 * q) = u;
+                *reinterpret_cast<f32x4 *>(g_out + at) = g;
+                *reinterpret_cast<f32x4 *>(u_out + at) = u;
             }
         }
     }
@@ -338,44 +574,45 @@ __global__ __launch_bounds__(256, 2) void gate_up_kernel(FfnShape s, TileGrid gr
 // Two parts of each operand are enough where the result is rounded to 16 bits: what is left out is below 2^-16 of a product.
 template <class T> constexpr int kHiddenParts = sizeof(T) == 4 ? 3 : 2;
 
-template <class T>
-__global__ __launch_bounds__(256, 2) void down_kernel(FfnShape s, TileGrid grid, const float *h, Params down, Rows<T> y)
+template <class TL, class T> SVGD_TILE_KERNEL void down_kernel(FfnShape s, TileGrid grid, const float *h, Params down, Rows<T> y)
 {
     constexpr int P = kHiddenParts<T>;
-    __shared__ bf16x8 lds[2 * P * kPlane];
+    __shared__ bf16x8 lds[2 * P * TL::kPlane];
+    __shared__ float scratches[TL::kWaves][kScratch];
+    float *const scratch = scratches[wave_of_block()];
     int particle, ti, tj;
     if (!grid.at(particle, ti, tj)) return;
     const float *const w = down.p + particle * down.stride, *const hs = h + particle * s.rows * s.hidden_ld;
-    const int64_t i0 = (int64_t)ti * kTile, j0 = (int64_t)tj * kTile;
-    AlongK<float, P> a([&](int r) { return w + (i0 + r < s.width ? i0 + r : s.width - 1) * s.hidden; });
-    AlongK<float, P> b([&](int r) { return hs + (j0 + r < s.rows ? j0 + r : s.rows - 1) * s.hidden_ld; });
-    Acc acc;
-    tile_product<P, P>(a, b, s.hidden, acc, lds);
-    each_quad(acc, [&](int i, int j, f32x4 c) {
-        if (j0 + j >= s.rows || i0 + i >= s.width) return;
-        const float v[4] = {c[0], c[1], c[2], c[3]};
-        const int64_t left = s.width - i0 - i;
-        store_pack<T, 4>(y.p + particle * y.particle + (j0 + j) * y.row + i0 + i, left < 4 ? (int)left : 4, v);
+    const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
+    const int64_t first = iw < s.width ? iw : s.width - 1;
+    RowsOfA<P, 1> a(w + first * s.hidden, w, s.width - first, s.hidden);
+    RowsOfB<TL, float, P> b(hs + j0 * s.hidden_ld, s.hidden_ld, s.rows - j0);
+    Acc<TL::kBlocksJ> acc;
+    tile_product<TL, P, P>(a, b, s.hidden, acc, lds, scratch);
+    each_quad<TL, false>(acc, iw, s.width, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
+        if (j < s.rows) store_quad(y.p + particle * y.particle + j * y.row + i, c, (int)(first - i), s.width - i);
     });
 }
 
-template <class T, int ACT>
-__global__ __launch_bounds__(256, 2) void hidden_grad_kernel(FfnShape s, TileGrid grid, Rows<const T> dy, Params down, const float *g, const float *u,
-                                                             float *dg, float *du)
+template <class TL, class T, int ACT>
+SVGD_TILE_KERNEL void hidden_grad_kernel(FfnShape s, TileGrid grid, Rows<const T> dy, Params down, const float *g, const float *u, float *dg, float *du)
 {
-    __shared__ bf16x8 lds[(3 + kParts<T>)*kPlane];
+    __shared__ bf16x8 lds[2 * kParts<T> * TL::kPlane];
+    __shared__ float scratches[TL::kWaves][kScratch];
+    float *const scratch = scratches[wave_of_block()];
     int particle, ti, tj;
     if (!grid.at(particle, ti, tj)) return;
-    const int64_t i0 = (int64_t)ti * kTile, j0 = (int64_t)tj * kTile;
+    const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
     const T *const dys = dy.p + particle * dy.particle;
-    AcrossK<float, 3> a(down.p + particle * down.stride + i0, s.hidden, s.hidden - i0);
-    AlongK<T, kParts<T>> b([&](int r) { return dys + (j0 + r < s.rows ? j0 + r : s.rows - 1) * dy.row; });
-    Acc acc;
-    tile_product<3, kParts<T>>(a, b, s.width, acc, lds);
-    each_quad(acc, [&](int i, int j, f32x4 c) {
-        if (j0 + j >= s.rows || i0 + i >= s.hidden_ld) return;
-        const int64_t at = (particle * s.rows + j0 + j) * s.hidden_ld + i0 + i;
-        const f32x4 gv = *reinterpret_cast<const f32x4 *>(g + at), uv = *reinterpret_cast<const f32x4 *>(u + at);
+    ColumnsOfA<float, 3> a(down.p + particle * down.stride, s.hidden, iw, s.hidden);
+    RowsOfB<TL, T, kParts<T>> b(dys + j0 * dy.row, dy.row, s.rows - j0);
+    Acc<TL::kBlocksJ> acc;
+    tile_product<TL, 3, kParts<T>>(a, b, s.width, acc, lds, scratch);
+    each_quad<TL, true>(acc, iw, s.hidden, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t) {
+        if (j >= s.rows) return;
+        // (two lanes may have values of the same places here, and then the same values)
+        const int64_t at = (particle * s.rows + j) * s.hidden_ld + i;
+        const f32x4 gv = *reinterpret_cast<const f32x4u *>(g + at), uv = *reinterpret_cast<const f32x4u *>(u + at);
         f32x4 dgv, duv;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -384,66 +621,70 @@ __global__ __launch_bounds__(256, 2) void hidden_grad_kernel(FfnShape s, TileGri
             dgv[e] = c[e] * uv[e] * slope;
             duv[e] = c[e] * act;
         }
-        *reinterpret_cast<f32x4 *>(dg + at) = dgv;
-        *reinterpret_cast<f32x4 *>(du + at) = duv;
+        *reinterpret_cast<f32x4u *>(dg + at) = dgv;
+        *reinterpret_cast<f32x4u *>(du + at) = duv;
     });
 }
 
-template <class T>
-__global__ __launch_bounds__(256, 2) void input_grad_kernel(FfnShape s, TileGrid grid, const float *dg, const float *du, Params gate, Params up, Rows<T> dx)
+template <class TL, class T>
+SVGD_TILE_KERNEL void input_grad_kernel(FfnShape s, TileGrid grid, const float *dg, const float *du, Params gate, Params up, Rows<T> dx)
 {
     constexpr int P = kHiddenParts<T>;
-    __shared__ bf16x8 lds[2 * P * kPlane];
+    __shared__ bf16x8 lds[2 * P * TL::kPlane];
+    __shared__ float scratches[TL::kWaves][kScratch];
+    float *const scratch = scratches[wave_of_block()];
     int particle, ti, tj;
     if (!grid.at(particle, ti, tj)) return;
-    const int64_t i0 = (int64_t)ti * kTile, j0 = (int64_t)tj * kTile;
-    Acc acc;
+    const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
+    Acc<TL::kBlocksJ> acc;
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {
         const float *const w = half ? up.p + particle * up.stride : gate.p + particle * gate.stride;
         const float *const d = (half ? du : dg) + particle * s.rows * s.hidden_ld;
-        AcrossK<float, P> a(w + i0, s.width, s.width - i0);
-        AlongK<float, P> b([&](int r) { return d + (j0 + r < s.rows ? j0 + r : s.rows - 1) * s.hidden_ld; });
-        tile_product<P, P>(a, b, s.hidden, acc, lds);
+        ColumnsOfA<float, P> a(w, s.width, iw, s.width);
+        RowsOfB<TL, float, P> b(d + j0 * s.hidden_ld, s.hidden_ld, s.rows - j0);
+        tile_product<TL, P, P>(a, b, s.hidden, acc, lds, scratch);
     }
-    each_quad(acc, [&](int i, int j, f32x4 c) {
-        if (j0 + j >= s.rows || i0 + i >= s.width) return;
-        const float v[4] = {c[0], c[1], c[2], c[3]};
-        const int64_t left = s.width - i0 - i;
-        store_pack<T, 4>(dx.p + particle * dx.particle + (j0 + j) * dx.row + i0 + i, left < 4 ? (int)left : 4, v);
+    each_quad<TL, true>(acc, iw, s.width, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
+        if (j < s.rows) store_quad(dx.p + particle * dx.particle + j * dx.row + i, c, (int)(first - i), s.width - i);
     });
 }
 
-// out[j][i] (+)= sum over the rows t of b[t][j] a[t][i], `wide` values of i and `high` of j, for one or two pairs (b, out).
-template <class TA, class TB>
-__global__ __launch_bounds__(256, 2) void weight_grad_kernel(int64_t rows, int64_t wide, int64_t high, TileGrid grid, int tiles_high, Rows<const TA> a_rows,
-                                                             Rows<const TB> b_rows0, Rows<const TB> b_rows1, Params out0, Params out1, bool accumulate)
+// out[j][i] (+)= sum over the rows t of b[t][j] a[t][i], `wide` values of i and `high` of j, for one or two pairs (b, out).  The activations
+// of the network, of which 16-bit ones have fewer parts, are a: SWAPPED stores out[i][j], so that this holds for all three gradients.
+template <class TL, class TA, class TB, bool SWAPPED>
+SVGD_TILE_KERNEL void weight_grad_kernel(int64_t rows, int64_t wide, int64_t high, TileGrid grid, int tiles_high, Rows<const TA> a_rows,
+                                         Rows<const TB> b_rows0, Rows<const TB> b_rows1, Params out0, Params out1, bool accumulate)
 {
     constexpr int PA = kParts<TA>, PB = kParts<TB>;
-    __shared__ bf16x8 lds[(PA + PB) * kPlane];
+    __shared__ bf16x8 lds[2 * PB * TL::kPlane];
+    __shared__ float scratches[TL::kWaves][kScratch];
+    float *const scratch = scratches[wave_of_block()];
     int particle, ti, tj;
     if (!grid.at(particle, ti, tj)) return;
     const bool second = tj >= tiles_high;
     if (second) tj -= tiles_high;
     const Rows<const TB> b_rows = second ? b_rows1 : b_rows0;
     float *const out = const_cast<float *>(second ? out1.p + particle * out1.stride : out0.p + particle * out0.stride);
-    const int64_t i0 = (int64_t)ti * kTile, j0 = (int64_t)tj * kTile;
-    AcrossK<TA, PA> a(a_rows.p + particle * a_rows.particle + i0, a_rows.row, wide - i0);
-    AcrossK<TB, PB> b(b_rows.p + particle * b_rows.particle + j0, b_rows.row, high - j0);
-    Acc acc;
-    tile_product<PA, PB>(a, b, rows, acc, lds);
-    each_quad(acc, [&](int i, int j, f32x4 c) {
-        if (j0 + j >= high || i0 + i >= wide) return;
-        float *const p = out + (j0 + j) * wide + i0 + i;
-        const int64_t left = wide - i0 - i;
-        float v[4] = {c[0], c[1], c[2], c[3]};
-        if (accumulate) {
-            float old[4];
-            load_pack<float, 4>(p, left < 4 ? (int)left : 4, old);
+    const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
+    ColumnsOfA<TA, PA> a(a_rows.p + particle * a_rows.particle, a_rows.row, iw, wide);
+    ColumnsOfB<TL, TB, PB> b(b_rows.p + particle * b_rows.particle, b_rows.row, j0, high);
+    Acc<TL::kBlocksJ> acc;
+    tile_product<TL, PA, PB>(a, b, rows, acc, lds, scratch);
+    each_quad<TL, true>(acc, iw, wide, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
+        if (j >= high) return;
+        const int skip = (int)(first - i);
+        const int64_t left = wide - i;
+        if (accumulate || SWAPPED) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += old[e];
+            for (int e = 0; e < 4; ++e) {
+                if (e < skip || e >= left) continue;
+                float *const p = out + (SWAPPED ? (i + e) * high + j : j * wide + i + e);
+                *p = accumulate ? c[e] + *p : c[e];
+            }
+        } else {
+            store_quad(out + j * wide + i, c, skip, left);
         }
-        store_pack<float, 4>(p, left < 4 ? (int)left : 4, v);
     });
 }
 

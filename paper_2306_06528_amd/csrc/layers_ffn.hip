@@ -57,12 +57,13 @@ template <class T, int ACT> int forward(const Call &c, const svgd_rows &x, const
     float *const h = buffer, *const g = buffer + plane, *const u = buffer + 2 * plane;
     if (c.s.rows <= kThinRows)
         return c.s.rows <= 16 ? thin_forward<T, ACT, 1>(c, x, y, h, g, u, save) : thin_forward<T, ACT, 2>(c, x, y, h, g, u, save);
-    const TileGrid first(c.n, tiles(c.s.hidden, kTile / 2), tiles(c.s.rows, kTile)), second(c.n, tiles(c.s.width, kTile), tiles(c.s.rows, kTile));
+    typedef Tile<4, 8> TL;
+    const TileGrid first(c.n, tiles(c.s.hidden, TL::kI / 2), tiles(c.s.rows, TL::kJ)), second(c.n, tiles(c.s.width, TL::kI), tiles(c.s.rows, TL::kJ));
     if (first.total < 0 || second.total < 0) return SVGD_ERR_TOO_LARGE;
-    if (save) gate_up_kernel<T, ACT, true><<<first.blocks(), 256, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, g, u);
-    else gate_up_kernel<T, ACT, false><<<first.blocks(), 256, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
+    if (save) gate_up_kernel<TL, T, ACT, true><<<first.blocks(), TL::kThreads, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, g, u);
+    else gate_up_kernel<TL, T, ACT, false><<<first.blocks(), TL::kThreads, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
     if (const int rc = launched()) return rc;
-    down_kernel<T><<<second.blocks(), 256, 0, c.stream>>>(c.s, second, h, c.down, out<T>(y));
+    down_kernel<TL, T><<<second.blocks(), TL::kThreads, 0, c.stream>>>(c.s, second, h, c.down, out<T>(y));
     return launched();
 }
 
@@ -73,33 +74,35 @@ int backward(const Call &c, const svgd_rows &dy, const svgd_rows &x, const float
     const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
     const float *const h = saved, *const g = saved + plane, *const u = saved + 2 * plane;
     float *const dg = scratch, *const du = scratch + plane;
-    const TileGrid hidden(c.n, tiles(c.s.hidden, kTile), tiles(c.s.rows, kTile)), input(c.n, tiles(c.s.width, kTile), tiles(c.s.rows, kTile));
-    const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0), high = (int)tiles(c.s.hidden, kTile);
-    const TileGrid gate_up(c.n, tiles(c.s.width, kTile), (int64_t)high * gates), down(c.n, tiles(c.s.hidden, kTile), tiles(c.s.width, kTile));
+    typedef Tile<4, 8> TL;
+    const int64_t tj = tiles(c.s.rows, TL::kJ);
+    const TileGrid hidden(c.n, tiles(c.s.hidden, TL::kI), tj), input(c.n, tiles(c.s.width, TL::kI), tj);
+    const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0), high = (int)tiles(c.s.hidden, TL::kJ);
+    const TileGrid gate_up(c.n, tiles(c.s.width, TL::kI), (int64_t)high * gates), down(c.n, tiles(c.s.width, TL::kI), high);
     if (hidden.total < 0 || input.total < 0 || gate_up.total < 0 || down.total < 0) return SVGD_ERR_TOO_LARGE;
     const bool thin = c.s.rows <= kThinRows;
     if (thin && c.s.rows > 0 && (dx.data || gates)) {
         if (const int rc = c.s.rows <= 16 ? thin_backward<T, ACT, 1>(c, dy, g, u, dx, dg, du) : thin_backward<T, ACT, 2>(c, dy, g, u, dx, dg, du)) return rc;
     }
     if (!thin && (dx.data || gates)) {
-        hidden_grad_kernel<T, ACT><<<hidden.blocks(), 256, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
+        hidden_grad_kernel<TL, T, ACT><<<hidden.blocks(), TL::kThreads, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
         if (const int rc = launched()) return rc;
     }
     if (!thin && dx.data) {
-        input_grad_kernel<T><<<input.blocks(), 256, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
+        input_grad_kernel<TL, T><<<input.blocks(), TL::kThreads, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
         if (const int rc = launched()) return rc;
     }
     const int64_t particle = c.s.rows * c.s.hidden_ld, row = c.s.hidden_ld;
     if (gates) {
         const Rows<const float> a{dgate.p ? dg : du, particle, row}, b{du, particle, row};
-        weight_grad_kernel<T, float><<<gate_up.blocks(), 256, 0, c.stream>>>(c.s.rows, c.s.width, c.s.hidden, gate_up, high, in<T>(x), a, b,
+        weight_grad_kernel<TL, T, float, false><<<gate_up.blocks(), TL::kThreads, 0, c.stream>>>(c.s.rows, c.s.width, c.s.hidden, gate_up, high, in<T>(x), a, b,
                                                                              dgate.p ? dgate : dup, dup, accumulate);
         if (const int rc = launched()) return rc;
     }
     if (ddown.p) {
         const Rows<const float> hs{h, particle, row};
-        weight_grad_kernel<float, T><<<down.blocks(), 256, 0, c.stream>>>(c.s.rows, c.s.hidden, c.s.width, down, down.tj, hs, in<T>(dy), in<T>(dy),
-                                                                          ddown, ddown, accumulate);
+        weight_grad_kernel<TL, T, float, true><<<down.blocks(), TL::kThreads, 0, c.stream>>>(c.s.rows, c.s.width, c.s.hidden, down, high, in<T>(dy), hs, hs,
+                                                                                            ddown, ddown, accumulate);
         if (const int rc = launched()) return rc;
     }
     return SVGD_OK;
