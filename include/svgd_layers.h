@@ -84,14 +84,16 @@ int svgd_layer_norm_backward(int dtype, int n, int64_t rows, int64_t width, svgd
  *     g = gate x,  u = up x,  h = act(g) * u,  y = down h            for every row x
  * gate and up: hidden x width, down: width x hidden values per particle.  buffer (DEVICE, 16-byte
  * aligned, svgd_gated_ffn_buffer bytes) holds h during the call; with `save` it also receives g and u and is, as it
- * is afterwards, what the backward pass takes.  Non-finite inputs make what depends on them non-finite, but an
+ * is afterwards, what the backward pass takes.  scratch (DEVICE, 16-byte aligned): svgd_gated_ffn_forward_scratch
+ * bytes, may be NULL if these are 0.  Non-finite inputs make what depends on them non-finite, but an
  * infinity may come out as NaN.
  */
 size_t svgd_gated_ffn_buffer(int n, int64_t rows, int64_t width, int64_t hidden, int save);
+size_t svgd_gated_ffn_forward_scratch(int n, int64_t rows, int64_t width, int64_t hidden);
 int svgd_gated_ffn_forward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t hidden, svgd_rows x,
                            const float *gate, int64_t gate_stride, const float *up, int64_t up_stride,
                            const float *down, int64_t down_stride, svgd_rows y, int save, void *buffer,
-                           size_t buffer_bytes, void *stream);
+                           size_t buffer_bytes, void *scratch, size_t scratch_bytes, void *stream);
 
 /*
  * Its backward pass, `saved` being the buffer of the forward call with `save` (read only here):

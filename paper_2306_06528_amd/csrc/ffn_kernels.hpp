@@ -337,15 +337,16 @@ template <int NJ> struct Acc {
     }
 };
 
-// Adds the product over K columns to acc.  Products of parts pa, pb with pa + pb beyond the last part are below 2^-24
+// Adds the product over the columns from begin (a multiple of kTileK) to end to acc.  Products of parts pa, pb with pa + pb beyond the last part are below 2^-24
 // (three parts; 2^-16 with two) of the whole and left out.  While the matrix cores work on a step, the next one's rows are
 // on their way, those of B then go to the other half of LDS, and those of A are split into the registers of the last
 // columns' blocks as these get free: one barrier per step, and nothing but it between one step's products and the next one's.
 // lds: 2 * PB * kPlane units; scratch: the wave's own kScratch floats.
 constexpr int kScratch = 64 * kTileK; // 64 rows of a step of A; 16 rows of 68 values of C
 template <class TL, int PA, int PB, class LA, class LB>
-__device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t K, Acc<TL::kBlocksJ> &acc, bf16x8 *lds, float *scratch)
+__device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_t K, Acc<TL::kBlocksJ> &acc, bf16x8 *lds, float *scratch)
 {
+    if (begin >= K) return;
     constexpr int kOrder = (PA > PB ? PA : PB) - 1, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
     constexpr int kLast = PB == 1 ? 2 : 1;
     static_assert(NJ / 2 <= NJ - kLast, "every column once");
@@ -371,17 +372,17 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t K, Acc<TL::kB
                     }
         }
     };
-    const int64_t whole = a.narrow || b.narrow ? 0 : K / kTileK * kTileK;
-    if (whole > 0) {
-        b.fetch(0);
-        a.fetch(0);
+    const int64_t whole = a.narrow || b.narrow ? begin : K / kTileK * kTileK;
+    if (whole > begin) {
+        b.fetch(begin);
+        a.fetch(begin);
         __syncthreads(); // (an earlier product's last step has been read)
         b.store(lds, sc);
         a.stage(scratch);
 #pragma unroll
         for (int ib = 0; ib < 4; ++ib) a.parts(ib, sc, fa[ib], scratch);
         __syncthreads();
-        for (int64_t k0 = kTileK; k0 < whole; k0 += kTileK) {
+        for (int64_t k0 = begin + kTileK; k0 < whole; k0 += kTileK) {
             b.fetch(k0);
             __builtin_amdgcn_sched_barrier(0); // (the compiler would move the loads down to where their values are needed)
             columns(0, NJ / 2 - 1);
@@ -430,31 +431,39 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t K, Acc<TL::kB
     }
 }
 
-// Which tile a workgroup computes.  Workgroups go round the eight dies in turn: every die gets tiles that follow one another, so
-// that the operands they share meet in its L2; and they follow one another in blocks of kBand tiles of j.
+// Which tile a workgroup computes, over which part of the columns.  Workgroups go round the eight dies in turn: every die gets
+// tiles that follow one another, so that the operands they share meet in its L2; and they follow one another in blocks of kBand tiles of j.
+// Where there are few tiles the columns are split into `splits` parts of `per` columns: the parts' sums are added up afterwards,
+// in order (reduce_rows_kernel, reduce_params_kernel).
 constexpr int kDies = 8, kBand = 8;
 struct TileGrid {
-    int ti, tj, per_die, total;
-    __host__ TileGrid(int n, int64_t i, int64_t j) : ti((int)i), tj((int)j), per_die(0), total(0)
+    int ti, tj, splits, per_die, total;
+    int64_t per, columns;
+    __host__ TileGrid() : ti(0), tj(0), splits(1), per_die(0), total(0), per(0), columns(0) {}
+    __host__ TileGrid(int n, int64_t i, int64_t j, int64_t cols, int parts) : ti((int)i), tj((int)j), splits(parts), columns(cols)
     {
-        const int64_t t = (int64_t)n * i * j;
+        per = ((cols + parts - 1) / parts + kTileK - 1) / kTileK * kTileK;
+        const int64_t t = n * i * j * parts;
         total = t > (1 << 24) - kDies ? -1 : (int)t; // (more than memory holds, and than a launch takes)
-        per_die = total < 0 ? 0 : (int)((t + kDies - 1) / kDies);
+        per_die = total < 0 ? 0 : (total + kDies - 1) / kDies;
     }
     __host__ int blocks() const { return per_die * kDies; }
     // false: nothing to do
-    __device__ __forceinline__ bool at(int &particle, int &i, int &j) const
+    __device__ __forceinline__ bool at(int block, int &particle, int &part, int &i, int &j) const
     {
-        const int id = (blockIdx.x % kDies) * per_die + blockIdx.x / kDies;
+        const int id = (block % kDies) * per_die + block / kDies;
         if (id >= total) return false;
-        particle = id / (ti * tj);
-        const int r = id - particle * ti * tj;
+        const int each = ti * tj, p = id / each, r = id - p * each;
+        particle = p / splits;
+        part = p - particle * splits;
         const int band = r / (ti * kBand), left = r - band * ti * kBand;
         const int high = tj - band * kBand < kBand ? tj - band * kBand : kBand;
         i = left / high;
         j = band * kBand + left - i * high;
         return true;
     }
+    __device__ __forceinline__ int64_t begin(int part) const { return part * per; }
+    __device__ __forceinline__ int64_t end(int part) const { return (part + 1) * per < columns ? (part + 1) * per : columns; } // (may lie before begin)
 };
 
 template <int ACT> __device__ __forceinline__ void activate(float g, float &a, float &slope)
@@ -471,7 +480,8 @@ template <int ACT> __device__ __forceinline__ void activate(float g, float &a, f
 }
 
 struct FfnShape {
-    int64_t rows, width, hidden, hidden_ld; // hidden_ld: row stride of g, u, h, dg, du in the buffers
+    int n;
+    int64_t rows, width, hidden, hidden_ld, width_ld; // *_ld: row stride of g, u, h, dg, du in the buffers; of partial sums of y and dx
 };
 template <class T> struct Rows {
     T *p;
@@ -533,8 +543,8 @@ SVGD_TILE_KERNEL void gate_up_kernel(FfnShape s, TileGrid grid, Rows<const T> x,
     __shared__ bf16x8 lds[2 * kParts<T> * TL::kPlane];
     __shared__ float scratches[TL::kWaves][kScratch];
     float *const scratch = scratches[wave_of_block()];
-    int particle, ti, tj;
-    if (!grid.at(particle, ti, tj)) return;
+    int particle, part, ti, tj;
+    if (!grid.at(blockIdx.x, particle, part, ti, tj)) return;
     const T *const xs = x.p + particle * x.particle;
     const int lane = threadIdx.x & 63;
     const int64_t i0 = (int64_t)ti * (TL::kI / 2) + wave_of_block() * 32, j0 = (int64_t)tj * TL::kJ;
@@ -542,7 +552,7 @@ SVGD_TILE_KERNEL void gate_up_kernel(FfnShape s, TileGrid grid, Rows<const T> x,
     RowsOfA<3, 2> a(gate.p + particle * gate.stride + first * s.width, up.p + particle * up.stride + first * s.width, s.hidden - first, s.width);
     RowsOfB<TL, T, kParts<T>> b(xs + j0 * x.row, x.row, s.rows - j0);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, 3, kParts<T>>(a, b, s.width, acc, lds, scratch);
+    tile_product<TL, 3, kParts<T>>(a, b, 0, s.width, acc, lds, scratch);
     const int piece = lane & 7; // four values: in the wave's rows of C those of gate are 16 (piece / 2) + 4 (piece % 2) on, those of up 8 behind
     const int64_t i = i0 + 4 * piece;
 #pragma unroll
@@ -574,23 +584,27 @@ SVGD_TILE_KERNEL void gate_up_kernel(FfnShape s, TileGrid grid, Rows<const T> x,
 // Two parts of each operand are enough where the result is rounded to 16 bits: what is left out is below 2^-16 of a product.
 template <class T> constexpr int kHiddenParts = sizeof(T) == 4 ? 3 : 2;
 
-template <class TL, class T> SVGD_TILE_KERNEL void down_kernel(FfnShape s, TileGrid grid, const float *h, Params down, Rows<T> y)
+// partial: with more than one part, their sums [part][particle][row][width_ld]
+template <class TL, class T> SVGD_TILE_KERNEL void down_kernel(FfnShape s, TileGrid grid, const float *h, Params down, Rows<T> y, float *partial)
 {
     constexpr int P = kHiddenParts<T>;
     __shared__ bf16x8 lds[2 * P * TL::kPlane];
     __shared__ float scratches[TL::kWaves][kScratch];
     float *const scratch = scratches[wave_of_block()];
-    int particle, ti, tj;
-    if (!grid.at(particle, ti, tj)) return;
+    int particle, part, ti, tj;
+    if (!grid.at(blockIdx.x, particle, part, ti, tj)) return;
     const float *const w = down.p + particle * down.stride, *const hs = h + particle * s.rows * s.hidden_ld;
     const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
     const int64_t first = iw < s.width ? iw : s.width - 1;
     RowsOfA<P, 1> a(w + first * s.hidden, w, s.width - first, s.hidden);
     RowsOfB<TL, float, P> b(hs + j0 * s.hidden_ld, s.hidden_ld, s.rows - j0);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, P, P>(a, b, s.hidden, acc, lds, scratch);
-    each_quad<TL, false>(acc, iw, s.width, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
-        if (j < s.rows) store_quad(y.p + particle * y.particle + j * y.row + i, c, (int)(first - i), s.width - i);
+    tile_product<TL, P, P>(a, b, grid.begin(part), grid.end(part), acc, lds, scratch);
+    float *const sums = partial + ((int64_t)part * s.n + particle) * s.rows * s.width_ld;
+    each_quad<TL, false>(acc, iw, s.width, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t) {
+        if (j >= s.rows) return;
+        if (grid.splits > 1) *reinterpret_cast<f32x4 *>(sums + j * s.width_ld + i) = c; // (what is beyond the width is not used)
+        else store_quad(y.p + particle * y.particle + j * y.row + i, c, 0, s.width - i);
     });
 }
 
@@ -600,14 +614,14 @@ SVGD_TILE_KERNEL void hidden_grad_kernel(FfnShape s, TileGrid grid, Rows<const T
     __shared__ bf16x8 lds[2 * kParts<T> * TL::kPlane];
     __shared__ float scratches[TL::kWaves][kScratch];
     float *const scratch = scratches[wave_of_block()];
-    int particle, ti, tj;
-    if (!grid.at(particle, ti, tj)) return;
+    int particle, part, ti, tj;
+    if (!grid.at(blockIdx.x, particle, part, ti, tj)) return;
     const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
     const T *const dys = dy.p + particle * dy.particle;
     ColumnsOfA<float, 3> a(down.p + particle * down.stride, s.hidden, iw, s.hidden);
     RowsOfB<TL, T, kParts<T>> b(dys + j0 * dy.row, dy.row, s.rows - j0);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, 3, kParts<T>>(a, b, s.width, acc, lds, scratch);
+    tile_product<TL, 3, kParts<T>>(a, b, 0, s.width, acc, lds, scratch);
     each_quad<TL, true>(acc, iw, s.hidden, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t) {
         if (j >= s.rows) return;
         // (two lanes may have values of the same places here, and then the same values)
@@ -626,66 +640,131 @@ SVGD_TILE_KERNEL void hidden_grad_kernel(FfnShape s, TileGrid grid, Rows<const T
     });
 }
 
+// A tile of dx.  The columns are those of gate and then those of up: with more than one part the first half of the parts is gate's.
 template <class TL, class T>
-SVGD_TILE_KERNEL void input_grad_kernel(FfnShape s, TileGrid grid, const float *dg, const float *du, Params gate, Params up, Rows<T> dx)
+__device__ __forceinline__ void input_grad_tile(const FfnShape &s, const TileGrid &grid, int block, const float *dg, const float *du, const Params &gate,
+                                                const Params &up, const Rows<T> &dx, float *partial, bf16x8 *lds, float *scratch)
 {
     constexpr int P = kHiddenParts<T>;
-    __shared__ bf16x8 lds[2 * P * TL::kPlane];
-    __shared__ float scratches[TL::kWaves][kScratch];
-    float *const scratch = scratches[wave_of_block()];
-    int particle, ti, tj;
-    if (!grid.at(particle, ti, tj)) return;
+    int particle, part, ti, tj;
+    if (!grid.at(block, particle, part, ti, tj)) return;
     const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
+    const int halves = grid.splits / 2, first_half = grid.splits > 1 ? part / halves : 0, last_half = grid.splits > 1 ? first_half : 1;
+    const int sub = grid.splits > 1 ? part - first_half * halves : 0;
     Acc<TL::kBlocksJ> acc;
 #pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
+    for (int half = first_half; half <= last_half; ++half) {
         const float *const w = half ? up.p + particle * up.stride : gate.p + particle * gate.stride;
         const float *const d = (half ? du : dg) + particle * s.rows * s.hidden_ld;
         ColumnsOfA<float, P> a(w, s.width, iw, s.width);
         RowsOfB<TL, float, P> b(d + j0 * s.hidden_ld, s.hidden_ld, s.rows - j0);
-        tile_product<TL, P, P>(a, b, s.hidden, acc, lds, scratch);
+        tile_product<TL, P, P>(a, b, grid.begin(sub), grid.end(sub), acc, lds, scratch);
     }
+    float *const sums = partial + ((int64_t)part * s.n + particle) * s.rows * s.width_ld;
     each_quad<TL, true>(acc, iw, s.width, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
-        if (j < s.rows) store_quad(dx.p + particle * dx.particle + j * dx.row + i, c, (int)(first - i), s.width - i);
+        if (j >= s.rows) return;
+        if (grid.splits > 1) store_quad(sums + j * s.width_ld + i, c, (int)(first - i), s.width - i);
+        else store_quad(dx.p + particle * dx.particle + j * dx.row + i, c, (int)(first - i), s.width - i);
     });
 }
 
 // out[j][i] (+)= sum over the rows t of b[t][j] a[t][i], `wide` values of i and `high` of j, for one or two pairs (b, out).  The activations
 // of the network, of which 16-bit ones have fewer parts, are a: SWAPPED stores out[i][j], so that this holds for all three gradients.
-template <class TL, class TA, class TB, bool SWAPPED>
-SVGD_TILE_KERNEL void weight_grad_kernel(int64_t rows, int64_t wide, int64_t high, TileGrid grid, int tiles_high, Rows<const TA> a_rows,
-                                         Rows<const TB> b_rows0, Rows<const TB> b_rows1, Params out0, Params out1, bool accumulate)
+// partial: with more than one part, their sums [part][particle][which of the two][wide * high].
+template <class TA, class TB> struct WeightGrad {
+    TileGrid grid;
+    int64_t wide, high;
+    int tiles_high, outs; // tiles of j, of one pair; pairs
+    Rows<const TA> a;
+    Rows<const TB> b[2];
+    Params out[2];
+    float *partial;
+};
+
+template <class TL, bool SWAPPED, class TA, class TB>
+__device__ __forceinline__ void weight_grad_tile(const WeightGrad<TA, TB> &w, int block, bool accumulate, bf16x8 *lds, float *scratch)
 {
     constexpr int PA = kParts<TA>, PB = kParts<TB>;
-    __shared__ bf16x8 lds[2 * PB * TL::kPlane];
-    __shared__ float scratches[TL::kWaves][kScratch];
-    float *const scratch = scratches[wave_of_block()];
-    int particle, ti, tj;
-    if (!grid.at(particle, ti, tj)) return;
-    const bool second = tj >= tiles_high;
-    if (second) tj -= tiles_high;
-    const Rows<const TB> b_rows = second ? b_rows1 : b_rows0;
-    float *const out = const_cast<float *>(second ? out1.p + particle * out1.stride : out0.p + particle * out0.stride);
+    int particle, part, ti, tj;
+    if (!w.grid.at(block, particle, part, ti, tj)) return;
+    const int which = tj >= w.tiles_high;
+    if (which) tj -= w.tiles_high;
+    const Rows<const TB> b_rows = which ? w.b[1] : w.b[0];
+    const bool split = w.grid.splits > 1;
+    const int n = w.grid.total / (w.grid.ti * w.grid.tj * w.grid.splits);
+    float *const out = split ? w.partial + (((int64_t)part * n + particle) * w.outs + which) * w.wide * w.high
+                             : const_cast<float *>(which ? w.out[1].p + particle * w.out[1].stride : w.out[0].p + particle * w.out[0].stride);
+    const bool add = accumulate && !split;
     const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
-    ColumnsOfA<TA, PA> a(a_rows.p + particle * a_rows.particle, a_rows.row, iw, wide);
-    ColumnsOfB<TL, TB, PB> b(b_rows.p + particle * b_rows.particle, b_rows.row, j0, high);
+    ColumnsOfA<TA, PA> a(w.a.p + particle * w.a.particle, w.a.row, iw, w.wide);
+    ColumnsOfB<TL, TB, PB> b(b_rows.p + particle * b_rows.particle, b_rows.row, j0, w.high);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, PA, PB>(a, b, rows, acc, lds, scratch);
-    each_quad<TL, true>(acc, iw, wide, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
-        if (j >= high) return;
+    tile_product<TL, PA, PB>(a, b, w.grid.begin(part), w.grid.end(part), acc, lds, scratch);
+    each_quad<TL, true>(acc, iw, w.wide, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
+        if (j >= w.high) return;
         const int skip = (int)(first - i);
-        const int64_t left = wide - i;
-        if (accumulate || SWAPPED) {
+        const int64_t left = w.wide - i;
+        if (add || SWAPPED) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (e < skip || e >= left) continue;
-                float *const p = out + (SWAPPED ? (i + e) * high + j : j * wide + i + e);
-                *p = accumulate ? c[e] + *p : c[e];
+                float *const p = out + (SWAPPED ? (i + e) * w.high + j : j * w.wide + i + e);
+                *p = add ? c[e] + *p : c[e];
             }
         } else {
-            store_quad(out + j * wide + i, c, skip, left);
+            store_quad(out + j * w.wide + i, c, skip, left);
         }
     });
+}
+
+// What a backward pass has to do once dg and du are there, none of which waits for another, in one launch: the tiles of dx, then those of
+// dgate and dup, then those of ddown.
+template <class TL, class T>
+SVGD_TILE_KERNEL void gradients_kernel(FfnShape s, TileGrid input, const float *dg, const float *du, Params gate, Params up, Rows<T> dx, float *dx_partial,
+                                       WeightGrad<T, float> gates, WeightGrad<T, float> down, bool accumulate)
+{
+    constexpr int P = kHiddenParts<T> > kParts<float> ? kHiddenParts<T> : kParts<float>;
+    __shared__ bf16x8 lds[2 * P * TL::kPlane];
+    __shared__ float scratches[TL::kWaves][kScratch];
+    float *const scratch = scratches[wave_of_block()];
+    int block = blockIdx.x;
+    if (block < input.per_die * kDies) {
+        input_grad_tile<TL, T>(s, input, block, dg, du, gate, up, dx, dx_partial, lds, scratch);
+        return;
+    }
+    block -= input.per_die * kDies;
+    if (block < gates.grid.per_die * kDies) {
+        weight_grad_tile<TL, false>(gates, block, accumulate, lds, scratch);
+        return;
+    }
+    weight_grad_tile<TL, true>(down, block - gates.grid.per_die * kDies, accumulate, lds, scratch);
+}
+
+// y = the sum of the parts' sums, in order.
+template <class T> __global__ __launch_bounds__(256) void reduce_rows_kernel(FfnShape s, const float *partial, int parts, Rows<T> y)
+{
+    const int64_t quads = s.width_ld / 4, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (k >= s.n * s.rows * quads) return;
+    const int64_t line = k / quads, i = (k - line * quads) * 4, particle = line / s.rows, j = line - particle * s.rows;
+    const int64_t each = s.n * s.rows * s.width_ld;
+    const float *p = partial + line * s.width_ld + i;
+    f32x4 total = {0.f, 0.f, 0.f, 0.f};
+    for (int part = 0; part < parts; ++part) total += *reinterpret_cast<const f32x4 *>(p + part * each);
+    store_quad(y.p + particle * y.particle + j * y.row + i, total, 0, s.width - i);
+}
+
+// The same for gradients of parameters: `size` values of each of `outs` per particle.
+__global__ __launch_bounds__(256) void reduce_params_kernel(int n, int64_t size, int outs, const float *partial, int parts, Params out0, Params out1,
+                                                            bool accumulate)
+{
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, each = n * outs * size;
+    if (k >= each) return;
+    float total = 0.f;
+    for (int part = 0; part < parts; ++part) total += partial[part * each + k];
+    const int64_t line = k / size, at = k - line * size, particle = line / outs;
+    const Params &out = line - particle * outs ? out1 : out0;
+    float *const p = const_cast<float *>(out.p) + particle * out.stride + at;
+    *p = accumulate ? total + *p : total;
 }
 
 } // namespace svgd

@@ -280,10 +280,13 @@ PyObject *gated_ffn_forward(PyObject *, PyObject *const *a, Py_ssize_t na)
         if (!current_stream(x, a, stream)) Py_RETURN_NONE;
         const at::Tensor y = new_like(x);
         const size_t need = svgd_gated_ffn_buffer(x.particles(), x.rows(), x.width(), b.hidden, save);
-        at::Tensor buffer = at::empty({(int64_t)(need / 4)}, x.given.options().dtype(at::kFloat));
+        const size_t scratch_need = svgd_gated_ffn_forward_scratch(x.particles(), x.rows(), x.width(), b.hidden);
+        at::Tensor buffer = at::empty({(int64_t)(need / 4)}, x.given.options().dtype(at::kFloat)), scratch;
+        if (scratch_need) scratch = bytes(scratch_need, x);
         const int rc = unlocked([&] {
             return svgd_gated_ffn_forward(x.dtype(), b.activation, x.particles(), x.rows(), x.width(), b.hidden, x.desc(), b.gate.p(), b.gate.stride, b.up.p(),
-                                          b.up.stride, b.down.p(), b.down.stride, dense(y, x), save, buffer.data_ptr(), need, stream);
+                                          b.up.stride, b.down.p(), b.down.stride, dense(y, x), save, buffer.data_ptr(), need,
+                                          scratch_need ? scratch.data_ptr() : nullptr, scratch_need, stream);
         });
         if (!save) buffer = at::Tensor();
         return result(rc, {&y, &buffer});

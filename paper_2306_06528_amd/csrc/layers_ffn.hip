@@ -15,6 +15,95 @@ bool sized(int n, int64_t rows, int64_t width, int64_t hidden)
 
 int64_t tiles(int64_t size, int tile) { return (size + tile - 1) / tile; }
 
+// ---------------------------------------------------------------------------------------------
+// Which tiles, and into how many parts the columns go: by sizes alone, the same for every type
+// ---------------------------------------------------------------------------------------------
+enum TileKind { kLarge, kMiddle, kSmall, kTileKinds };
+typedef Tile<4, 8> LargeTile;
+typedef Tile<4, 4> MiddleTile;
+typedef Tile<2, 4> SmallTile;
+struct KindOf {
+    int i, j;
+    double step;  // time of a step (32 columns) of one tile when a CU is full, in steps of a large one
+    int at_a_time; // workgroups on the whole part then
+};
+constexpr KindOf kKinds[kTileKinds] = {{LargeTile::kI, LargeTile::kJ, 1.0, 512}, {MiddleTile::kI, MiddleTile::kJ, 0.6, 512}, {SmallTile::kI, SmallTile::kJ, 0.6, 1024}};
+
+struct Choice {
+    TileKind kind;
+    int parts;
+    double cost;
+};
+
+// The cheaper of the choices for `tiles` tiles over `columns` columns of each of n particles: time of the workgroups that run one after
+// another, kStart steps for the first rows of each and its results, and what adding up the parts takes.
+constexpr double kStart = 4.0, kReduce = 4.0;
+double cost_of(TileKind kind, int64_t tiles, int64_t columns, int parts)
+{
+    const KindOf &k = kKinds[kind];
+    const double steps = (double)((columns + parts - 1) / parts + kTileK - 1) / kTileK + kStart;
+    const int64_t all = tiles * parts, rounds = all / k.at_a_time, rest = all - rounds * k.at_a_time;
+    // the last ones have the CUs to themselves if they are few
+    const double last = rest == 0 ? 0.0 : rest * 2 <= k.at_a_time ? 0.6 : 1.0;
+    return ((double)rounds + last) * steps * k.step + (parts > 1 ? kReduce : 0.0);
+}
+
+Choice choose(int n, int64_t i, int64_t j, int64_t columns, int per_wave_i, bool may_split)
+{
+    Choice best{kLarge, 1, 0.0};
+    for (int kind = 0; kind < kTileKinds; ++kind) {
+        const int64_t t = n * tiles(i, kKinds[kind].i / per_wave_i) * tiles(j, kKinds[kind].j);
+        for (int parts = 1; parts <= (may_split ? 32 : 1); parts += parts < 4 ? 1 : parts < 8 ? 2 : parts < 16 ? 4 : 8) {
+            if (parts > 1 && (columns / parts < 4 * kTileK || t * (parts - 1) > 1024)) break;
+            const double c = cost_of((TileKind)kind, t, columns, parts);
+            if ((kind == 0 && parts == 1) || c < best.cost) best = {(TileKind)kind, parts, c};
+        }
+    }
+    return best;
+}
+
+template <class F> int with_tile(TileKind kind, F f)
+{
+    return kind == kLarge ? f(LargeTile{}) : kind == kMiddle ? f(MiddleTile{}) : f(SmallTile{});
+}
+
+constexpr int64_t kThinRows = 32; // up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp)
+
+int64_t width_ld(int64_t width) { return (width + 3) / 4 * 4; }
+
+struct ForwardPlan {
+    Choice gate_up, down;
+    ForwardPlan(int n, int64_t rows, int64_t width, int64_t hidden)
+        : gate_up(choose(n, hidden, rows, width, 2, false)), down(choose(n, width, rows, hidden, 1, true))
+    {
+        if (rows <= kThinRows) down.parts = 1;
+    }
+    size_t scratch(int n, int64_t rows, int64_t width) const { return down.parts > 1 ? (size_t)down.parts * n * rows * width_ld(width) * 4 : 0; }
+};
+
+// The tiles of one launch are of one kind: that of most of them, dgate's and dup's.
+struct BackwardPlan {
+    Choice hidden, gradients;
+    int input_parts, gate_parts, down_parts;
+    size_t hidden_floats, input_floats, gate_floats, down_floats;
+    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid)
+        : hidden(choose(n, hid, rows, width, 1, false)), gradients(choose(n, width, 3 * hid, rows, 1, true)), input_parts(1), gate_parts(gradients.parts),
+          down_parts(gradients.parts)
+    {
+        const KindOf &k = kKinds[gradients.kind];
+        // dx: parts so that its workgroups take about as long as those of the other gradients
+        const int64_t t = n * tiles(width, k.i) * tiles(rows, k.j), steps = (rows + gate_parts - 1) / gate_parts;
+        if (rows > kThinRows)
+            while (input_parts < 32 && 2 * hid / (2 * input_parts) >= 4 * kTileK && t * input_parts < k.at_a_time && 2 * hid / input_parts > steps * 3 / 2) input_parts *= 2;
+        hidden_floats = (size_t)n * rows * hidden_ld(hid);
+        input_floats = input_parts > 1 ? (size_t)input_parts * n * rows * width_ld(width) : 0;
+        gate_floats = gate_parts > 1 ? (size_t)gate_parts * n * 2 * width * hid : 0;
+        down_floats = down_parts > 1 ? (size_t)down_parts * n * width * hid : 0;
+    }
+    size_t scratch() const { return (2 * hidden_floats + input_floats + gate_floats + down_floats + 16) * 4; } // (each begins on 16 bytes)
+};
+size_t aligned4(size_t floats) { return (floats + 3) & ~(size_t)3; }
+
 struct Call {
     int dtype, activation, n;
     FfnShape s;
@@ -26,8 +115,12 @@ template <class T> Rows<const T> in(const svgd_rows &r) { return {(const T *)r.d
 template <class T> Rows<T> out(const svgd_rows &r) { return {(T *)r.data, r.particle_stride, r.row_stride}; }
 int launched() { return hipGetLastError() == hipSuccess ? SVGD_OK : SVGD_ERR_DEVICE; }
 
-// Up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp).
-constexpr int64_t kThinRows = 32;
+template <class T> int reduce_rows(const Call &c, const float *partial, int parts, const Rows<T> &y)
+{
+    const int64_t quads = c.n * c.s.rows * c.s.width_ld / 4;
+    reduce_rows_kernel<T><<<(unsigned)tiles(quads, 256), 256, 0, c.stream>>>(c.s, partial, parts, y);
+    return launched();
+}
 
 template <class T, int ACT, int JB> int thin_forward(const Call &c, const svgd_rows &x, const svgd_rows &y, float *h, float *g, float *u, bool save)
 {
@@ -51,20 +144,31 @@ int thin_backward(const Call &c, const svgd_rows &dy, const float *g, const floa
     return launched();
 }
 
-template <class T, int ACT> int forward(const Call &c, const svgd_rows &x, const svgd_rows &y, float *buffer, bool save)
+template <class T, int ACT> int forward(const Call &c, const svgd_rows &x, const svgd_rows &y, float *buffer, bool save, float *scratch)
 {
     const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
     float *const h = buffer, *const g = buffer + plane, *const u = buffer + 2 * plane;
     if (c.s.rows <= kThinRows)
         return c.s.rows <= 16 ? thin_forward<T, ACT, 1>(c, x, y, h, g, u, save) : thin_forward<T, ACT, 2>(c, x, y, h, g, u, save);
-    typedef Tile<4, 8> TL;
-    const TileGrid first(c.n, tiles(c.s.hidden, TL::kI / 2), tiles(c.s.rows, TL::kJ)), second(c.n, tiles(c.s.width, TL::kI), tiles(c.s.rows, TL::kJ));
-    if (first.total < 0 || second.total < 0) return SVGD_ERR_TOO_LARGE;
-    if (save) gate_up_kernel<TL, T, ACT, true><<<first.blocks(), TL::kThreads, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, g, u);
-    else gate_up_kernel<TL, T, ACT, false><<<first.blocks(), TL::kThreads, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
-    if (const int rc = launched()) return rc;
-    down_kernel<TL, T><<<second.blocks(), TL::kThreads, 0, c.stream>>>(c.s, second, h, c.down, out<T>(y));
-    return launched();
+    const ForwardPlan plan(c.n, c.s.rows, c.s.width, c.s.hidden);
+    int rc = with_tile(plan.gate_up.kind, [&](auto tile) {
+        using TL = decltype(tile);
+        const TileGrid grid(c.n, tiles(c.s.hidden, TL::kI / 2), tiles(c.s.rows, TL::kJ), c.s.width, 1);
+        if (grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+        if (save) gate_up_kernel<TL, T, ACT, true><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(x), c.gate, c.up, h, g, u);
+        else gate_up_kernel<TL, T, ACT, false><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
+        return launched();
+    });
+    if (rc) return rc;
+    rc = with_tile(plan.down.kind, [&](auto tile) {
+        using TL = decltype(tile);
+        const TileGrid grid(c.n, tiles(c.s.width, TL::kI), tiles(c.s.rows, TL::kJ), c.s.hidden, plan.down.parts);
+        if (grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+        down_kernel<TL, T><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, h, c.down, out<T>(y), scratch);
+        return launched();
+    });
+    if (rc || plan.down.parts == 1) return rc;
+    return reduce_rows<T>(c, scratch, plan.down.parts, out<T>(y));
 }
 
 template <class T, int ACT>
@@ -73,39 +177,62 @@ int backward(const Call &c, const svgd_rows &dy, const svgd_rows &x, const float
 {
     const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
     const float *const h = saved, *const g = saved + plane, *const u = saved + 2 * plane;
-    float *const dg = scratch, *const du = scratch + plane;
-    typedef Tile<4, 8> TL;
-    const int64_t tj = tiles(c.s.rows, TL::kJ);
-    const TileGrid hidden(c.n, tiles(c.s.hidden, TL::kI), tj), input(c.n, tiles(c.s.width, TL::kI), tj);
-    const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0), high = (int)tiles(c.s.hidden, TL::kJ);
-    const TileGrid gate_up(c.n, tiles(c.s.width, TL::kI), (int64_t)high * gates), down(c.n, tiles(c.s.width, TL::kI), high);
-    if (hidden.total < 0 || input.total < 0 || gate_up.total < 0 || down.total < 0) return SVGD_ERR_TOO_LARGE;
+    const BackwardPlan plan(c.n, c.s.rows, c.s.width, c.s.hidden);
+    float *const dg = scratch, *const du = dg + plan.hidden_floats, *const dx_partial = du + plan.hidden_floats;
+    float *const gate_partial = dx_partial + aligned4(plan.input_floats), *const down_partial = gate_partial + aligned4(plan.gate_floats);
+    const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0);
     const bool thin = c.s.rows <= kThinRows;
     if (thin && c.s.rows > 0 && (dx.data || gates)) {
         if (const int rc = c.s.rows <= 16 ? thin_backward<T, ACT, 1>(c, dy, g, u, dx, dg, du) : thin_backward<T, ACT, 2>(c, dy, g, u, dx, dg, du)) return rc;
     }
     if (!thin && (dx.data || gates)) {
-        hidden_grad_kernel<TL, T, ACT><<<hidden.blocks(), TL::kThreads, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
-        if (const int rc = launched()) return rc;
+        const int rc = with_tile(plan.hidden.kind, [&](auto tile) {
+            using TL = decltype(tile);
+            const TileGrid grid(c.n, tiles(c.s.hidden, TL::kI), tiles(c.s.rows, TL::kJ), c.s.width, 1);
+            if (grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+            hidden_grad_kernel<TL, T, ACT><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(dy), c.down, g, u, dg, du);
+            return launched();
+        });
+        if (rc) return rc;
     }
-    if (!thin && dx.data) {
-        input_grad_kernel<TL, T><<<input.blocks(), TL::kThreads, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
-        if (const int rc = launched()) return rc;
+    const bool input = !thin && dx.data;
+    if (!input && !gates && !ddown.p) return SVGD_OK;
+    int rc = with_tile(plan.gradients.kind, [&](auto tile) {
+        using TL = decltype(tile);
+        const int64_t particle = c.s.rows * c.s.hidden_ld, row = c.s.hidden_ld;
+        const int high = (int)tiles(c.s.hidden, TL::kJ);
+        const int64_t wide = tiles(c.s.width, TL::kI);
+        TileGrid input_grid;
+        if (input) {
+            const int parts = plan.input_parts;
+            input_grid = TileGrid(c.n, wide, tiles(c.s.rows, TL::kJ), c.s.hidden, parts);
+            if (parts > 1) input_grid.per = ((c.s.hidden + parts / 2 - 1) / (parts / 2) + kTileK - 1) / kTileK * kTileK; // half of the parts for either half
+        }
+        WeightGrad<T, float> of_gates{}, of_down{};
+        const Rows<const float> dgs{dg, particle, row}, dus{du, particle, row}, hs{h, particle, row};
+        if (gates)
+            of_gates = {TileGrid(c.n, wide, (int64_t)high * gates, c.s.rows, plan.gate_parts), c.s.width, c.s.hidden, high, gates, in<T>(x),
+                        {dgate.p ? dgs : dus, dus}, {dgate.p ? dgate : dup, dup}, gate_partial};
+        if (ddown.p)
+            of_down = {TileGrid(c.n, wide, high, c.s.rows, plan.down_parts), c.s.width, c.s.hidden, high, 1, in<T>(dy), {hs, hs}, {ddown, ddown}, down_partial};
+        if (input_grid.total < 0 || of_gates.grid.total < 0 || of_down.grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+        gradients_kernel<TL, T><<<input_grid.blocks() + of_gates.grid.blocks() + of_down.grid.blocks(), TL::kThreads, 0, c.stream>>>(
+            c.s, input_grid, dg, du, c.gate, c.up, out<T>(dx), dx_partial, of_gates, of_down, accumulate);
+        return launched();
+    });
+    if (rc) return rc;
+    if (input && plan.input_parts > 1 && (rc = reduce_rows<T>(c, dx_partial, plan.input_parts, out<T>(dx)))) return rc;
+    const int64_t size = c.s.width * c.s.hidden;
+    if (gates && plan.gate_parts > 1) {
+        reduce_params_kernel<<<(unsigned)tiles(c.n * gates * size, 256), 256, 0, c.stream>>>(c.n, size, gates, gate_partial, plan.gate_parts,
+                                                                                            dgate.p ? dgate : dup, dup, accumulate);
+        if ((rc = launched())) return rc;
     }
-    const int64_t particle = c.s.rows * c.s.hidden_ld, row = c.s.hidden_ld;
-    if (gates) {
-        const Rows<const float> a{dgate.p ? dg : du, particle, row}, b{du, particle, row};
-        weight_grad_kernel<TL, T, float, false><<<gate_up.blocks(), TL::kThreads, 0, c.stream>>>(c.s.rows, c.s.width, c.s.hidden, gate_up, high, in<T>(x), a, b,
-                                                                             dgate.p ? dgate : dup, dup, accumulate);
-        if (const int rc = launched()) return rc;
+    if (ddown.p && plan.down_parts > 1) {
+        reduce_params_kernel<<<(unsigned)tiles(c.n * size, 256), 256, 0, c.stream>>>(c.n, size, 1, down_partial, plan.down_parts, ddown, ddown, accumulate);
+        rc = launched();
     }
-    if (ddown.p) {
-        const Rows<const float> hs{h, particle, row};
-        weight_grad_kernel<TL, T, float, true><<<down.blocks(), TL::kThreads, 0, c.stream>>>(c.s.rows, c.s.width, c.s.hidden, down, high, in<T>(dy), hs, hs,
-                                                                                            ddown, ddown, accumulate);
-        if (const int rc = launched()) return rc;
-    }
-    return SVGD_OK;
+    return rc;
 }
 
 template <class F> int for_type(int dtype, int activation, F f)
@@ -141,31 +268,40 @@ size_t svgd_gated_ffn_buffer(int n, int64_t rows, int64_t width, int64_t hidden,
     return (size_t)n * (size_t)rows * (size_t)hidden_ld(hidden) * 4 * (save ? 3 : 1);
 }
 
+size_t svgd_gated_ffn_forward_scratch(int n, int64_t rows, int64_t width, int64_t hidden)
+{
+    if (!sized(n, rows, width, hidden) || rows == 0) return 0;
+    return ForwardPlan(n, rows, width, hidden).scratch(n, rows, width);
+}
+
 size_t svgd_gated_ffn_scratch(int n, int64_t rows, int64_t width, int64_t hidden)
 {
     if (!sized(n, rows, width, hidden)) return 0;
-    return (size_t)n * (size_t)rows * (size_t)hidden_ld(hidden) * 4 * 2;
+    return BackwardPlan(n, rows, width, hidden).scratch();
 }
 
 int svgd_gated_ffn_forward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t hidden, svgd_rows x, const float *gate,
                            int64_t gate_stride, const float *up, int64_t up_stride, const float *down, int64_t down_stride, svgd_rows y, int save,
-                           void *buffer, size_t buffer_bytes, void *stream)
+                           void *buffer, size_t buffer_bytes, void *scratch, size_t scratch_bytes, void *stream)
 {
     const int64_t size = width > 0 && hidden > 0 && width <= SVGD_LAYER_MAX_WIDTH && hidden <= SVGD_LAYER_MAX_WIDTH ? width * hidden : 0;
-    const Call c{dtype, activation, n, {rows, width, hidden, hidden_ld(hidden)}, {gate, gate_stride, size}, {up, up_stride, size}, {down, down_stride, size},
+    const Call c{dtype, activation, n, {n, rows, width, hidden, hidden_ld(hidden), width_ld(width)}, {gate, gate_stride, size}, {up, up_stride, size}, {down, down_stride, size},
                  (hipStream_t)stream};
     if (const int rc = check(dtype, activation, n, rows, width, hidden, x, c.gate, c.up, c.down)) return rc;
     if (rows == 0) return SVGD_OK;
     const size_t need = svgd_gated_ffn_buffer(n, rows, width, hidden, save);
-    if (!valid_output(y, dtype, n, rows, width) || !buffer || !aligned_to(buffer, 16) || buffer_bytes < need) return SVGD_ERR_INVALID_ARG;
-    const Extent written[2] = {extent(y, dtype, n, rows, width), extent(buffer, need)};
+    const size_t scratch_need = svgd_gated_ffn_forward_scratch(n, rows, width, hidden);
+    if (!valid_output(y, dtype, n, rows, width) || !buffer || !aligned_to(buffer, 16) || buffer_bytes < need ||
+        (scratch_need > 0 && (!scratch || !aligned_to(scratch, 16) || scratch_bytes < scratch_need)))
+        return SVGD_ERR_INVALID_ARG;
+    const Extent written[3] = {extent(y, dtype, n, rows, width), extent(buffer, need), extent(scratch, scratch_need)};
     const Extent read[4] = {extent(x, dtype, n, rows, width), extent(gate, gate_stride, n, size), extent(up, up_stride, n, size),
                             extent(down, down_stride, n, size)};
-    if (written[0].meets(written[1])) return SVGD_ERR_INVALID_ARG;
+    if (written[0].meets(written[1]) || written[0].meets(written[2]) || written[1].meets(written[2])) return SVGD_ERR_INVALID_ARG;
     for (const Extent &w : written)
         for (const Extent &r : read)
             if (w.meets(r)) return SVGD_ERR_INVALID_ARG;
-    return for_type(dtype, activation, [&](auto t, auto act) { return forward<decltype(t), decltype(act)::value>(c, x, y, (float *)buffer, save != 0); });
+    return for_type(dtype, activation, [&](auto t, auto act) { return forward<decltype(t), decltype(act)::value>(c, x, y, (float *)buffer, save != 0, (float *)scratch); });
 }
 
 int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t hidden, svgd_rows dy, svgd_rows x, const float *gate,
@@ -174,7 +310,7 @@ int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int6
                             int64_t ddown_stride, int accumulate, void *scratch, size_t scratch_bytes, void *stream)
 {
     const int64_t size = width > 0 && hidden > 0 && width <= SVGD_LAYER_MAX_WIDTH && hidden <= SVGD_LAYER_MAX_WIDTH ? width * hidden : 0;
-    const Call c{dtype, activation, n, {rows, width, hidden, hidden_ld(hidden)}, {gate, gate_stride, size}, {up, up_stride, size}, {down, down_stride, size},
+    const Call c{dtype, activation, n, {n, rows, width, hidden, hidden_ld(hidden), width_ld(width)}, {gate, gate_stride, size}, {up, up_stride, size}, {down, down_stride, size},
                  (hipStream_t)stream};
     if (const int rc = check(dtype, activation, n, rows, width, hidden, x, c.gate, c.up, c.down)) return rc;
     const Params grads[3] = {{dgate, dgate_stride, size}, {dup, dup_stride, size}, {ddown, ddown_stride, size}};

@@ -32,7 +32,8 @@ class Library:
                 ("svgd_layer_norm_scratch", z, [i, l, l]),
                 ("svgd_layer_norm_backward", i, [i, i, l, l, Rows, Rows, p, l, p, p, Rows, p, l, p, l, i, p, z, p]),
                 ("svgd_gated_ffn_buffer", z, [i, l, l, l, i]),
-                ("svgd_gated_ffn_forward", i, [i, i, i, l, l, l, Rows, p, l, p, l, p, l, Rows, i, p, z, p]),
+                ("svgd_gated_ffn_forward_scratch", z, [i, l, l, l]),
+                ("svgd_gated_ffn_forward", i, [i, i, i, l, l, l, Rows, p, l, p, l, p, l, Rows, i, p, z, p, z, p]),
                 ("svgd_gated_ffn_scratch", z, [i, l, l, l]),
                 ("svgd_gated_ffn_backward", i, [i, i, i, l, l, l, Rows, Rows, p, l, p, l, p, l, p, z, Rows, p, l, p, l, p, l, i, p, z, p]),
                 ("svgd_dropout", i, [i, i, l, l, Rows, Rows, Rows, d, u, u, p, p])):
@@ -47,7 +48,7 @@ def layers():
 def test_every_declared_symbol_is_exported(layers):
     text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(svgd_[a-z_]+)\s*\(", text)))
-    assert len(names) == 8
+    assert len(names) == 9
     for name in names:
         assert hasattr(layers._lib, name), name
 
@@ -98,9 +99,9 @@ def test_norm_backward_refuses(layers, bad, status):
 
 
 def ffn_forward(L, dtype=0, act=0, n=2, rows=3, width=4, hidden=5, x=X, g=W, u=W + 80, d=W + 160, stride=60, y=Y, ys=(12, 4), save=1, buffer=B,
-                nbytes=1 << 20):
+                nbytes=1 << 20, scratch=S, sbytes=1 << 30):
     return L._lib.svgd_gated_ffn_forward(dtype, act, n, rows, width, hidden, L._Rows(x, 12, 4), g, stride, u, stride, d, stride, L._Rows(y, *ys), save,
-                                         buffer, nbytes, None)
+                                         buffer, nbytes, scratch, sbytes, None)
 
 
 @pytest.mark.parametrize("bad,status", [
