@@ -95,7 +95,7 @@ template <int P, int STEP> struct RowsOfA { // STEP: 2 where the groups of 8 row
     int last;             // rows beyond this one: this one again
     uint32_t row_bytes;   // below 2^24
     f32x4 v[8];
-    static constexpr bool narrow = false;
+    static constexpr bool narrow = false, kStaged = true;
     __device__ __forceinline__ RowsOfA(const float *even, const float *odd, int64_t rows_left, int64_t width)
         : last(rows_left < 64 ? (int)rows_left - 1 : 63), row_bytes((uint32_t)width * 4)
     {
@@ -160,6 +160,7 @@ template <class T, int P> struct ColumnsOfA {
     uint32_t column; // the lane's first row (fewer than four rows: the first one)
     int rows;        // of them, if they are fewer than four; otherwise 4
     bool narrow;
+    static constexpr bool kStaged = false;
     typename Pack<T, 4>::raw v[8];
     __device__ __forceinline__ ColumnsOfA(const T *b, int64_t s, int64_t first, int64_t count)
         : base(b), stride(s), column(count < 4 ? 0 : (uint32_t)quad_of(first + 4 * quad_of_lane(), count)), rows(count < 4 ? (int)count : 4),
@@ -338,9 +339,9 @@ template <int NJ> struct Acc {
 };
 
 // Adds the product over the columns from begin (a multiple of kTileK) to end to acc.  Products of parts pa, pb with pa + pb beyond the last part are below 2^-24
-// (three parts; 2^-16 with two) of the whole and left out.  While the matrix cores work on a step, the next one's rows are
-// on their way, those of B then go to the other half of LDS, and those of A are split into the registers of the last
-// columns' blocks as these get free: one barrier per step, and nothing but it between one step's products and the next one's.
+// (three parts; 2^-16 with two) of the whole and left out.  While the matrix cores work on a step, the next one's rows of B go to the
+// other half of LDS and those of A are split into the registers of the last columns' blocks as these get free, and the rows of the
+// step after it are on their way: one barrier per step.
 // lds: 2 * PB * kPlane units; scratch: the wave's own kScratch floats.
 constexpr int kScratch = 64 * kTileK; // 64 rows of a step of A; 16 rows of 68 values of C
 template <class TL, int PA, int PB, class LA, class LB>
@@ -348,8 +349,11 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
 {
     if (begin >= K) return;
     constexpr int kOrder = (PA > PB ? PA : PB) - 1, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
-    constexpr int kLast = PB == 1 ? 2 : 1;
-    static_assert(NJ / 2 <= NJ - kLast, "every column once");
+    constexpr int kLast = NJ <= 4 ? 2 : PB == 3 ? 1 : 2; // columns that go block of A by block of A: as many as there are registers for
+    // Whether a step's rows are fetched during the whole step before it, or while it goes on: the former where there are registers for it
+    // and A needs no detour (hidden_grad_kernel of the large bf16 block 727 -> 705 us, gate_up_kernel 1096 -> 1179).
+    constexpr bool kAhead = !LA::kStaged && !(PA == 3 && PB == 3 && NJ > 4);
+    static_assert(kLast < NJ, "columns to begin with");
     const SplitConst sc = split_const();
     const int lane = threadIdx.x & 63;
     const int frag = unit_of(lane & 15, lane >> 4);
@@ -374,6 +378,7 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
     };
     const int64_t whole = a.narrow || b.narrow ? begin : K / kTileK * kTileK;
     if (whole > begin) {
+        const int64_t last = whole - kTileK; // (what is fetched ahead of the end is the last step again)
         b.fetch(begin);
         a.fetch(begin);
         __syncthreads(); // (an earlier product's last step has been read)
@@ -381,18 +386,31 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
         a.stage(scratch);
 #pragma unroll
         for (int ib = 0; ib < 4; ++ib) a.parts(ib, sc, fa[ib], scratch);
+        if constexpr (kAhead) {
+            b.fetch(begin + kTileK < last ? begin + kTileK : last);
+            a.fetch(begin + kTileK < last ? begin + kTileK : last);
+        }
         __syncthreads();
+        // (the scheduling barriers: the compiler would move the loads down to where their values are needed)
         for (int64_t k0 = begin + kTileK; k0 < whole; k0 += kTileK) {
-            b.fetch(k0);
-            __builtin_amdgcn_sched_barrier(0); // (the compiler would move the loads down to where their values are needed)
-            columns(0, NJ / 2 - 1);
-            b.store(lds + (kStage - stage), sc);
-            __builtin_amdgcn_sched_barrier(0);
-            a.fetch(k0);
-            __builtin_amdgcn_sched_barrier(0);
-            columns(NJ / 2 - 1, NJ - kLast);
-            __builtin_amdgcn_sched_barrier(0); // (and up to here what waits for A's)
-            a.stage(scratch);
+            const int64_t next = k0 + kTileK < last ? k0 + kTileK : last;
+            if constexpr (kAhead) {
+                b.store(lds + (kStage - stage), sc);
+                b.fetch(next);
+                __builtin_amdgcn_sched_barrier(0);
+                columns(0, NJ - kLast);
+            } else {
+                b.fetch(k0);
+                __builtin_amdgcn_sched_barrier(0);
+                columns(0, NJ / 2 - 1);
+                b.store(lds + (kStage - stage), sc);
+                __builtin_amdgcn_sched_barrier(0);
+                a.fetch(k0);
+                __builtin_amdgcn_sched_barrier(0);
+                columns(NJ / 2 - 1, NJ - kLast);
+                __builtin_amdgcn_sched_barrier(0);
+                a.stage(scratch);
+            }
             bf16x8 fb[kLast][PB];
 #pragma unroll
             for (int q = 0; q < kLast; ++q)
@@ -411,6 +429,7 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
                         }
                 a.parts(ib, sc, fa[ib], scratch);
             }
+            if constexpr (kAhead) a.fetch(next);
             stage = kStage - stage;
             __syncthreads();
         }

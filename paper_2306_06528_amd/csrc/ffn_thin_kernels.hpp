@@ -130,7 +130,7 @@ template <class T, int ACT, bool SAVE, int JB>
 __global__ __launch_bounds__(kThinBlock) void thin_gate_up_kernel(FfnShape s, ThinGrid grid, Rows<const T> x, Params gate, Params up, float *h,
                                                                   float *g_out, float *u_out)
 {
-    constexpr int P = kParts<T>, U = 2;
+    constexpr int P = kParts<T>, U = JB > 2 ? 1 : 2;
     const int lane = threadIdx.x & 63, particle = grid.particle();
     const int64_t i0 = grid.first(), i = i0 + (lane & 15) < s.hidden ? i0 + (lane & 15) : s.hidden - 1;
     const int kl = (lane >> 4) * 8;

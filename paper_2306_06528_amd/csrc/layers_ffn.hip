@@ -24,39 +24,45 @@ typedef Tile<4, 4> MiddleTile;
 typedef Tile<2, 4> SmallTile;
 struct KindOf {
     int i, j;
-    double step;  // time of a step (32 columns) of one tile when a CU is full, in steps of a large one
+    double step;   // time of a step (32 columns) of one tile on a full CU, in those of a large one
     int at_a_time; // workgroups on the whole part then
 };
 constexpr KindOf kKinds[kTileKinds] = {{LargeTile::kI, LargeTile::kJ, 1.0, 512}, {MiddleTile::kI, MiddleTile::kJ, 0.6, 512}, {SmallTile::kI, SmallTile::kJ, 0.6, 1024}};
 
+// What a launch takes, in steps of a large tile on a full CU (4.4 us fp32, 3 us bf16): workgroups of `longest` steps and `work` steps in all.  Fewer than
+// run at a time take as long as the longest, and that is 0.6 times as long where a CU has only half of them; of more, the last
+// ones end 0.4 of their length late.  Against measured times of 60 launches (8 shapes, kinds and parts): within 15 %, and what it finds cheapest
+// is within 5 % of the fastest.
+constexpr double kStart = 4.0; // steps until a workgroup's first rows are there, and for its results
+double launch_cost(TileKind kind, int64_t workgroups, double work, double longest)
+{
+    const KindOf &k = kKinds[kind];
+    if (workgroups <= k.at_a_time) return longest * k.step * (2 * workgroups <= k.at_a_time ? 0.6 : 1.0);
+    return (work / k.at_a_time + 0.4 * longest) * k.step;
+}
+double steps_of(int64_t columns, int parts) { return (double)(((columns + parts - 1) / parts + kTileK - 1) / kTileK) + kStart; }
+// Parts' sums are written and read once more: the launch that adds them up, and its bytes at 4 TB/s.
+double reduce_cost(int parts, int64_t floats) { return parts > 1 ? 1.0 + (double)floats * parts * 8.0 / 16e6 : 0.0; }
+
 struct Choice {
     TileKind kind;
     int parts;
-    double cost;
 };
 
-// The cheaper of the choices for `tiles` tiles over `columns` columns of each of n particles: time of the workgroups that run one after
-// another, kStart steps for the first rows of each and its results, and what adding up the parts takes.
-constexpr double kStart = 4.0, kReduce = 4.0;
-double cost_of(TileKind kind, int64_t tiles, int64_t columns, int parts)
+// The cheapest kind for C[j][i] of each of n particles over `columns` columns, and with `sums` (floats in a part's sums, 0: not
+// to be split) the cheapest number of parts.
+Choice choose(int n, int64_t i, int64_t j, int64_t columns, int per_i, int64_t sums)
 {
-    const KindOf &k = kKinds[kind];
-    const double steps = (double)((columns + parts - 1) / parts + kTileK - 1) / kTileK + kStart;
-    const int64_t all = tiles * parts, rounds = all / k.at_a_time, rest = all - rounds * k.at_a_time;
-    // the last ones have the CUs to themselves if they are few
-    const double last = rest == 0 ? 0.0 : rest * 2 <= k.at_a_time ? 0.6 : 1.0;
-    return ((double)rounds + last) * steps * k.step + (parts > 1 ? kReduce : 0.0);
-}
-
-Choice choose(int n, int64_t i, int64_t j, int64_t columns, int per_wave_i, bool may_split)
-{
-    Choice best{kLarge, 1, 0.0};
+    Choice best{kLarge, 1};
+    double least = 1e30;
     for (int kind = 0; kind < kTileKinds; ++kind) {
-        const int64_t t = n * tiles(i, kKinds[kind].i / per_wave_i) * tiles(j, kKinds[kind].j);
-        for (int parts = 1; parts <= (may_split ? 32 : 1); parts += parts < 4 ? 1 : parts < 8 ? 2 : parts < 16 ? 4 : 8) {
-            if (parts > 1 && (columns / parts < 4 * kTileK || t * (parts - 1) > 1024)) break;
-            const double c = cost_of((TileKind)kind, t, columns, parts);
-            if ((kind == 0 && parts == 1) || c < best.cost) best = {(TileKind)kind, parts, c};
+        const int64_t t = n * tiles(i, kKinds[kind].i / per_i) * tiles(j, kKinds[kind].j);
+        for (int parts = 1; parts <= (sums ? 32 : 1) && (parts == 1 || (columns / parts >= 4 * kTileK && t * parts <= 1024)); parts *= 2) {
+            const double steps = steps_of(columns, parts), c = launch_cost((TileKind)kind, t * parts, (double)(t * parts) * steps, steps) + reduce_cost(parts, sums);
+            if (c < least) {
+                least = c;
+                best = {(TileKind)kind, parts};
+            }
         }
     }
     return best;
@@ -67,38 +73,57 @@ template <class F> int with_tile(TileKind kind, F f)
     return kind == kLarge ? f(LargeTile{}) : kind == kMiddle ? f(MiddleTile{}) : f(SmallTile{});
 }
 
-constexpr int64_t kThinRows = 32; // up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp)
+// Up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp): 8 x 17 rows, 384 x 1,024 fp32,
+// forward 17 us, in tiles 114; backward 43 and 179.  Forward up to 64 rows where the tiles of g and u are few (8 x 64 rows of these 29 and 46,
+// 1 x 64 rows, 1,024 x 2,730 fp32 41 and 87, but 40 x 64 rows, 256 x 700 bf16, 240 tiles, 49 and 42).
+constexpr int64_t kThinRows = 32;
+bool thin_forward_rows(int n, int64_t rows, int64_t hidden)
+{
+    return rows <= kThinRows || (rows <= 64 && n * tiles(hidden, LargeTile::kI / 2) < 200);
+}
 
 int64_t width_ld(int64_t width) { return (width + 3) / 4 * 4; }
 
 struct ForwardPlan {
     Choice gate_up, down;
     ForwardPlan(int n, int64_t rows, int64_t width, int64_t hidden)
-        : gate_up(choose(n, hidden, rows, width, 2, false)), down(choose(n, width, rows, hidden, 1, true))
+        : gate_up(choose(n, hidden, rows, width, 2, 0)), down(choose(n, width, rows, hidden, 1, n * rows * width))
     {
-        if (rows <= kThinRows) down.parts = 1;
+        if (thin_forward_rows(n, rows, hidden)) down.parts = 1;
     }
     size_t scratch(int n, int64_t rows, int64_t width) const { return down.parts > 1 ? (size_t)down.parts * n * rows * width_ld(width) * 4 : 0; }
 };
 
-// The tiles of one launch are of one kind: that of most of them, dgate's and dup's.
+// The gradients' tiles are of one kind, being of one launch.  input_parts is 1 or even, see input_grad_tile.
 struct BackwardPlan {
-    Choice hidden, gradients;
-    int input_parts, gate_parts, down_parts;
+    Choice hidden;
+    TileKind gradients = kLarge;
+    int input_parts = 1, param_parts = 1;
     size_t hidden_floats, input_floats, gate_floats, down_floats;
-    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid)
-        : hidden(choose(n, hid, rows, width, 1, false)), gradients(choose(n, width, 3 * hid, rows, 1, true)), input_parts(1), gate_parts(gradients.parts),
-          down_parts(gradients.parts)
+    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid) : hidden(choose(n, hid, rows, width, 1, 0))
     {
-        const KindOf &k = kKinds[gradients.kind];
-        // dx: parts so that its workgroups take about as long as those of the other gradients
-        const int64_t t = n * tiles(width, k.i) * tiles(rows, k.j), steps = (rows + gate_parts - 1) / gate_parts;
-        if (rows > kThinRows)
-            while (input_parts < 32 && 2 * hid / (2 * input_parts) >= 4 * kTileK && t * input_parts < k.at_a_time && 2 * hid / input_parts > steps * 3 / 2) input_parts *= 2;
+        double least = 1e30;
+        for (int kind = 0; kind < kTileKinds; ++kind) {
+            const KindOf &k = kKinds[kind];
+            const int64_t params = 3 * n * tiles(width, k.i) * tiles(hid, k.j), input = rows > kThinRows ? n * tiles(width, k.i) * tiles(rows, k.j) : 0;
+            for (int pp = 1; pp <= 32 && (pp == 1 || (rows / pp >= 4 * kTileK && params * pp <= 1024)); pp *= 2)
+                for (int ip = 1; ip <= 32 && (ip == 1 || (2 * hid / ip >= 4 * kTileK && input * ip <= 1024 && input > 0)); ip *= 2) {
+                    const double of_params = steps_of(rows, pp), of_input = input ? steps_of(2 * hid, ip) : 0.0;
+                    const double c = launch_cost((TileKind)kind, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
+                                                 of_params > of_input ? of_params : of_input) +
+                                     reduce_cost(pp, 3 * n * width * hid) + (pp > 1 ? 1.0 : 0.0) + reduce_cost(ip, n * rows * width);
+                    if (c < least) {
+                        least = c;
+                        gradients = (TileKind)kind;
+                        param_parts = pp;
+                        input_parts = ip;
+                    }
+                }
+        }
         hidden_floats = (size_t)n * rows * hidden_ld(hid);
         input_floats = input_parts > 1 ? (size_t)input_parts * n * rows * width_ld(width) : 0;
-        gate_floats = gate_parts > 1 ? (size_t)gate_parts * n * 2 * width * hid : 0;
-        down_floats = down_parts > 1 ? (size_t)down_parts * n * width * hid : 0;
+        gate_floats = param_parts > 1 ? (size_t)param_parts * n * 2 * width * hid : 0;
+        down_floats = param_parts > 1 ? (size_t)param_parts * n * width * hid : 0;
     }
     size_t scratch() const { return (2 * hidden_floats + input_floats + gate_floats + down_floats + 16) * 4; } // (each begins on 16 bytes)
 };
@@ -148,8 +173,10 @@ template <class T, int ACT> int forward(const Call &c, const svgd_rows &x, const
 {
     const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
     float *const h = buffer, *const g = buffer + plane, *const u = buffer + 2 * plane;
-    if (c.s.rows <= kThinRows)
-        return c.s.rows <= 16 ? thin_forward<T, ACT, 1>(c, x, y, h, g, u, save) : thin_forward<T, ACT, 2>(c, x, y, h, g, u, save);
+    if (thin_forward_rows(c.n, c.s.rows, c.s.hidden))
+        return c.s.rows <= 16   ? thin_forward<T, ACT, 1>(c, x, y, h, g, u, save)
+               : c.s.rows <= 32 ? thin_forward<T, ACT, 2>(c, x, y, h, g, u, save)
+                                : thin_forward<T, ACT, 4>(c, x, y, h, g, u, save);
     const ForwardPlan plan(c.n, c.s.rows, c.s.width, c.s.hidden);
     int rc = with_tile(plan.gate_up.kind, [&](auto tile) {
         using TL = decltype(tile);
@@ -197,7 +224,7 @@ int backward(const Call &c, const svgd_rows &dy, const svgd_rows &x, const float
     }
     const bool input = !thin && dx.data;
     if (!input && !gates && !ddown.p) return SVGD_OK;
-    int rc = with_tile(plan.gradients.kind, [&](auto tile) {
+    int rc = with_tile(plan.gradients, [&](auto tile) {
         using TL = decltype(tile);
         const int64_t particle = c.s.rows * c.s.hidden_ld, row = c.s.hidden_ld;
         const int high = (int)tiles(c.s.hidden, TL::kJ);
@@ -211,10 +238,10 @@ int backward(const Call &c, const svgd_rows &dy, const svgd_rows &x, const float
         WeightGrad<T, float> of_gates{}, of_down{};
         const Rows<const float> dgs{dg, particle, row}, dus{du, particle, row}, hs{h, particle, row};
         if (gates)
-            of_gates = {TileGrid(c.n, wide, (int64_t)high * gates, c.s.rows, plan.gate_parts), c.s.width, c.s.hidden, high, gates, in<T>(x),
+            of_gates = {TileGrid(c.n, wide, (int64_t)high * gates, c.s.rows, plan.param_parts), c.s.width, c.s.hidden, high, gates, in<T>(x),
                         {dgate.p ? dgs : dus, dus}, {dgate.p ? dgate : dup, dup}, gate_partial};
         if (ddown.p)
-            of_down = {TileGrid(c.n, wide, high, c.s.rows, plan.down_parts), c.s.width, c.s.hidden, high, 1, in<T>(dy), {hs, hs}, {ddown, ddown}, down_partial};
+            of_down = {TileGrid(c.n, wide, high, c.s.rows, plan.param_parts), c.s.width, c.s.hidden, high, 1, in<T>(dy), {hs, hs}, {ddown, ddown}, down_partial};
         if (input_grid.total < 0 || of_gates.grid.total < 0 || of_down.grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
         gradients_kernel<TL, T><<<input_grid.blocks() + of_gates.grid.blocks() + of_down.grid.blocks(), TL::kThreads, 0, c.stream>>>(
             c.s, input_grid, dg, du, c.gate, c.up, out<T>(dx), dx_partial, of_gates, of_down, accumulate);
@@ -223,13 +250,13 @@ int backward(const Call &c, const svgd_rows &dy, const svgd_rows &x, const float
     if (rc) return rc;
     if (input && plan.input_parts > 1 && (rc = reduce_rows<T>(c, dx_partial, plan.input_parts, out<T>(dx)))) return rc;
     const int64_t size = c.s.width * c.s.hidden;
-    if (gates && plan.gate_parts > 1) {
-        reduce_params_kernel<<<(unsigned)tiles(c.n * gates * size, 256), 256, 0, c.stream>>>(c.n, size, gates, gate_partial, plan.gate_parts,
+    if (gates && plan.param_parts > 1) {
+        reduce_params_kernel<<<(unsigned)tiles(c.n * gates * size, 256), 256, 0, c.stream>>>(c.n, size, gates, gate_partial, plan.param_parts,
                                                                                             dgate.p ? dgate : dup, dup, accumulate);
         if ((rc = launched())) return rc;
     }
-    if (ddown.p && plan.down_parts > 1) {
-        reduce_params_kernel<<<(unsigned)tiles(c.n * size, 256), 256, 0, c.stream>>>(c.n, size, 1, down_partial, plan.down_parts, ddown, ddown, accumulate);
+    if (ddown.p && plan.param_parts > 1) {
+        reduce_params_kernel<<<(unsigned)tiles(c.n * size, 256), 256, 0, c.stream>>>(c.n, size, 1, down_partial, plan.param_parts, ddown, ddown, accumulate);
         rc = launched();
     }
     return rc;
