@@ -26,8 +26,8 @@ template <int W, int NJ> struct Tile {
 };
 
 template <class T> constexpr int kParts = 3;
-template <> constexpr int kParts<f16_t> = 2;
-template <> constexpr int kParts<bf16_t> = 1;
+template <> inline constexpr int kParts<f16_t> = 2;
+template <> inline constexpr int kParts<bf16_t> = 1;
 
 // B's rows in LDS, one plane per part, each row four 16-byte units (8 values of k).  Two rows share 128 bytes; which half a row takes
 // and where its units lie in it is permuted so that neither 8 rows in succession nor 8 every-second rows (what eight
@@ -349,7 +349,7 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
 {
     if (begin >= K) return;
     constexpr int kOrder = (PA > PB ? PA : PB) - 1, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
-    constexpr int kLast = NJ <= 4 ? 2 : PB == 3 ? 1 : 2; // columns that go block of A by block of A: as many as there are registers for
+    constexpr int kLast = NJ <= 2 ? 1 : NJ <= 4 ? 2 : PB == 3 ? 1 : 2; // columns that go block of A by block of A: as many as there are registers for
     // Whether a step's rows are fetched during the whole step before it, or while it goes on: the former where there are registers for it
     // and A needs no detour (hidden_grad_kernel of the large bf16 block 727 -> 705 us, gate_up_kernel 1096 -> 1179).
     constexpr bool kAhead = !LA::kStaged && !(PA == 3 && PB == 3 && NJ > 4);
@@ -773,7 +773,7 @@ template <class T> __global__ __launch_bounds__(256) void reduce_rows_kernel(Ffn
 }
 
 // The same for gradients of parameters: `size` values of each of `outs` per particle.
-__global__ __launch_bounds__(256) void reduce_params_kernel(int n, int64_t size, int outs, const float *partial, int parts, Params out0, Params out1,
+static __global__ __launch_bounds__(256) void reduce_params_kernel(int n, int64_t size, int outs, const float *partial, int parts, Params out0, Params out1,
                                                             bool accumulate)
 {
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, each = n * outs * size;

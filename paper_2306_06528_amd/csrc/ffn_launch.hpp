@@ -1,0 +1,284 @@
+// Which tiles a call takes, into how many parts its columns go, and the launches of both passes.  The kernels' instances are compiled
+// type by type (layers_ffn_*.hip).
+#pragma once
+#include "ffn_thin_kernels.hpp"
+
+namespace svgd {
+
+inline int64_t hidden_ld(int64_t hidden) { return (hidden + 31) / 32 * 32; } // rows of the buffers start on 128 bytes
+
+inline int64_t tiles(int64_t size, int tile) { return (size + tile - 1) / tile; }
+
+// ---------------------------------------------------------------------------------------------
+// Which tiles, and into how many parts the columns go: by sizes alone, the same for every type
+// ---------------------------------------------------------------------------------------------
+enum TileKind { kLarge, kSmall, kTiny, kTileKinds };
+typedef Tile<4, 8> LargeTile;
+typedef Tile<2, 4> SmallTile;
+typedef Tile<1, 2> TinyTile;
+struct KindOf {
+    int i, j;
+    double step;   // time of a step (32 columns) of one tile on a full CU, in those of a large one
+    int at_a_time; // workgroups on the whole part then
+};
+constexpr KindOf kKinds[kTileKinds] = {{LargeTile::kI, LargeTile::kJ, 1.0, 512}, {SmallTile::kI, SmallTile::kJ, 0.6, 1024}, {TinyTile::kI, TinyTile::kJ, 0.35, 2048}};
+
+// What a launch takes, in steps of a large tile on a full CU (4.4 us fp32, 3 us bf16): workgroups of `longest` steps and `work` steps in all.  Fewer than
+// run at a time take as long as the longest, and that is 0.6 times as long where a CU has only half of them; of more, the last
+// ones end 0.4 of their length late.  Of the kinds and parts measured at 15 shapes (1 to 57 particles of 64 to 16,000 rows, 32 to 1,322 wide)
+// what it finds cheapest takes up to 20 % more than the fastest where a pass takes less than 100 us, 5 % beyond.
+constexpr double kStart = 4.0; // steps until a workgroup's first rows are there, and for its results
+inline double launch_cost(TileKind kind, int64_t workgroups, double work, double longest)
+{
+    const KindOf &k = kKinds[kind];
+    if (workgroups <= k.at_a_time) return longest * k.step * (2 * workgroups <= k.at_a_time ? 0.6 : 1.0);
+    return (work / k.at_a_time + 0.4 * longest) * k.step;
+}
+inline double steps_of(int64_t columns, int parts) { return (double)(((columns + parts - 1) / parts + kTileK - 1) / kTileK) + kStart; }
+// Parts' sums are written and read once more: the launch that adds them up, and its bytes at 4 TB/s.
+inline double reduce_cost(int parts, int64_t floats) { return parts > 1 ? 0.6 + (double)floats * parts * 8.0 / 16e6 : 0.0; }
+
+struct Choice {
+    TileKind kind;
+    int parts;
+};
+
+// The cheapest kind for C[j][i] of each of n particles over `columns` columns, and with `sums` (floats in a part's sums, 0: not
+// to be split) the cheapest number of parts.
+inline Choice choose(int n, int64_t i, int64_t j, int64_t columns, int per_i, int64_t sums)
+{
+    Choice best{kLarge, 1};
+    double least = 1e30;
+    for (int kind = 0; kind < kTileKinds; ++kind) {
+        const int64_t t = n * tiles(i, kKinds[kind].i / per_i) * tiles(j, kKinds[kind].j);
+        for (int parts = 1; parts <= (sums ? 32 : 1) && (parts == 1 || (columns / parts >= 4 * kTileK && t * parts <= 1024)); parts *= 2) {
+            const double steps = steps_of(columns, parts), c = launch_cost((TileKind)kind, t * parts, (double)(t * parts) * steps, steps) + reduce_cost(parts, sums);
+            if (c < least) {
+                least = c;
+                best = {(TileKind)kind, parts};
+            }
+        }
+    }
+    return best;
+}
+
+template <class F> int with_tile(TileKind kind, F f)
+{
+    return kind == kLarge ? f(LargeTile{}) : kind == kSmall ? f(SmallTile{}) : f(TinyTile{});
+}
+
+// Up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp): 8 x 17 rows, 384 x 1,024 fp32,
+// forward 17 us, in tiles 114; backward 43 and 179.  Forward up to 64 rows where the tiles of g and u are few (8 x 64 rows of these 29 and 46,
+// 1 x 64 rows, 1,024 x 2,730 fp32 41 and 87, but 40 x 64 rows, 256 x 700 bf16, 240 tiles, 49 and 42).
+constexpr int64_t kThinRows = 32;
+inline bool thin_forward_rows(int n, int64_t rows, int64_t hidden)
+{
+    return rows <= kThinRows || (rows <= 64 && n * tiles(hidden, LargeTile::kI / 2) < 200);
+}
+
+inline int64_t width_ld(int64_t width) { return (width + 3) / 4 * 4; }
+
+struct ForwardPlan {
+    Choice gate_up, down;
+    ForwardPlan(int n, int64_t rows, int64_t width, int64_t hidden)
+        : gate_up(choose(n, hidden, rows, width, 2, 0)), down(choose(n, width, rows, hidden, 1, n * rows * width))
+    {
+        if (thin_forward_rows(n, rows, hidden)) down.parts = 1;
+    }
+    size_t scratch(int n, int64_t rows, int64_t width) const { return down.parts > 1 ? (size_t)down.parts * n * rows * width_ld(width) * 4 : 0; }
+};
+
+// The gradients' tiles are of one kind, being of one launch.  input_parts is 1 or even, see input_grad_tile.
+struct BackwardPlan {
+    Choice hidden;
+    TileKind gradients = kLarge;
+    int input_parts = 1, param_parts = 1;
+    size_t hidden_floats, input_floats, gate_floats, down_floats;
+    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid) : hidden(choose(n, hid, rows, width, 1, 0))
+    {
+        double least = 1e30;
+        for (int kind = 0; kind < kTileKinds; ++kind) {
+            const KindOf &k = kKinds[kind];
+            const int64_t params = 3 * n * tiles(width, k.i) * tiles(hid, k.j), input = rows > kThinRows ? n * tiles(width, k.i) * tiles(rows, k.j) : 0;
+            for (int pp = 1; pp <= 32 && (pp == 1 || (rows / pp >= 4 * kTileK && params * pp <= 1024)); pp *= 2)
+                for (int ip = 1; ip <= 32 && (ip == 1 || (2 * hid / ip >= 4 * kTileK && input * ip <= 1024 && input > 0)); ip *= 2) {
+                    const double of_params = steps_of(rows, pp), of_input = input ? steps_of(2 * hid, ip) : 0.0;
+                    const double c = launch_cost((TileKind)kind, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
+                                                 of_params > of_input ? of_params : of_input) +
+                                     reduce_cost(pp, 3 * n * width * hid) + (pp > 1 ? 0.6 : 0.0) + reduce_cost(ip, n * rows * width);
+                    if (c < least) {
+                        least = c;
+                        gradients = (TileKind)kind;
+                        param_parts = pp;
+                        input_parts = ip;
+                    }
+                }
+        }
+        hidden_floats = (size_t)n * rows * hidden_ld(hid);
+        input_floats = input_parts > 1 ? (size_t)input_parts * n * rows * width_ld(width) : 0;
+        gate_floats = param_parts > 1 ? (size_t)param_parts * n * 2 * width * hid : 0;
+        down_floats = param_parts > 1 ? (size_t)param_parts * n * width * hid : 0;
+    }
+    size_t scratch() const { return (2 * hidden_floats + input_floats + gate_floats + down_floats + 16) * 4; } // (each begins on 16 bytes)
+};
+inline size_t aligned4(size_t floats) { return (floats + 3) & ~(size_t)3; }
+
+struct FfnCall {
+    int dtype, activation, n;
+    FfnShape s;
+    Params gate, up, down;
+    hipStream_t stream;
+};
+
+template <class T> Rows<const T> in(const svgd_rows &r) { return {(const T *)r.data, r.particle_stride, r.row_stride}; }
+template <class T> Rows<T> out(const svgd_rows &r) { return {(T *)r.data, r.particle_stride, r.row_stride}; }
+inline int launched() { return hipGetLastError() == hipSuccess ? SVGD_OK : SVGD_ERR_DEVICE; }
+
+template <class T> int reduce_rows(const FfnCall &c, const float *partial, int parts, const Rows<T> &y)
+{
+    const int64_t quads = c.n * c.s.rows * c.s.width_ld / 4;
+    reduce_rows_kernel<T><<<(unsigned)tiles(quads, 256), 256, 0, c.stream>>>(c.s, partial, parts, y);
+    return launched();
+}
+
+template <class T, int ACT, int JB> int thin_forward(const FfnCall &c, const svgd_rows &x, const svgd_rows &y, float *h, float *g, float *u, bool save)
+{
+    const ThinGrid first(c.s.hidden, 16), second(c.s.width, 16);
+    const int blocks = c.n * first.per_particle;
+    if (save) thin_gate_up_kernel<T, ACT, true, JB><<<blocks, kThinBlock, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, g, u);
+    else thin_gate_up_kernel<T, ACT, false, JB><<<blocks, kThinBlock, 0, c.stream>>>(c.s, first, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
+    if (const int rc = launched()) return rc;
+    thin_down_kernel<T, JB><<<c.n * second.per_particle, kThinBlock, 0, c.stream>>>(c.s, second, h, c.down, out<T>(y));
+    return launched();
+}
+
+template <class T, int ACT, int JB>
+int thin_backward(const FfnCall &c, const svgd_rows &dy, const float *g, const float *u, const svgd_rows &dx, float *dg, float *du)
+{
+    const ThinGrid hidden(c.s.hidden, 32), input(c.s.width, 32);
+    thin_hidden_grad_kernel<T, ACT, JB><<<c.n * hidden.per_particle, kThinBlock, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
+    const int rc = launched();
+    if (rc || !dx.data) return rc;
+    thin_input_grad_kernel<T, JB><<<c.n * input.per_particle, kThinBlock, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
+    return launched();
+}
+
+template <class T, int ACT> int forward_as(const FfnCall &c, const svgd_rows &x, const svgd_rows &y, float *buffer, bool save, float *scratch)
+{
+    const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
+    float *const h = buffer, *const g = buffer + plane, *const u = buffer + 2 * plane;
+    if (thin_forward_rows(c.n, c.s.rows, c.s.hidden))
+        return c.s.rows <= 16   ? thin_forward<T, ACT, 1>(c, x, y, h, g, u, save)
+               : c.s.rows <= 32 ? thin_forward<T, ACT, 2>(c, x, y, h, g, u, save)
+                                : thin_forward<T, ACT, 4>(c, x, y, h, g, u, save);
+    const ForwardPlan plan(c.n, c.s.rows, c.s.width, c.s.hidden);
+    int rc = with_tile(plan.gate_up.kind, [&](auto tile) {
+        using TL = decltype(tile);
+        const TileGrid grid(c.n, tiles(c.s.hidden, TL::kI / 2), tiles(c.s.rows, TL::kJ), c.s.width, 1);
+        if (grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+        if (save) gate_up_kernel<TL, T, ACT, true><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(x), c.gate, c.up, h, g, u);
+        else gate_up_kernel<TL, T, ACT, false><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(x), c.gate, c.up, h, nullptr, nullptr);
+        return launched();
+    });
+    if (rc) return rc;
+    rc = with_tile(plan.down.kind, [&](auto tile) {
+        using TL = decltype(tile);
+        const TileGrid grid(c.n, tiles(c.s.width, TL::kI), tiles(c.s.rows, TL::kJ), c.s.hidden, plan.down.parts);
+        if (grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+        down_kernel<TL, T><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, h, c.down, out<T>(y), scratch);
+        return launched();
+    });
+    if (rc || plan.down.parts == 1) return rc;
+    return reduce_rows<T>(c, scratch, plan.down.parts, out<T>(y));
+}
+
+template <class T, int ACT>
+int backward_as(const FfnCall &c, const svgd_rows &dy, const svgd_rows &x, const float *saved, const svgd_rows &dx, const Params &dgate, const Params &dup,
+             const Params &ddown, bool accumulate, float *scratch)
+{
+    const int64_t plane = c.n * c.s.rows * c.s.hidden_ld;
+    const float *const h = saved, *const g = saved + plane, *const u = saved + 2 * plane;
+    const BackwardPlan plan(c.n, c.s.rows, c.s.width, c.s.hidden);
+    float *const dg = scratch, *const du = dg + plan.hidden_floats, *const dx_partial = du + plan.hidden_floats;
+    float *const gate_partial = dx_partial + aligned4(plan.input_floats), *const down_partial = gate_partial + aligned4(plan.gate_floats);
+    const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0);
+    const bool thin = c.s.rows <= kThinRows;
+    if (thin && c.s.rows > 0 && (dx.data || gates)) {
+        if (const int rc = c.s.rows <= 16 ? thin_backward<T, ACT, 1>(c, dy, g, u, dx, dg, du) : thin_backward<T, ACT, 2>(c, dy, g, u, dx, dg, du)) return rc;
+    }
+    if (!thin && (dx.data || gates)) {
+        const int rc = with_tile(plan.hidden.kind, [&](auto tile) {
+            using TL = decltype(tile);
+            const TileGrid grid(c.n, tiles(c.s.hidden, TL::kI), tiles(c.s.rows, TL::kJ), c.s.width, 1);
+            if (grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+            hidden_grad_kernel<TL, T, ACT><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(dy), c.down, g, u, dg, du);
+            return launched();
+        });
+        if (rc) return rc;
+    }
+    const bool input = !thin && dx.data;
+    if (!input && !gates && !ddown.p) return SVGD_OK;
+    int rc = with_tile(plan.gradients, [&](auto tile) {
+        using TL = decltype(tile);
+        const int64_t particle = c.s.rows * c.s.hidden_ld, row = c.s.hidden_ld;
+        const int high = (int)tiles(c.s.hidden, TL::kJ);
+        const int64_t wide = tiles(c.s.width, TL::kI);
+        TileGrid input_grid;
+        if (input) {
+            const int parts = plan.input_parts;
+            input_grid = TileGrid(c.n, wide, tiles(c.s.rows, TL::kJ), c.s.hidden, parts);
+            if (parts > 1) input_grid.per = ((c.s.hidden + parts / 2 - 1) / (parts / 2) + kTileK - 1) / kTileK * kTileK; // half of the parts for either half
+        }
+        WeightGrad<T, float> of_gates{}, of_down{};
+        const Rows<const float> dgs{dg, particle, row}, dus{du, particle, row}, hs{h, particle, row};
+        if (gates)
+            of_gates = {TileGrid(c.n, wide, (int64_t)high * gates, c.s.rows, plan.param_parts), c.s.width, c.s.hidden, high, gates, in<T>(x),
+                        {dgate.p ? dgs : dus, dus}, {dgate.p ? dgate : dup, dup}, gate_partial};
+        if (ddown.p)
+            of_down = {TileGrid(c.n, wide, high, c.s.rows, plan.param_parts), c.s.width, c.s.hidden, high, 1, in<T>(dy), {hs, hs}, {ddown, ddown}, down_partial};
+        if (input_grid.total < 0 || of_gates.grid.total < 0 || of_down.grid.total < 0) return (int)SVGD_ERR_TOO_LARGE;
+        gradients_kernel<TL, T><<<input_grid.blocks() + of_gates.grid.blocks() + of_down.grid.blocks(), TL::kThreads, 0, c.stream>>>(
+            c.s, input_grid, dg, du, c.gate, c.up, out<T>(dx), dx_partial, of_gates, of_down, accumulate);
+        return launched();
+    });
+    if (rc) return rc;
+    if (input && plan.input_parts > 1 && (rc = reduce_rows<T>(c, dx_partial, plan.input_parts, out<T>(dx)))) return rc;
+    const int64_t size = c.s.width * c.s.hidden;
+    if (gates && plan.param_parts > 1) {
+        reduce_params_kernel<<<(unsigned)tiles(c.n * gates * size, 256), 256, 0, c.stream>>>(c.n, size, gates, gate_partial, plan.param_parts,
+                                                                                            dgate.p ? dgate : dup, dup, accumulate);
+        if ((rc = launched())) return rc;
+    }
+    if (ddown.p && plan.param_parts > 1) {
+        reduce_params_kernel<<<(unsigned)tiles(c.n * size, 256), 256, 0, c.stream>>>(c.n, size, 1, down_partial, plan.param_parts, ddown, ddown, accumulate);
+        rc = launched();
+    }
+    return rc;
+}
+
+template <class T> int ffn_forward(const FfnCall &c, const svgd_rows &x, const svgd_rows &y, float *buffer, bool save, float *scratch)
+{
+    return c.activation == SVGD_SILU ? forward_as<T, SVGD_SILU>(c, x, y, buffer, save, scratch) : forward_as<T, SVGD_GELU>(c, x, y, buffer, save, scratch);
+}
+
+template <class T>
+int ffn_backward(const FfnCall &c, const svgd_rows &dy, const svgd_rows &x, const float *saved, const svgd_rows &dx, const Params &dgate, const Params &dup,
+                 const Params &ddown, bool accumulate, float *scratch)
+{
+    return c.activation == SVGD_SILU ? backward_as<T, SVGD_SILU>(c, dy, x, saved, dx, dgate, dup, ddown, accumulate, scratch)
+                                     : backward_as<T, SVGD_GELU>(c, dy, x, saved, dx, dgate, dup, ddown, accumulate, scratch);
+}
+
+#ifndef SVGD_FFN_TYPE
+extern template int ffn_forward<float>(const FfnCall &, const svgd_rows &, const svgd_rows &, float *, bool, float *);
+extern template int ffn_forward<bf16_t>(const FfnCall &, const svgd_rows &, const svgd_rows &, float *, bool, float *);
+extern template int ffn_forward<f16_t>(const FfnCall &, const svgd_rows &, const svgd_rows &, float *, bool, float *);
+extern template int ffn_backward<float>(const FfnCall &, const svgd_rows &, const svgd_rows &, const float *, const svgd_rows &, const Params &,
+                                        const Params &, const Params &, bool, float *);
+extern template int ffn_backward<bf16_t>(const FfnCall &, const svgd_rows &, const svgd_rows &, const float *, const svgd_rows &, const Params &,
+                                         const Params &, const Params &, bool, float *);
+extern template int ffn_backward<f16_t>(const FfnCall &, const svgd_rows &, const svgd_rows &, const float *, const svgd_rows &, const Params &,
+                                        const Params &, const Params &, bool, float *);
+#endif
+
+} // namespace svgd
