@@ -5,13 +5,14 @@
 //     dx = dg Wg + du Wu                                         input_grad_kernel
 //     dWg = dg^T x, dWu = du^T x, dWd = dy^T h                   weight_grad_kernel
 //
-// All of them are one tile product, C[j][i] = sum_k A[i][k] B[j][k], 128 x 128 values of C per workgroup of four waves
-// of 64 x 64.  Operands are fp32 or 16 bits wide in memory; on their way into LDS they become bf16 parts whose sum is the value
+// All of them are one tile product, C[j][i] = sum_k A[i][k] B[j][k], 256 x 128 values of C (i x j) per workgroup of four waves of 64 x 128, or
+// less where there are few tiles (ffn_launch.hpp).  Operands are fp32 or 16 bits wide in memory; on their way into LDS they become bf16 parts whose sum is the value
 // EXACTLY (split3: three parts of an fp32 value, two of an fp16 one, one of a bf16 one), and the matrix cores
 // add up the products of parts that are not below 2^-24 of the whole: six for two fp32 operands, three for fp32 and bf16.  That is
 // the accuracy of fp32 products at 2.5 PFLOP/s / 6 (or / 3), where the fp32 matrix instructions end at 157 TFLOP/s; and
 // since each part is read from LDS once for several products, LDS keeps up with half the traffic a
-// plain bf16 product needs.
+// plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 4.95 PFLOP
+// of theirs and take 4.81 ms, 1,030 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,113 on the same card).
 #pragma once
 #include "layer_common.hpp"
 
@@ -350,9 +351,10 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
     if (begin >= K) return;
     constexpr int kOrder = (PA > PB ? PA : PB) - 1, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
     constexpr int kLast = NJ <= 2 ? 1 : NJ <= 4 ? 2 : PB == 3 ? 1 : 2; // columns that go block of A by block of A: as many as there are registers for
-    // Whether a step's rows are fetched during the whole step before it, or while it goes on: the former where there are registers for it
-    // and A needs no detour (hidden_grad_kernel of the large bf16 block 727 -> 705 us, gate_up_kernel 1096 -> 1179).
-    constexpr bool kAhead = !LA::kStaged && !(PA == 3 && PB == 3 && NJ > 4);
+    // Whether a step's rows are fetched during the whole step before it, or while it goes on: the former where there are registers for it;
+    // in large tiles not if A takes the detour through LDS (large bf16 block: hidden_grad_kernel 705 us, otherwise 727, but
+    // gate_up_kernel 1179 and 1096; tiles of 64 x 32: 1 x 500 x 256 x 700 fp32 forward 25.0 and 27.0).
+    constexpr bool kAhead = NJ <= 4 || (!LA::kStaged && !(PA == 3 && PB == 3));
     static_assert(kLast < NJ, "columns to begin with");
     const SplitConst sc = split_const();
     const int lane = threadIdx.x & 63;
@@ -399,6 +401,10 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
                 b.fetch(next);
                 __builtin_amdgcn_sched_barrier(0);
                 columns(0, NJ - kLast);
+                if constexpr (LA::kStaged) {
+                    a.stage(scratch);
+                    a.fetch(next);
+                }
             } else {
                 b.fetch(k0);
                 __builtin_amdgcn_sched_barrier(0);
@@ -429,7 +435,7 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
                         }
                 a.parts(ib, sc, fa[ib], scratch);
             }
-            if constexpr (kAhead) a.fetch(next);
+            if constexpr (kAhead && !LA::kStaged) a.fetch(next);
             stage = kStage - stage;
             __syncthreads();
         }

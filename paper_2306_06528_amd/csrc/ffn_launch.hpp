@@ -17,24 +17,29 @@ typedef Tile<4, 8> LargeTile;
 typedef Tile<2, 4> SmallTile;
 typedef Tile<1, 2> TinyTile;
 struct KindOf {
-    int i, j;
-    double step;   // time of a step (32 columns) of one tile on a full CU, in those of a large one
-    int at_a_time; // workgroups on the whole part then
+    int i, j, at_a_time; // workgroups that run at a time on the whole part
 };
-constexpr KindOf kKinds[kTileKinds] = {{LargeTile::kI, LargeTile::kJ, 1.0, 512}, {SmallTile::kI, SmallTile::kJ, 0.6, 1024}, {TinyTile::kI, TinyTile::kJ, 0.35, 2048}};
+constexpr KindOf kKinds[kTileKinds] = {{LargeTile::kI, LargeTile::kJ, 512}, {SmallTile::kI, SmallTile::kJ, 1024}, {TinyTile::kI, TinyTile::kJ, 2048}};
 
-// What a launch takes, in steps of a large tile on a full CU (4.4 us fp32, 3 us bf16): workgroups of `longest` steps and `work` steps in all.  Fewer than
-// run at a time take as long as the longest, and that is 0.6 times as long where a CU has only half of them; of more, the last
-// ones end 0.4 of their length late.  Of the kinds and parts measured at 15 shapes (1 to 57 particles of 64 to 16,000 rows, 32 to 1,322 wide)
-// what it finds cheapest takes up to 20 % more than the fastest where a pass takes less than 100 us, 5 % beyond.
-constexpr double kStart = 4.0; // steps until a workgroup's first rows are there, and for its results
-inline double launch_cost(TileKind kind, int64_t workgroups, double work, double longest)
+// What a launch takes, in steps (32 columns) of a large tile on a full CU (4.4 us fp32, 3 us bf16): workgroups of `longest` steps and `work` steps
+// in all.  Fewer than run at a time take as long as the longest, and that is `half` times as long where a CU has only half of them;
+// of more, the last ones end 0.4 of their length late.  Of the kinds and parts measured at 15 shapes (1 to 57 particles of 64 to 16,000 rows, 32 to
+// 1,322 wide) what it finds cheapest takes up to 20 % more than the fastest where a pass takes less than 100 us, 5 % beyond.
+struct Rates {
+    double step[kTileKinds], half, start; // a tile's step; see above; steps until a workgroup's first rows are there, and for its results
+};
+constexpr Rates kUsual = {{1.0, 0.6, 0.35}, 0.6, 4.0};
+// y = h down^T: the one product whose operands both lie along the columns, h of three parts.  Small tiles cost more there (at 15 shapes, 1 to 40 particles
+// of 64 to 16,000 rows, 64 to 1,024 wide, this finds the fastest or one within 5 % of it; with the usual ones forward took 8 x 1,576 x 384 x
+// 1,024 bf16 146 us for 134, 2 x 3,000 x 768 x 2,048 fp32 345 for 299).
+constexpr Rates kOfDown = {{1.0, 0.6, 0.5}, 0.8, 3.0};
+inline double launch_cost(const Rates &r, TileKind kind, int64_t workgroups, double work, double longest)
 {
-    const KindOf &k = kKinds[kind];
-    if (workgroups <= k.at_a_time) return longest * k.step * (2 * workgroups <= k.at_a_time ? 0.6 : 1.0);
-    return (work / k.at_a_time + 0.4 * longest) * k.step;
+    const int at_a_time = kKinds[kind].at_a_time;
+    if (workgroups <= at_a_time) return longest * r.step[kind] * (2 * workgroups <= at_a_time ? r.half : 1.0);
+    return (work / at_a_time + 0.4 * longest) * r.step[kind];
 }
-inline double steps_of(int64_t columns, int parts) { return (double)(((columns + parts - 1) / parts + kTileK - 1) / kTileK) + kStart; }
+inline double steps_of(const Rates &r, int64_t columns, int parts) { return (double)(((columns + parts - 1) / parts + kTileK - 1) / kTileK) + r.start; }
 // Parts' sums are written and read once more: the launch that adds them up, and its bytes at 4 TB/s.
 inline double reduce_cost(int parts, int64_t floats) { return parts > 1 ? 0.6 + (double)floats * parts * 8.0 / 16e6 : 0.0; }
 
@@ -45,14 +50,14 @@ struct Choice {
 
 // The cheapest kind for C[j][i] of each of n particles over `columns` columns, and with `sums` (floats in a part's sums, 0: not
 // to be split) the cheapest number of parts.
-inline Choice choose(int n, int64_t i, int64_t j, int64_t columns, int per_i, int64_t sums)
+inline Choice choose(const Rates &r, int n, int64_t i, int64_t j, int64_t columns, int per_i, int64_t sums)
 {
     Choice best{kLarge, 1};
     double least = 1e30;
     for (int kind = 0; kind < kTileKinds; ++kind) {
         const int64_t t = n * tiles(i, kKinds[kind].i / per_i) * tiles(j, kKinds[kind].j);
         for (int parts = 1; parts <= (sums ? 32 : 1) && (parts == 1 || (columns / parts >= 4 * kTileK && t * parts <= 1024)); parts *= 2) {
-            const double steps = steps_of(columns, parts), c = launch_cost((TileKind)kind, t * parts, (double)(t * parts) * steps, steps) + reduce_cost(parts, sums);
+            const double steps = steps_of(r, columns, parts), c = launch_cost(r, (TileKind)kind, t * parts, (double)(t * parts) * steps, steps) + reduce_cost(parts, sums);
             if (c < least) {
                 least = c;
                 best = {(TileKind)kind, parts};
@@ -81,7 +86,7 @@ inline int64_t width_ld(int64_t width) { return (width + 3) / 4 * 4; }
 struct ForwardPlan {
     Choice gate_up, down;
     ForwardPlan(int n, int64_t rows, int64_t width, int64_t hidden)
-        : gate_up(choose(n, hidden, rows, width, 2, 0)), down(choose(n, width, rows, hidden, 1, n * rows * width))
+        : gate_up(choose(kUsual, n, hidden, rows, width, 2, 0)), down(choose(kOfDown, n, width, rows, hidden, 1, n * rows * width))
     {
         if (thin_forward_rows(n, rows, hidden)) down.parts = 1;
     }
@@ -94,7 +99,7 @@ struct BackwardPlan {
     TileKind gradients = kLarge;
     int input_parts = 1, param_parts = 1;
     size_t hidden_floats, input_floats, gate_floats, down_floats;
-    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid) : hidden(choose(n, hid, rows, width, 1, 0))
+    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid) : hidden(choose(kUsual, n, hid, rows, width, 1, 0))
     {
         double least = 1e30;
         for (int kind = 0; kind < kTileKinds; ++kind) {
@@ -102,8 +107,8 @@ struct BackwardPlan {
             const int64_t params = 3 * n * tiles(width, k.i) * tiles(hid, k.j), input = rows > kThinRows ? n * tiles(width, k.i) * tiles(rows, k.j) : 0;
             for (int pp = 1; pp <= 32 && (pp == 1 || (rows / pp >= 4 * kTileK && params * pp <= 1024)); pp *= 2)
                 for (int ip = 1; ip <= 32 && (ip == 1 || (2 * hid / ip >= 4 * kTileK && input * ip <= 1024 && input > 0)); ip *= 2) {
-                    const double of_params = steps_of(rows, pp), of_input = input ? steps_of(2 * hid, ip) : 0.0;
-                    const double c = launch_cost((TileKind)kind, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
+                    const double of_params = steps_of(kUsual, rows, pp), of_input = input ? steps_of(kUsual, 2 * hid, ip) : 0.0;
+                    const double c = launch_cost(kUsual, (TileKind)kind, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
                                                  of_params > of_input ? of_params : of_input) +
                                      reduce_cost(pp, 3 * n * width * hid) + (pp > 1 ? 0.6 : 0.0) + reduce_cost(ip, n * rows * width);
                     if (c < least) {
