@@ -11,7 +11,7 @@
 // add up the products of parts that are not below 2^-24 of the whole: six for two fp32 operands, three for fp32 and bf16.  That is
 // the accuracy of fp32 products at 2.5 PFLOP/s / 6 (or / 3), where the fp32 matrix instructions end at 157 TFLOP/s; and
 // since each part is read from LDS once for several products, LDS keeps up with half the traffic a
-// plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 4.95 PFLOP
+// plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 4.95 TFLOP
 // of theirs and take 4.81 ms, 1,030 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,113 on the same card).
 #pragma once
 #include "layer_common.hpp"

@@ -159,14 +159,20 @@ class _Dropout(torch.autograd.Function):
 
 def layer_norm(x, weight, bias=None, eps: float = 1e-5):
     """Layer norm as an autograd function of x, weight and bias."""
+    if not torch.is_grad_enabled():
+        return layer_norm_forward(x, weight, bias, eps)[0]
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
 def gated_ffn(x, gate, up, down, activation: str = "silu"):
     """The gated feed-forward block as an autograd function of x and its three parameters."""
+    if not torch.is_grad_enabled():  # (within the function this could not be told, and g, u and h would be kept)
+        return gated_ffn_forward(x, gate, up, down, activation)[0]
     return _GatedFfn.apply(x, gate, up, down, activation)
 
 
 def dropout(x, p: float, seed: int, call: int = 0, residual=None, counter=None):
     """Dropout, and the addition to a residual stream, as an autograd function of x and residual."""
+    if not torch.is_grad_enabled():
+        return dropout_forward(x, p, seed, call, residual, counter)
     return _Dropout.apply(x, p, seed, call, residual, counter)
