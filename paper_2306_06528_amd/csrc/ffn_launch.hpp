@@ -23,16 +23,21 @@ constexpr KindOf kKinds[kTileKinds] = {{LargeTile::kI, LargeTile::kJ, 512}, {Sma
 
 // What a launch takes, in steps (32 columns) of a large tile on a full CU (4.4 us fp32, 3 us bf16): workgroups of `longest` steps and `work` steps
 // in all.  Fewer than run at a time take as long as the longest, and that is `half` times as long where a CU has only half of them;
-// of more, the last ones end 0.4 of their length late.  Of the kinds and parts measured at 15 shapes (1 to 57 particles of 64 to 16,000 rows, 32 to
-// 1,322 wide) what it finds cheapest takes up to 20 % more than the fastest where a pass takes less than 100 us, 5 % beyond.
+// of more, the last ones end 0.4 of their length late.
 struct Rates {
     double step[kTileKinds], half, start; // a tile's step; see above; steps until a workgroup's first rows are there, and for its results
+    double launch, bytes;                 // what adding up parts' sums costs: a launch, and the bytes that it moves in a step's time
 };
-constexpr Rates kUsual = {{1.0, 0.6, 0.35}, 0.6, 4.0};
+// g and u, dh: at 15 shapes (1 to 40 particles of 64 to 16,000 rows, 64 to 1,024 wide) this finds the fastest or one within 5 % of it.
+constexpr Rates kUsual = {{1.0, 0.6, 0.35}, 0.6, 4.0, 0.0, 1.0}; // (never in parts)
 // y = h down^T: the one product whose operands both lie along the columns, h of three parts.  Small tiles cost more there (at 15 shapes, 1 to 40 particles
 // of 64 to 16,000 rows, 64 to 1,024 wide, this finds the fastest or one within 5 % of it; with the usual ones forward took 8 x 1,576 x 384 x
 // 1,024 bf16 146 us for 134, 2 x 3,000 x 768 x 2,048 fp32 345 for 299).
-constexpr Rates kOfDown = {{1.0, 0.6, 0.5}, 0.8, 3.0};
+constexpr Rates kOfDown = {{1.0, 0.6, 0.5}, 0.8, 3.0, 0.6, 16e6};
+// The gradients, tiles of dx and of the parameters in one launch: workgroups of other lengths side by side, results of four bytes each.  Of all kinds
+// and parts at 27 shapes (1 to 64 particles of 50 to 16,000 rows, 48 to 1,024 wide) this finds the fastest or one within 5 % of it at 23 and
+// never takes more than 20 % more; with the usual rates and kOfDown's reductions these would be 17 and 22 %.
+constexpr Rates kOfGradients = {{1.0, 0.62, 0.4}, 0.9, 10.0, 0.3, 6e6};
 inline double launch_cost(const Rates &r, TileKind kind, int64_t workgroups, double work, double longest)
 {
     const int at_a_time = kKinds[kind].at_a_time;
@@ -40,8 +45,8 @@ inline double launch_cost(const Rates &r, TileKind kind, int64_t workgroups, dou
     return (work / at_a_time + 0.4 * longest) * r.step[kind];
 }
 inline double steps_of(const Rates &r, int64_t columns, int parts) { return (double)(((columns + parts - 1) / parts + kTileK - 1) / kTileK) + r.start; }
-// Parts' sums are written and read once more: the launch that adds them up, and its bytes at 4 TB/s.
-inline double reduce_cost(int parts, int64_t floats) { return parts > 1 ? 0.6 + (double)floats * parts * 8.0 / 16e6 : 0.0; }
+// Parts' sums are written and read once more.
+inline double reduce_cost(const Rates &r, int parts, int64_t floats) { return parts > 1 ? r.launch + (double)floats * parts * 8.0 / r.bytes : 0.0; }
 
 struct Choice {
     TileKind kind;
@@ -57,7 +62,7 @@ inline Choice choose(const Rates &r, int n, int64_t i, int64_t j, int64_t column
     for (int kind = 0; kind < kTileKinds; ++kind) {
         const int64_t t = n * tiles(i, kKinds[kind].i / per_i) * tiles(j, kKinds[kind].j);
         for (int parts = 1; parts <= (sums ? 32 : 1) && (parts == 1 || (columns / parts >= 4 * kTileK && t * parts <= 1024)); parts *= 2) {
-            const double steps = steps_of(r, columns, parts), c = launch_cost(r, (TileKind)kind, t * parts, (double)(t * parts) * steps, steps) + reduce_cost(parts, sums);
+            const double steps = steps_of(r, columns, parts), c = launch_cost(r, (TileKind)kind, t * parts, (double)(t * parts) * steps, steps) + reduce_cost(r, parts, sums);
             if (c < least) {
                 least = c;
                 best = {(TileKind)kind, parts};
@@ -107,10 +112,11 @@ struct BackwardPlan {
             const int64_t params = 3 * n * tiles(width, k.i) * tiles(hid, k.j), input = rows > kThinRows ? n * tiles(width, k.i) * tiles(rows, k.j) : 0;
             for (int pp = 1; pp <= 32 && (pp == 1 || (rows / pp >= 4 * kTileK && params * pp <= 1024)); pp *= 2)
                 for (int ip = 1; ip <= 32 && (ip == 1 || (2 * hid / ip >= 4 * kTileK && input * ip <= 1024 && input > 0)); ip *= 2) {
-                    const double of_params = steps_of(kUsual, rows, pp), of_input = input ? steps_of(kUsual, 2 * hid, ip) : 0.0;
-                    const double c = launch_cost(kUsual, (TileKind)kind, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
-                                                 of_params > of_input ? of_params : of_input) +
-                                     reduce_cost(pp, 3 * n * width * hid) + (pp > 1 ? 0.6 : 0.0) + reduce_cost(ip, n * rows * width);
+                    const double of_params = steps_of(kOfGradients, rows, pp), of_input = input ? steps_of(kOfGradients, 2 * hid, ip) : 0.0;
+                    const double c = launch_cost(kOfGradients, (TileKind)kind, params * pp + input * ip,
+                                                 (double)(params * pp) * of_params + (double)(input * ip) * of_input, of_params > of_input ? of_params : of_input) +
+                                     reduce_cost(kOfGradients, pp, 3 * n * width * hid) + (pp > 1 ? kOfGradients.launch : 0.0) +
+                                     reduce_cost(kOfGradients, ip, n * rows * width);
                     if (c < least) {
                         least = c;
                         gradients = (TileKind)kind;

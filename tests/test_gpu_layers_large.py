@@ -13,6 +13,9 @@ pytestmark = pytest.mark.gpu
 TILED = [(40, 1_028, 133, 83), (24, 77, 665, 1_602), (5, 3_501, 66, 43), (24, 70, 208, 513), (40, 741, 32, 68), (13, 3_361, 34, 35), (24, 453, 203, 165),
          (5, 70, 502, 595), (8, 1_910, 130, 103), (1, 3_413, 403, 1_039), (64, 267, 67, 135), (40, 73, 107, 309), (3, 4_629, 72, 44), (2, 2_865, 197, 401),
          (8, 3_862, 44, 131), (8, 5_985, 32, 66)]
+# The same for the gradients with later rates: large tiles whole and with the parameters' rows in parts, small ones with these in parts, and with both,
+# the smallest with both.
+TILED += [(64, 227, 199, 122), (8, 3_543, 133, 105), (5, 5_030, 74, 46), (3, 1_769, 198, 474), (1, 284, 46, 135)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
