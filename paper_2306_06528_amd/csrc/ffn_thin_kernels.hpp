@@ -16,7 +16,7 @@ constexpr int kThinStride = kThinWaves * kTileK; // columns between two steps of
 
 // A wave's operand of 16 rows and 32 columns, K contiguous in memory.  The matrix instructions want lane l to have row l % 16, columns
 // 8 (l / 16) .. + 7, but the vector memory unit joins what 16 lanes in a row read: loaded like that, every load costs 64 accesses, which
-// bound these kernels (8 x 32 rows, 1,024 x 2,730 bf16, forward: 74 us, like this 63; 8 x 5 rows 56 and 53).  So eight lanes (four of 16-bit values) read 16 bytes each side by
+// bound these kernels (8 x 32 rows, 1,024 x 2,730 bf16, forward: 74 us, like this 64; 1 x 64 rows fp32 39 and 30).  So eight lanes (four of 16-bit values) read 16 bytes each side by
 // side, and the values change lanes in the wave's own part of LDS, as they are.
 template <class T> struct ThinRows {
     static constexpr int W = 16 / sizeof(T), kPieces = kTileK / W, kAtATime = 64 / kPieces, N = 16 / kAtATime;
@@ -44,13 +44,13 @@ template <class T> struct ThinRows {
     }
     __device__ __forceinline__ void load_last(const From &from, int64_t k, int64_t K) // columns from K on are 0 and not read
     {
-        const int64_t end = K - column();
+        const int left = (int)(K - k) - column(); // (may be less than 1)
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int e = 0; e < W; ++e) {
-                const T x = from.row[n][k + e < end ? k + e : end - 1];
-                v[n][e] = k + e < end ? x : (T)0.f;
+                const T x = from.row[n][k + (e < left ? e : left - 1)];
+                v[n][e] = e < left ? x : (T)0.f;
             }
     }
     __device__ __forceinline__ void stage(f32x4 *slot) const
@@ -70,6 +70,11 @@ template <class T> struct ThinRows {
     }
 };
 constexpr int kSlot = 16 * kTileK / 4; // one operand, in 16 bytes
+
+// Forward with up to 16 rows three workgroups fit a CU, which the compiler has to be told, if a wave has one step of gate and up on its way, or two
+// of down: 16 x 1 rows, 256 x 683 fp32 9.8 us; two workgroups and twice the steps 10.9 (8 x 5 rows, 1,024 x 2,731 bf16 55 both, 1 x 8 rows, 4,096 x
+// 11,008 110 and 106).
+#define SVGD_THIN_KERNEL __global__ __launch_bounds__(kThinBlock) __attribute__((amdgpu_waves_per_eu(JB == 1 ? 6 : 2)))
 
 // A wave's part of LDS: `slots` operands, and later its sums of N blocks of 16 x 16.
 template <int N, int SLOTS> constexpr int kThinPart = 64 * N > SLOTS * kSlot ? 64 * N : SLOTS * kSlot;
@@ -226,10 +231,10 @@ template <int U, class Load, class Last, class Use> __device__ __forceinline__ v
 }
 
 template <class T, int ACT, bool SAVE, int JB>
-__global__ __launch_bounds__(kThinBlock) void thin_gate_up_kernel(FfnShape s, ThinGrid grid, Rows<const T> x, Params gate, Params up, float *h,
+SVGD_THIN_KERNEL void thin_gate_up_kernel(FfnShape s, ThinGrid grid, Rows<const T> x, Params gate, Params up, float *h,
                                                                   float *g_out, float *u_out)
 {
-    constexpr int P = kParts<T>, U = JB > 2 ? 1 : 2, kPart = kThinPart<2 * JB, 3>;
+    constexpr int P = kParts<T>, U = 1, kPart = kThinPart<2 * JB, 3>;
     __shared__ f32x4 parts[kThinWaves * kPart];
     f32x4 *const slots = parts + wave_of_block() * kPart;
     const int particle = grid.particle();
@@ -284,9 +289,9 @@ __global__ __launch_bounds__(kThinBlock) void thin_gate_up_kernel(FfnShape s, Th
     });
 }
 
-template <class T, int JB> __global__ __launch_bounds__(kThinBlock) void thin_down_kernel(FfnShape s, ThinGrid grid, const float *h, Params down, Rows<T> y)
+template <class T, int JB> SVGD_THIN_KERNEL void thin_down_kernel(FfnShape s, ThinGrid grid, const float *h, Params down, Rows<T> y)
 {
-    constexpr int U = 4 / JB, kPart = kThinPart<JB, 2>;
+    constexpr int U = JB == 1 ? 2 : 4 / JB, kPart = kThinPart<JB, 2>;
     __shared__ f32x4 parts[kThinWaves * kPart];
     f32x4 *const slots = parts + wave_of_block() * kPart;
     const int particle = grid.particle();
