@@ -77,13 +77,14 @@ template <class F> int with_tile(TileKind kind, F f)
     return kind == kLarge ? f(LargeTile{}) : kind == kSmall ? f(SmallTile{}) : f(TinyTile{});
 }
 
-// Up to so many rows per particle the weights go straight from memory to the matrix cores (ffn_thin_kernels.hpp): 8 x 17 rows, 384 x 1,024 fp32,
-// forward 17 us, in tiles 114; backward 43 and 179.  Forward up to 64 rows where the tiles of g and u are few (8 x 64 rows of these 29 and 46,
-// 1 x 64 rows, 1,024 x 2,730 fp32 41 and 87, but 40 x 64 rows, 256 x 700 bf16, 240 tiles, 49 and 42).
+// Up to so many rows per particle every weight is read once, by a wave of its own (ffn_thin_kernels.hpp): 8 x 17 rows, 384 x 1,024 fp32, forward 15 us,
+// in tiles 27, 8 x 32 rows 16 and 28; backward of 8 x 17 rows 41, in tiles (of the time) 179.  Forward up to 64 rows where the tiles of g and u are few: 1 x 64
+// rows, 1,024 x 2,730 fp32, 22 tiles, 29 and 51, 8 x 64 rows, 384 x 1,024, 64 tiles, 23 and 29, but 16 x 64 rows, 512 x 1,400 bf16, 176 tiles, 50 and 45,
+// 40 x 64 rows, 256 x 700, 240 tiles, 49 and 36.
 constexpr int64_t kThinRows = 32;
 inline bool thin_forward_rows(int n, int64_t rows, int64_t hidden)
 {
-    return rows <= kThinRows || (rows <= 64 && n * tiles(hidden, LargeTile::kI / 2) < 200);
+    return rows <= kThinRows || (rows <= 64 && n * tiles(hidden, LargeTile::kI / 2) < 128);
 }
 
 inline int64_t width_ld(int64_t width) { return (width + 3) / 4 * 4; }
