@@ -2,17 +2,17 @@
 //     g = x Wg^T, u = x Wu^T, h = act(g) u                       gate_up_kernel   (the activation in its epilogue)
 //     y = h Wd^T                                                 down_kernel
 //     dh = dy Wd, dg = dh u act'(g), du = dh act(g)              hidden_grad_kernel (these in its epilogue)
-//     dx = dg Wg + du Wu                                         input_grad_kernel
-//     dWg = dg^T x, dWu = du^T x, dWd = dy^T h                   weight_grad_kernel
+//     dx = dg Wg + du Wu                                         gradients_kernel, input_grad_tile
+//     dWg = dg^T x, dWu = du^T x, dWd = dy^T h                   gradients_kernel, weight_grad_tile
 //
 // All of them are one tile product, C[j][i] = sum_k A[i][k] B[j][k], 256 x 128 values of C (i x j) per workgroup of four waves of 64 x 128, or
 // less where there are few tiles (ffn_launch.hpp).  Operands are fp32 or 16 bits wide in memory; on their way into LDS they become bf16 parts whose sum is the value
 // EXACTLY (split3: three parts of an fp32 value, two of an fp16 one, one of a bf16 one), and the matrix cores
-// add up the products of parts that are not below 2^-24 of the whole: six for two fp32 operands, three for fp32 and bf16.  That is
-// the accuracy of fp32 products at 2.5 PFLOP/s / 6 (or / 3), where the fp32 matrix instructions end at 157 TFLOP/s; and
+// add up the products of parts that are not below 2^-24 of the whole: six for two fp32 operands, five for fp32 and fp16, three for fp32 and bf16.  That is
+// the accuracy of fp32 products at 2.5 PFLOP/s / 6 (5, 3), where the fp32 matrix instructions end at 157 TFLOP/s; and
 // since each part is read from LDS once for several products, LDS keeps up with half the traffic a
-// plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 4.95 TFLOP
-// of theirs and take 4.81 ms, 1,030 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,113 on the same card).
+// plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 6.60 TFLOP
+// of theirs and take 5.51 ms, 1,198 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,156 on the same card).
 #pragma once
 #include "layer_common.hpp"
 
@@ -606,13 +606,14 @@ SVGD_TILE_KERNEL void gate_up_kernel(FfnShape s, TileGrid grid, Rows<const T> x,
     }
 }
 
-// Two parts of each operand are enough where the result is rounded to 16 bits: what is left out is below 2^-16 of a product.
-template <class T> constexpr int kHiddenParts = sizeof(T) == 4 ? 3 : 2;
+// h, dg and du and the parameters that they meet are fp32 whatever the activations' type, and so are these products: two parts of each, which leave out
+// 2^-16 of a product, would show in 16-bit results of sums that cancel, and the same row would come out differently beside 32 and beside 65 others.
+constexpr int kHiddenParts = 3;
 
 // partial: with more than one part, their sums [part][particle][row][width_ld]
 template <class TL, class T> SVGD_TILE_KERNEL void down_kernel(FfnShape s, TileGrid grid, const float *h, Params down, Rows<T> y, float *partial)
 {
-    constexpr int P = kHiddenParts<T>;
+    constexpr int P = kHiddenParts;
     __shared__ bf16x8 lds[2 * P * TL::kPlane];
     __shared__ float scratches[TL::kWaves][kScratch];
     float *const scratch = scratches[wave_of_block()];
@@ -670,7 +671,7 @@ template <class TL, class T>
 __device__ __forceinline__ void input_grad_tile(const FfnShape &s, const TileGrid &grid, int block, const float *dg, const float *du, const Params &gate,
                                                 const Params &up, const Rows<T> &dx, float *partial, bf16x8 *lds, float *scratch)
 {
-    constexpr int P = kHiddenParts<T>;
+    constexpr int P = kHiddenParts;
     int particle, part, ti, tj;
     if (!grid.at(block, particle, part, ti, tj)) return;
     const int64_t i0 = (int64_t)ti * TL::kI, j0 = (int64_t)tj * TL::kJ, iw = i0 + wave_of_block() * 64;
@@ -748,7 +749,7 @@ template <class TL, class T>
 SVGD_TILE_KERNEL void gradients_kernel(FfnShape s, TileGrid input, const float *dg, const float *du, Params gate, Params up, Rows<T> dx, float *dx_partial,
                                        WeightGrad<T, float> gates, WeightGrad<T, float> down, bool accumulate)
 {
-    constexpr int P = kHiddenParts<T> > kParts<float> ? kHiddenParts<T> : kParts<float>;
+    constexpr int P = kHiddenParts;
     __shared__ bf16x8 lds[2 * P * TL::kPlane];
     __shared__ float scratches[TL::kWaves][kScratch];
     float *const scratch = scratches[wave_of_block()];

@@ -1,0 +1,43 @@
+"""What the layers' header says about precision, at inputs that show it."""
+import pytest
+import torch
+
+import layer_reference as ref
+from test_gpu_layers import IDS, TYPES, gen, layers  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows", [5, 32, 70, 1_000])
+def test_ffn_products_are_those_of_fp32_whatever_the_type(layers, rows, dtype):  # noqa: F811
+    """y and dx of two terms each that cancel but for 2^-12 of them.  x and dy are unit rows, so g, u and dh are the parameters' values
+    themselves: h, dg and du are off by at most ten roundings of fp32, and two products in fp32, each as six of parts that are added up one by one, by
+    sixteen more; then the result is rounded to its type.  (Operands of 16 bits would be off by 2^-17 each.)"""
+    g = gen(31)
+    n, width, hidden = 3, 200, 70
+    gate, up, down = torch.zeros(n, hidden, width), torch.zeros(n, hidden, width), torch.zeros(n, width, hidden)
+    gate[:, :, 0] = torch.rand(n, hidden, generator=g) + 0.5
+    up[:, :, 0] = torch.rand(n, hidden, generator=g) + 0.5
+    gv, uv = gate[:, :2, 0].double(), up[:, :2, 0].double()
+    a, slope, _, _ = ref.activation(gv, "silu")
+    h = a * uv
+    near = 1.0 + 2.0 ** -12
+    down[:, :, 0] = torch.rand(n, width, generator=g) + 0.5
+    down[:, :, 1] = (-near * (h[:, :1] / h[:, 1:]) * down[:, :, 0].double()).float()
+    dg, du = (down[:, 0, :2].double() * t for t in (uv * slope, a))
+    for d, w, cols in ((dg, gate, slice(1, 100)), (du, up, slice(100, 200))):  # (where x is 0)
+        w[:, 0, cols] = torch.rand(n, cols.stop - cols.start, generator=g) + 0.5
+        w[:, 1, cols] = (-near * (d[:, :1] / d[:, 1:]) * w[:, 0, cols].double()).float()
+    x = torch.zeros(n, rows, width, dtype=dtype)
+    x[:, :, 0] = 1.0
+    want = {"y": down[:, :, :2].double() @ h.unsqueeze(2), "dx": gate[:, :2].double().transpose(1, 2) @ dg.unsqueeze(2) + up[:, :2].double().transpose(1, 2) @ du.unsqueeze(2)}
+    size = {"y": down[:, :, :2].double().abs() @ h.abs().unsqueeze(2),
+            "dx": gate[:, :2].double().abs().transpose(1, 2) @ dg.abs().unsqueeze(2) + up[:, :2].double().abs().transpose(1, 2) @ du.abs().unsqueeze(2)}
+    x, gate, up, down = (t.cuda() for t in (x, gate, up, down))
+    y, saved = layers.gated_ffn_forward(x, gate, up, down, save=True)
+    got = {"y": y, "dx": layers.gated_ffn_backward(x, x, gate, up, down, saved)}
+    for name in got:
+        v = want[name].transpose(1, 2)
+        assert v[:, :, 1:].abs().max() < 1e-3
+        ref.check(got[name], (v.expand(n, rows, width), (ref.rounding(dtype) * v.abs() + 26 * ref.U * size[name].transpose(1, 2)).expand(n, rows, width)), name)
