@@ -126,8 +126,8 @@ class _LayerNorm(torch.autograd.Function):
 
 class _GatedFfn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, gate, up, down, activation):
-        y, saved = gated_ffn_forward(x, gate, up, down, activation, save=any(ctx.needs_input_grad))
+    def forward(ctx, x, gate, up, down, activation, grad_enabled):
+        y, saved = gated_ffn_forward(x, gate, up, down, activation, save=grad_enabled and any(ctx.needs_input_grad))
         ctx.save_for_backward(x, gate, up, down, saved)
         ctx.activation = activation
         return y
@@ -136,43 +136,40 @@ class _GatedFfn(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x, gate, up, down, saved = ctx.saved_tensors
-        want_dx, *want, _ = ctx.needs_input_grad
+        want_dx, *want, _, _ = ctx.needs_input_grad
         grads = [_new_grad(w, p) for w, p in zip(want, (gate, up, down))]
         dx = gated_ffn_backward(_with_rows(dy), x, gate, up, down, saved, *grads, ctx.activation, want_dx=want_dx)
-        return dx, *grads, None
+        return dx, *grads, None, None
 
 
 class _Dropout(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, p, seed, call, residual, counter):
+    def forward(ctx, x, p, seed, call, residual, counter, grad_enabled):
         ctx.draw = (p, seed, call)
         # (the caller moves the counter on between the passes: what this one has drawn with is kept)
-        ctx.counter = counter.clone() if counter is not None and ctx.needs_input_grad[0] else None
+        ctx.counter = counter.clone() if counter is not None and grad_enabled and ctx.needs_input_grad[0] else None
         return dropout_forward(x, p, seed, call, residual, counter)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         dx = dropout_backward(_with_rows(dy), *ctx.draw, ctx.counter) if ctx.needs_input_grad[0] else None
-        return dx, None, None, None, dy if ctx.needs_input_grad[4] else None, None
+        return dx, None, None, None, dy if ctx.needs_input_grad[4] else None, None, None
 
 
+# Without gradients these go through autograd all the same, which knows the tensors that carry a tangent in forward mode (torch.no_grad leaves
+# that on) and refuses them: the layers have no rule for tangents.  Within the functions gradients are always off: whether they
+# are on outside, and g, u and h or the counter are to be kept, is handed over.
 def layer_norm(x, weight, bias=None, eps: float = 1e-5):
     """Layer norm as an autograd function of x, weight and bias."""
-    if not torch.is_grad_enabled():
-        return layer_norm_forward(x, weight, bias, eps)[0]
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
 def gated_ffn(x, gate, up, down, activation: str = "silu"):
     """The gated feed-forward block as an autograd function of x and its three parameters."""
-    if not torch.is_grad_enabled():  # (within the function this could not be told, and g, u and h would be kept)
-        return gated_ffn_forward(x, gate, up, down, activation)[0]
-    return _GatedFfn.apply(x, gate, up, down, activation)
+    return _GatedFfn.apply(x, gate, up, down, activation, torch.is_grad_enabled())
 
 
 def dropout(x, p: float, seed: int, call: int = 0, residual=None, counter=None):
     """Dropout, and the addition to a residual stream, as an autograd function of x and residual."""
-    if not torch.is_grad_enabled():
-        return dropout_forward(x, p, seed, call, residual, counter)
-    return _Dropout.apply(x, p, seed, call, residual, counter)
+    return _Dropout.apply(x, p, seed, call, residual, counter, torch.is_grad_enabled())
