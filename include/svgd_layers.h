@@ -28,8 +28,10 @@
  *     the same inputs give the same bits.
  *   - Return value: SVGD_OK or a negative svgd_status: INVALID_ARG for null pointers, sizes below 1 (rows: 0),
  *     misaligned pointers, an unknown type or activation, outputs that overlap each other or an input, a
- *     non-finite eps or p outside [0, 1]; TOO_LARGE beyond the limits below; DEVICE if a launch failed.  Nothing is
- *     launched then.  No entry point aborts or throws.  Non-finite DATA is not checked and propagates as NaN or Inf.
+ *     non-finite eps or p outside [0, 1]; TOO_LARGE beyond the limits below.  Nothing is launched then.  DEVICE if a launch failed: those
+ *     that the call made before it stay on the stream.  Tensors' extents count, from the first to the last of their elements, except
+ *     where the parts of parameters and of their gradients lie side by side in the same rows: those are looked at one by one.
+ *     No entry point aborts or throws.  Non-finite DATA is not checked and propagates as NaN or Inf.
  */
 #ifndef SVGD_LAYERS_H
 #define SVGD_LAYERS_H
@@ -55,7 +57,8 @@ typedef struct svgd_rows {
 #define SVGD_LAYER_MAX_ROWS ((int64_t)1 << 30)
 #define SVGD_LAYER_MAX_NORM 16384            /* width that svgd_layer_norm_* takes */
 #define SVGD_LAYER_MAX_WIDTH ((int64_t)1 << 20) /* width and hidden width of svgd_gated_ffn_* */
-/* (svgd_dropout takes rows of up to SVGD_MAX_D values) */
+/* (svgd_dropout takes rows of up to SVGD_MAX_D values; svgd_gated_ffn_* work in tiles, and those of a launch are below 2^24: of g, u and
+ * their gradients, n ceil(rows / 128) ceil(hidden / 128) of them, of y and dx half as many by the width, of the parameters' gradients 3 n ceil(width / 256) ceil(hidden / 128)) */
 
 /*
  * Layer norm over the values of each row:

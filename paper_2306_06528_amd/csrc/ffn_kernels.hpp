@@ -14,11 +14,10 @@
 // plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 6.60 TFLOP
 // of theirs and take 5.51 ms, 1,198 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,156 on the same card).
 #pragma once
+#include "ffn_rules.hpp"
 #include "layer_common.hpp"
 
 namespace svgd {
-
-constexpr int kTileK = 32; // columns of both operands per step
 
 // A workgroup of W waves computes 64 W values of i and 16 NJ of j, each wave 64 of i and all of j.
 template <int W, int NJ> struct Tile {
@@ -460,7 +459,7 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
 // tiles that follow one another, so that the operands they share meet in its L2; and they follow one another in blocks of kBand tiles of j.
 // Where there are few tiles the columns are split into `splits` parts of `per` columns: the parts' sums are added up afterwards,
 // in order (reduce_rows_kernel, reduce_params_kernel).
-constexpr int kDies = 8, kBand = 8;
+constexpr int kBand = 8;
 struct TileGrid {
     int ti, tj, splits, per_die, total;
     int64_t per, columns;
@@ -468,9 +467,8 @@ struct TileGrid {
     __host__ TileGrid(int n, int64_t i, int64_t j, int64_t cols, int parts) : ti((int)i), tj((int)j), splits(parts), columns(cols)
     {
         per = ((cols + parts - 1) / parts + kTileK - 1) / kTileK * kTileK;
-        const int64_t t = n * i * j * parts;
-        total = t > (1 << 24) - kDies ? -1 : (int)t; // (more than memory holds, and than a launch takes)
-        per_die = total < 0 ? 0 : (total + kDies - 1) / kDies;
+        total = (int)(n * i * j * parts); // (the plan has seen to it that a launch takes them)
+        per_die = (total + kDies - 1) / kDies;
     }
     __host__ int blocks() const { return per_die * kDies; }
     // false: nothing to do

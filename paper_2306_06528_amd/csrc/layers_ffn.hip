@@ -58,7 +58,8 @@ int svgd_gated_ffn_forward(int dtype, int activation, int n, int64_t rows, int64
     if (const int rc = check(dtype, activation, n, rows, width, hidden, x, c.gate, c.up, c.down)) return rc;
     if (rows == 0) return SVGD_OK;
     const size_t need = svgd_gated_ffn_buffer(n, rows, width, hidden, save);
-    const size_t scratch_need = svgd_gated_ffn_forward_scratch(n, rows, width, hidden);
+    const ForwardPlan plan(n, rows, width, hidden);
+    const size_t scratch_need = plan.scratch(n, rows, width);
     if (!valid_output(y, dtype, n, rows, width) || !buffer || !aligned_to(buffer, 16) || buffer_bytes < need ||
         (scratch_need > 0 && (!scratch || !aligned_to(scratch, 16) || scratch_bytes < scratch_need)))
         return SVGD_ERR_INVALID_ARG;
@@ -69,7 +70,8 @@ int svgd_gated_ffn_forward(int dtype, int activation, int n, int64_t rows, int64
     for (const Extent &w : written)
         for (const Extent &r : read)
             if (w.meets(r)) return SVGD_ERR_INVALID_ARG;
-    return for_type(dtype, [&](auto t) { return ffn_forward<decltype(t)>(c, x, y, (float *)buffer, save != 0, (float *)scratch); });
+    if (!plan.fits()) return SVGD_ERR_TOO_LARGE;
+    return for_type(dtype, [&](auto t) { return ffn_forward<decltype(t)>(c, plan, x, y, (float *)buffer, save != 0, (float *)scratch); });
 }
 
 int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t hidden, svgd_rows dy, svgd_rows x, const float *gate,
@@ -90,8 +92,9 @@ int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int6
         for (const Params &o : grads)
             if (&o > &g && o.p && params_meet(g, o, n)) return SVGD_ERR_INVALID_ARG;
     }
+    const BackwardPlan plan(n, rows, width, hidden);
     if (rows > 0) {
-        const size_t saved_need = svgd_gated_ffn_buffer(n, rows, width, hidden, 1), need = svgd_gated_ffn_scratch(n, rows, width, hidden);
+        const size_t saved_need = svgd_gated_ffn_buffer(n, rows, width, hidden, 1), need = plan.scratch();
         if (!valid_input(dy, dtype, rows) || !saved || !aligned_to(saved, 16) || saved_bytes < saved_need || !scratch || !aligned_to(scratch, 16) ||
             scratch_bytes < need || (dx.data && !valid_output(dx, dtype, n, rows, width)))
             return SVGD_ERR_INVALID_ARG;
@@ -109,8 +112,9 @@ int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int6
             if (work.meets(e) || dxe.meets(e) || acts[0].meets(e) || acts[1].meets(e) || acts[2].meets(e)) return SVGD_ERR_INVALID_ARG;
         }
     }
+    if (!plan.fits()) return SVGD_ERR_TOO_LARGE;
     return for_type(dtype, [&](auto t) {
-        return ffn_backward<decltype(t)>(c, dy, x, (const float *)saved, dx, grads[0], grads[1], grads[2], accumulate != 0, (float *)scratch);
+        return ffn_backward<decltype(t)>(c, plan, dy, x, (const float *)saved, dx, grads[0], grads[1], grads[2], accumulate != 0, (float *)scratch);
     });
 }
 
