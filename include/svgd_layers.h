@@ -64,7 +64,7 @@ typedef struct svgd_rows {
  * Layer norm over the values of each row:
  *     mean = avg_c x_c,  rstd = 1 / sqrt(avg_c (x_c - mean)^2 + eps),  y_c = (x_c - mean) rstd weight_c + bias_c
  * weight and bias: `width` values per particle; bias may be NULL.  mean and rstd (DEVICE, n * rows floats each,
- * particle-major) are what the backward pass needs; both may be NULL.
+ * particle-major) are what the backward pass needs, which takes them as they are, rounded to fp32; both may be NULL.
  */
 int svgd_layer_norm_forward(int dtype, int n, int64_t rows, int64_t width, svgd_rows x, const float *weight,
                             int64_t weight_stride, const float *bias, int64_t bias_stride, double eps, svgd_rows y,

@@ -41,3 +41,26 @@ def test_ffn_products_are_those_of_fp32_whatever_the_type(layers, rows, dtype): 
         v = want[name].transpose(1, 2)
         assert v[:, :, 1:].abs().max() < 1e-3
         ref.check(got[name], (v.expand(n, rows, width), (ref.rounding(dtype) * v.abs() + 26 * ref.U * size[name].transpose(1, 2)).expand(n, rows, width)), name)
+
+
+@pytest.mark.parametrize("width", [7, 48, 200, 384, 1_001, 2_000, 5_003, 16_001])
+def test_norm_of_rows_very_far_from_zero(layers, width):  # noqa: F811
+    """Rows at 1e5: one of equal values, whose result is the bias, and one with a spread of 0.1, twelve steps of fp32.  The first mean is off by at most E + 16 roundings
+    of 1e5 (E <= 16 values to a thread, 10 halvings), at most 0.2; what is taken off a second time is the mean of such distances, exact differences, to as many roundings of it, 4e-7, and rstd
+    is at most 317 for the first row."""
+    g = gen(32, width)
+    x = torch.full((1, 2, width), 1e5 + 0.3)
+    x[0, 1] += torch.randn(width, generator=g) * 0.1
+    w, b = torch.rand(1, width, generator=g) + 0.5, torch.rand(1, width, generator=g)
+    y, mean, rstd = (t.double().cpu() for t in layers.layer_norm_forward(x.cuda(), w.cuda(), b.cuda(), 1e-5))
+    assert ((y[0, 0] - b[0].double()).abs() <= 4e-7 * 317 * w[0].double() + 2 * ref.U * b[0].double()).all()
+    exact = x[0].double()
+    m = exact.mean(-1)
+    assert ((mean[0] - m).abs() <= 2 * ref.U * m).all()
+    c = exact[1] - m[1]
+    r = (c.square().mean() + 1e-5).rsqrt()
+    want = c * r * w[0].double() + b[0].double()
+    # (the second row's variance: some 1e-2, off by the square of 4e-7 and E + 20 roundings of it and of the square that is taken off, at most 0.04)
+    off = 4e-7 * r * w[0].double() + 36 * ref.U * 5 * (want.abs() + b[0].double())
+    assert ((y[0, 1] - want).abs() <= off).all()
+    assert (rstd[0, 1] - r).abs() <= 36 * ref.U * 5 * r
