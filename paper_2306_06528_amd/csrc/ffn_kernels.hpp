@@ -496,7 +496,7 @@ template <int ACT> __device__ __forceinline__ void activate(float g, float &a, f
         a = g * s;
         slope = s * (1.f + g * (1.f - s));
     } else {
-        const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        const float cdf = 0.5f * erfcf(g * -0.70710678118654752f); // (1 + erf has no digits left below -5)
         a = g * cdf;
         slope = cdf + g * 0.39894228040143268f * expf(-0.5f * g * g);
     }

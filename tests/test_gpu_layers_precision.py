@@ -1,4 +1,6 @@
 """What the layers' header says about precision, at inputs that show it."""
+import math
+
 import pytest
 import torch
 
@@ -64,3 +66,19 @@ def test_norm_of_rows_very_far_from_zero(layers, width):  # noqa: F811
     off = 4e-7 * r * w[0].double() + 36 * ref.U * 5 * (want.abs() + b[0].double())
     assert ((y[0, 1] - want).abs() <= off).all()
     assert (rstd[0, 1] - r).abs() <= 36 * ref.U * 5 * r
+
+
+@pytest.mark.parametrize("rows", [3, 80])
+def test_gelu_on_its_flat_side(layers, rows):  # noqa: F811
+    """g from -2 to -9, where 1 + erf(g / sqrt 2) has lost its digits and erfc(-g / sqrt 2) has not: that is off by a few
+    roundings, and by 2 t^2 = g^2 times the two of its argument t."""
+    n, width, hidden = 1, 33, 40
+    gate, up, down = torch.zeros(n, hidden, width), torch.zeros(n, hidden, width), torch.zeros(n, width, hidden)
+    g = -torch.linspace(2.0, 9.0, width)
+    gate[0, 0], up[0, 0], down[0, :, 0] = g, 1.0, 1.0
+    x = torch.eye(width).repeat(1, (rows + width - 1) // width, 1)[:, :rows]
+    d = g.double()[torch.arange(rows) % width]
+    h = d * 0.5 * torch.special.erfc(-d / math.sqrt(2))
+    y, _ = layers.gated_ffn_forward(x.cuda(), gate.cuda(), up.cuda(), down.cuda(), "gelu")
+    want = h[None, :, None].expand(n, rows, width)
+    ref.check(y, (want, (32 + 2 * d * d)[None, :, None] * ref.U * want.abs()), "y")
