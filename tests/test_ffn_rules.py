@@ -92,3 +92,37 @@ def test_every_plan_of_up_to_256_gib_can_be_launched(rules):
         assert all((count + 21) * THREADS[kind] < 1 << 32 for kind, count in launches(p)), shape
         assert p.input_parts == 1 or p.input_parts % 2 == 0
         assert p.down_parts <= max(1, shape[3] // 128) and p.param_parts <= max(1, shape[1] // 128)
+
+
+def test_the_shapes_that_are_tested_reach_every_tile(rules):
+    """Every kind of tile in every product, in one part and in several, with at least three whole steps and a part of one in each."""
+    from ffn_shapes import TILES
+    seen = set()
+    for (n, rows, width, hidden), p in zip(TILES, rules(TILES)):
+        steps = lambda columns, parts: columns // parts >= 96 and columns % 32
+        if not p.thin:
+            if steps(width, 1):
+                seen |= {("gate_up", p.gate_up)}
+            if steps(hidden, p.down_parts):
+                seen |= {("down", p.down, p.down_parts > 1)}
+            if rows <= 64:
+                seen |= {("33 to 64 rows", p.gate_up)}
+        if steps(width, 1):
+            seen |= {("dh", p.dh)}
+        if steps(hidden, max(1, p.input_parts // 2)) and steps(rows, p.param_parts):
+            seen |= {("gradients", p.gradients, p.input_parts > 1, p.param_parts > 1)}
+    want = {(what, kind) for what in ("gate_up", "dh") for kind in range(3)} | {("down", kind, parts) for kind in range(3) for parts in (False, True)}
+    want |= {("gradients", kind, a, b) for kind in range(3) for a in (False, True) for b in (False, True)}
+    want |= {("33 to 64 rows", kind) for kind in (1, 2)}
+    assert want <= seen, want - seen
+
+
+def test_the_shapes_that_are_tested_give_waves_of_few_rows_several_steps(rules):
+    """Eight waves take turns over steps of 32 columns: two steps at once, a third one by itself, and a part of a step behind whole ones."""
+    from ffn_shapes import THIN
+    seen = set()
+    for (n, rows, width, hidden), p in zip(THIN, rules(THIN)):
+        assert p.thin
+        if all(columns // 32 // 8 >= 2 and -(-(columns // 32) // 8) % 2 == 1 and columns % 32 for columns in (width, hidden)):
+            seen |= {(rows > 16) + (rows > 32)}
+    assert seen == {0, 1, 2}

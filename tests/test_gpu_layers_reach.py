@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import layer_reference as ref
+from ffn_shapes import THIN, TILES
 from test_gpu_layers import IDS, TYPES, acts, gen, layers, params, run_ffn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -17,3 +18,58 @@ def test_ffn_more_small_tiles_than_a_launch_takes(layers):  # noqa: F811
     for first in (0, rows // 2 - 7, (1 << 26) * 8 - 20, rows - 40):  # (the third: where x's values pass 2^32)
         part = slice(first, first + 40)
         ref.check(y[:, part], ref.gated_ffn(x[:, part], *p, "silu")["y"], f"y from row {first} on")
+
+
+def check_block(layers, n, rows, width, hidden, dtype, act, layout="gap"):  # noqa: F811
+    g = gen(n, rows, width, hidden, 5)
+    x, dy = acts(g, n, rows, width, dtype, layout), acts(g, n, rows, width, dtype, layout)
+    p, grads, G, D = params(g, n, 3, (hidden, width), (hidden, width), (width, hidden), spread=width ** -0.5)
+    got, want = run_ffn(layers, x, dy, p, grads, act), ref.gated_ffn(x, *p, act, dy)
+    for name in want:
+        ref.check(got[name], want[name], f"{name} of {n}x{rows}x{width}x{hidden}")
+    assert (G[:, :3] == -7.0).all() and (G[:, D - 3:] == -7.0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,rows,width,hidden", THIN)
+def test_ffn_few_rows_of_several_steps(layers, n, rows, width, hidden, dtype):  # noqa: F811
+    check_block(layers, n, rows, width, hidden, dtype, "gelu")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,rows,width,hidden", TILES)
+def test_ffn_tiles_of_several_steps(layers, n, rows, width, hidden, dtype):  # noqa: F811
+    check_block(layers, n, rows, width, hidden, dtype, "silu")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,rows,width,hidden", [(1, 3, 5, 1 << 20), (1, 35, 3, 1 << 20), (1, 3, 1 << 20, 4), (1, 70, (1 << 20) - 3, 5)])
+def test_ffn_as_wide_as_may_be(layers, n, rows, width, hidden, dtype):  # noqa: F811
+    check_block(layers, n, rows, width, hidden, dtype, "silu")
+
+
+def far_rows(g, n, rows, width, dtype):
+    """Rows (1 << 22) + 57 values apart, the particles' side by side."""
+    stride = (1 << 22) + 57
+    assert n * (width + 2) <= stride
+    buf = torch.empty(rows * stride, dtype=dtype, device="cuda")
+    return buf.as_strided((n, rows, width), (width + 2, stride, 1), 1).copy_(torch.randn(n, rows, width, generator=g).to(dtype).cuda())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("rows", [7, 70, 260])
+def test_rows_far_apart(layers, rows, dtype):  # noqa: F811
+    n, width, hidden = 2, 109, 131
+    g = gen(rows, 6)
+    x, dy = far_rows(g, n, rows, width, dtype), far_rows(g, n, rows, width, dtype)
+    p, grads, _, _ = params(g, n, 3, (hidden, width), (hidden, width), (width, hidden), spread=0.2)
+    got, want = run_ffn(layers, x, dy, p, grads, "silu"), ref.gated_ffn(x, *p, "silu", dy)
+    for name in want:
+        ref.check(got[name], want[name], name)
+    (w, b), (dw, db), _, _ = params(g, n, 1, (width,), (width,))
+    y, mean, rstd = layers.layer_norm_forward(x, w, b)
+    got = {"y": y, "dx": layers.layer_norm_backward(dy, x, w, mean, rstd, dw, db), "dweight": dw, "dbias": db}
+    want = ref.layer_norm(x, w, b, 1e-5, dy)
+    for name in got:
+        ref.check(got[name], want[name], name)
+    assert torch.equal(layers.dropout_forward(x, 0.3, 5, residual=dy), layers.dropout_forward(x.contiguous(), 0.3, 5, residual=dy.contiguous()))
