@@ -265,12 +265,12 @@ template <class TL, class T, int P> struct ColumnsOfB {
     static constexpr int kPairs = TL::kJ / 2, kAtATime = TL::kThreads / kPairs, N = (4 + kAtATime - 1) / kAtATime;
     static_assert(kAtATime >= 1, "a thread for every pair");
     const T *base;   // row 0
-    int64_t stride;  // beyond kFarStride the slow way, as above
+    int64_t stride;  // of the buffers' rows, at most 2^20: a thread's offset fits 32 bits
     uint32_t column; // the first row of the thread's pair
     bool late, single, narrow;
     T v[N][2][8];
     __device__ __forceinline__ ColumnsOfB(const T *b, int64_t s, int64_t first, int64_t count)
-        : base(b), stride(s), single(count < 2), narrow(count < 2 || s > kFarStride)
+        : base(b), stride(s), single(count < 2), narrow(count < 2)
     {
         const int64_t j = first + row();
         late = j + 2 > count && !single;

@@ -207,8 +207,8 @@ struct ThinGrid {
     __device__ __forceinline__ int64_t first() const { return (int64_t)(blockIdx.x % per_particle) * of; }
 };
 
-// calls full(k) for the wave's whole steps, kUnroll at a time through load(u, k) and use(u), then the last one, if it is this
-// wave's and not whole, through load_last(k) and use(0)
+// The wave's whole steps, U at a time through load(u, k) and then use(u), u = 0 .. U - 1, those that are left over one by one; then the last step, if it
+// is this wave's and not whole, through load_last(k) and use(0).
 template <int U, class Load, class Last, class Use> __device__ __forceinline__ void thin_steps(int64_t K, Load load, Last load_last, Use use)
 {
     const int wave = wave_of_block();

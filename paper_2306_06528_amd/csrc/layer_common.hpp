@@ -11,11 +11,6 @@ namespace svgd {
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
-template <int DTYPE> struct ActType;
-template <> struct ActType<SVGD_F32> { typedef float type; };
-template <> struct ActType<SVGD_BF16> { typedef bf16_t type; };
-template <> struct ActType<SVGD_F16> { typedef f16_t type; };
-
 // VEC values of T that are as aligned as T is: rows may start anywhere.  (Global loads and stores of 16 bytes need no
 // more than that here.)
 template <class T, int VEC> struct Pack {
