@@ -102,8 +102,8 @@ int svgd_gated_ffn_forward(int dtype, int activation, int n, int64_t rows, int64
  * Its backward pass, `saved` being the buffer of the forward call with `save` (read only here):
  *     dh = dy down,  dg = dh u act'(g),  du = dh act(g)
  *     dx = dg gate + du up,  dgate = sum_t dg x^T,  dup = sum_t du x^T,  ddown = sum_t dy h^T
- * dx.data, and each of dgate, dup and ddown, may be NULL: that gradient is not wanted then.  scratch (DEVICE,
- * 16-byte aligned): svgd_gated_ffn_scratch bytes.
+ * dx.data, and each of dgate, dup and ddown, may be NULL: that gradient is not wanted then (without any of the parameters'
+ * dx may be summed up in another order: its last bits may be others).  scratch (DEVICE, 16-byte aligned): svgd_gated_ffn_scratch bytes.
  */
 size_t svgd_gated_ffn_scratch(int n, int64_t rows, int64_t width, int64_t hidden);
 int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t hidden, svgd_rows dy,

@@ -45,12 +45,12 @@ template <class T, int ACT, int JB> int thin_forward(const FfnCall &c, const svg
 }
 
 template <class T, int ACT, int JB>
-int thin_backward(const FfnCall &c, const svgd_rows &dy, const float *g, const float *u, const svgd_rows &dx, float *dg, float *du)
+int thin_backward(const FfnCall &c, const svgd_rows &dy, const float *g, const float *u, const svgd_rows &dx, bool with_dx, float *dg, float *du)
 {
     const ThinGrid hidden(c.s.hidden, 32), input(c.s.width, 32);
     thin_hidden_grad_kernel<T, ACT, JB><<<c.n * hidden.per_particle, kThinBlock, 0, c.stream>>>(c.s, hidden, in<T>(dy), c.down, g, u, dg, du);
     const int rc = launched();
-    if (rc || !dx.data) return rc;
+    if (rc || !with_dx) return rc;
     thin_input_grad_kernel<T, JB><<<c.n * input.per_particle, kThinBlock, 0, c.stream>>>(c.s, input, dg, du, c.gate, c.up, out<T>(dx));
     return launched();
 }
@@ -92,18 +92,19 @@ int backward_as(const FfnCall &c, const BackwardPlan &plan, const svgd_rows &dy,
     const int gates = (dgate.p ? 1 : 0) + (dup.p ? 1 : 0);
     const bool thin = plan.thin;
     if (thin && c.s.rows > 0 && (dx.data || gates)) {
-        if (const int rc = c.s.rows <= 16 ? thin_backward<T, ACT, 1>(c, dy, g, u, dx, dg, du) : thin_backward<T, ACT, 2>(c, dy, g, u, dx, dg, du)) return rc;
+        const bool with_dx = plan.thin_input && dx.data;
+        if (const int rc = c.s.rows <= 16 ? thin_backward<T, ACT, 1>(c, dy, g, u, dx, with_dx, dg, du) : thin_backward<T, ACT, 2>(c, dy, g, u, dx, with_dx, dg, du)) return rc;
     }
     if (!thin && (dx.data || gates)) {
         const int rc = with_tile(plan.hidden.kind, [&](auto tile) {
             using TL = decltype(tile);
             const TileGrid grid(c.n, tiles(c.s.hidden, TL::kI), tiles(c.s.rows, TL::kJ), c.s.width, 1);
-                hidden_grad_kernel<TL, T, ACT><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(dy), c.down, g, u, dg, du);
+            hidden_grad_kernel<TL, T, ACT><<<grid.blocks(), TL::kThreads, 0, c.stream>>>(c.s, grid, in<T>(dy), c.down, g, u, dg, du);
             return launched();
         });
         if (rc) return rc;
     }
-    const bool input = !thin && dx.data;
+    const bool input = !plan.thin_input && dx.data;
     if (!input && !gates && !ddown.p) return SVGD_OK;
     int rc = with_tile(plan.gradients, [&](auto tile) {
         using TL = decltype(tile);

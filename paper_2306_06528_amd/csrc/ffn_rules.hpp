@@ -77,14 +77,26 @@ inline Choice choose(const Rates &r, int n, int64_t i, int64_t j, int64_t column
     return best;
 }
 
-// Up to so many rows per particle every weight is read once, by a wave of its own (ffn_thin_kernels.hpp): 8 x 17 rows, 384 x 1,024 fp32, forward 15 us,
-// in tiles 27, 8 x 32 rows 16 and 28; backward of 8 x 17 rows 41, in tiles (of the time) 179.  Forward up to 64 rows where the tiles of g and u are few: 1 x 64
-// rows, 1,024 x 2,730 fp32, 22 tiles, 29 and 51, 8 x 64 rows, 384 x 1,024, 64 tiles, 23 and 29, but 16 x 64 rows, 512 x 1,400 bf16, 176 tiles, 50 and 45,
-// 40 x 64 rows, 256 x 700, 240 tiles, 49 and 36.
+// Up to so many rows per particle every weight is read once, by a wave of its own (ffn_thin_kernels.hpp).  Forward: 8 x 17 rows, 384 x 1,024 fp32, 14 us, in
+// tiles 26, 8 x 32 rows 16 and 28; the worst, 8 x 32 rows, 1,024 x 2,730 bf16, 63 and 61.  dg and du: these and the gradients of the parameters, 4 x 16 rows, 384 x 1,024 fp32, 19 and
+// 29, 1 x 32 rows, 3,000 x 8,000, 159 and 218, 64 x 32 rows, 128 x 341, 32 and 31.
+// Forward up to 64 rows where the tiles of g and u are few: 1 x 64 rows, 1,024 x 2,730 fp32, 22 tiles, 30 and 51, 8 x 64 rows, 384 x 1,024, 64 tiles, 23 and 29,
+// 4 x 64 rows, 1,024 x 2,730, 88 tiles, 55 and 68, but 16 x 64 rows, 512 x 1,400, 176 tiles, 61 both, 40 x 64 rows, 256 x 700, 240 tiles, 52 and 41.
 constexpr int64_t kThinRows = 32;
 inline bool thin_forward_rows(int n, int64_t rows, int64_t hidden)
 {
     return rows <= kThinRows || (rows <= 64 && n * tiles(hidden, kKinds[kLarge].i / 2) < 128);
+}
+
+// The same for dx, whose waves have all of the hidden width to go through.  With gradients of parameters, in whose launch dx's tiles find room, only in narrow
+// layers: both, 3 x 16 rows, 64 x 200 fp32, 15 us, as tiles 18, 64 x 16 rows, 96 x 250, 26 and 31, but 64 x 16 rows, 128 x 341, 36 both, 8 x 16 rows, 384 x 1,024, 36 and 35, with 32 rows 42 and 35,
+// 1 x 32 rows, 1,024 x 2,730, 72 and 48.  dx alone, unless few waves would have long ways: 8 x 16 rows, 384 x 1,024, 17 and 21, 40 x 16 rows, 256 x 700, 34 and 50, but
+// 2 x 16 rows, 200 x 1,500, 31 and 20, 1 x 16 rows, 256 x 16,000, 120 and 47.
+inline bool thin_input_rows(int n, int64_t rows, int64_t width, int64_t hidden, bool params_too)
+{
+    if (rows == 0 || rows > kThinRows) return rows == 0;
+    if (params_too) return width * hidden <= 1 << 15;
+    return hidden <= 1024 || hidden <= 64 * n * tiles(width, 32);
 }
 
 inline int64_t width_ld(int64_t width) { return (width + 3) / 4 * 4; }
@@ -102,19 +114,21 @@ struct ForwardPlan {
     size_t scratch(int n, int64_t rows, int64_t width) const { return down.parts > 1 ? (size_t)down.parts * n * rows * width_ld(width) * 4 : 0; }
 };
 
-// The gradients' tiles are of one kind, being of one launch.  input_parts is 1 or even, see input_grad_tile.
+// The gradients' tiles are of one kind, being of one launch.  input_parts is 1 or even, see input_grad_tile.  params_too: gradients of parameters are wanted.
 struct BackwardPlan {
     Choice hidden;
     TileKind gradients = kLarge;
     int input_parts = 1, param_parts = 0;
-    bool thin;
+    bool thin, thin_input; // dg and du, dx by a wave for every weight
     size_t hidden_floats, input_floats, gate_floats, down_floats;
-    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid) : hidden(choose(kUsual, n, hid, rows, width, 1, 0)), thin(rows <= kThinRows)
+    BackwardPlan(int n, int64_t rows, int64_t width, int64_t hid, bool params_too)
+        : hidden(choose(kUsual, n, hid, rows, width, 1, 0)), thin(rows <= kThinRows), thin_input(thin_input_rows(n, rows, width, hid, params_too))
     {
         double least = 1e30;
         for (int kind = 0; kind < kTileKinds; ++kind) {
             const KindOf &k = kKinds[kind];
-            const int64_t params = 3 * n * tiles(width, k.i) * tiles(hid, k.j), input = !thin ? n * tiles(width, k.i) * tiles(rows, k.j) : 0;
+            const int64_t params = 3 * n * tiles(width, k.i) * tiles(hid, k.j), input = !thin_input ? n * tiles(width, k.i) * tiles(rows, k.j) : 0;
+            if (thin && kind == kLarge) continue; // (one step each: 8 x 8 rows, 384 x 1,024 fp32, all gradients 44 us, small ones 35, 40 x 8 rows, 256 x 700, 89 and 70; never the best by more than 2 %)
             if (!launchable((TileKind)kind, blocks_for(params / 3 * 2) + blocks_for(params / 3) + blocks_for(input))) continue;
             for (int pp = 1; pp <= 32 && (pp == 1 || (rows / pp >= 4 * kTileK && params * pp <= 1024)); pp *= 2)
                 for (int ip = 1; ip <= 32 && (ip == 1 || (2 * hid / ip >= 4 * kTileK && input * ip <= 1024 && input > 0)); ip *= 2) {

@@ -45,7 +45,8 @@ size_t svgd_gated_ffn_forward_scratch(int n, int64_t rows, int64_t width, int64_
 size_t svgd_gated_ffn_scratch(int n, int64_t rows, int64_t width, int64_t hidden)
 {
     if (!sized(n, rows, width, hidden)) return 0;
-    return BackwardPlan(n, rows, width, hidden).scratch();
+    const size_t all = BackwardPlan(n, rows, width, hidden, true).scratch(), dx_alone = BackwardPlan(n, rows, width, hidden, false).scratch();
+    return all > dx_alone ? all : dx_alone;
 }
 
 int svgd_gated_ffn_forward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t hidden, svgd_rows x, const float *gate,
@@ -92,7 +93,7 @@ int svgd_gated_ffn_backward(int dtype, int activation, int n, int64_t rows, int6
         for (const Params &o : grads)
             if (&o > &g && o.p && params_meet(g, o, n)) return SVGD_ERR_INVALID_ARG;
     }
-    const BackwardPlan plan(n, rows, width, hidden);
+    const BackwardPlan plan(n, rows, width, hidden, grads[0].p || grads[1].p || grads[2].p);
     if (rows > 0) {
         const size_t saved_need = svgd_gated_ffn_buffer(n, rows, width, hidden, 1), need = plan.scratch();
         if (!valid_input(dy, dtype, rows) || !saved || !aligned_to(saved, 16) || saved_bytes < saved_need || !scratch || !aligned_to(scratch, 16) ||

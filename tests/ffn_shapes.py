@@ -11,3 +11,7 @@ TILES = [(26, 68, 102, 1_101), (39, 34, 101, 1_118), (32, 35, 103, 402), (16, 2_
 
 # Few rows, with columns enough for every wave to work on several steps, the last one a part of one.
 THIN = [(2, 5, 545, 683), (1, 16, 577, 775), (3, 1, 600, 700), (2, 17, 700, 557), (1, 32, 570, 641), (1, 50, 600, 553), (1, 64, 555, 560), (1, 9, 768, 576)]
+
+# Few rows, backward: dx by a wave for every weight or in tiles, with the parameters' gradients and without them.
+DX_OF_FEW_ROWS = [(3, 7, 100, 203), (2, 16, 16, 2_000), (5, 9, 190, 301), (2, 13, 70, 1_501), (2, 31, 61, 333), (1, 20, 15, 1_700), (40, 25, 129, 321), (1, 32, 90, 2_003),
+                  (64, 3, 130, 260), (12, 1, 353, 1_001)]

@@ -19,19 +19,20 @@ int main()
     long long n, rows, width, hidden;
     while (std::scanf("%lld %lld %lld %lld", &n, &rows, &width, &hidden) == 4) {
         const ForwardPlan f((int)n, rows, width, hidden);
-        const BackwardPlan b((int)n, rows, width, hidden);
+        const BackwardPlan b((int)n, rows, width, hidden, true);
         const auto count = [&](TileKind k, long long i, long long j, int per_i) { return (long long)(n * tiles(i, kKinds[k].i / per_i) * tiles(j, kKinds[k].j)); };
         const TileKind g = b.gradients;
-        std::printf("%d %d %d %lld %d %d %lld %d %d %d %lld %d %d %d %lld\n", f.fits(), f.thin, f.gate_up.kind, count(f.gate_up.kind, hidden, rows, 2), f.down.kind,
+        std::printf("%d %d %d %lld %d %d %lld %d %d %d %lld %d %d %d %lld %d %d\n", f.fits(), f.thin, f.gate_up.kind, count(f.gate_up.kind, hidden, rows, 2), f.down.kind,
                     f.down.parts, count(f.down.kind, width, rows, 1) * f.down.parts, b.fits(), b.thin, b.hidden.kind, count(b.hidden.kind, hidden, rows, 1), g,
                     b.input_parts, b.param_parts,
-                    (b.thin ? 0 : count(g, width, rows, 1) * b.input_parts) + 3 * count(g, width, hidden, 1) * b.param_parts);
+                    (b.thin_input ? 0 : count(g, width, rows, 1) * b.input_parts) + 3 * count(g, width, hidden, 1) * b.param_parts, b.thin_input,
+                    BackwardPlan((int)n, rows, width, hidden, false).thin_input);
     }
 }
 """
 THREADS = (256, 128, 64)
 Plan = collections.namedtuple("Plan", "fits thin gate_up gate_up_tiles down down_parts down_tiles back_fits back_thin dh dh_tiles gradients input_parts param_parts "
-                              "gradients_tiles")
+                              "gradients_tiles dx_thin dx_alone_thin")
 
 
 @pytest.fixture(scope="module")
@@ -126,3 +127,15 @@ def test_the_shapes_that_are_tested_give_waves_of_few_rows_several_steps(rules):
         if all(columns // 32 // 8 >= 2 and -(-(columns // 32) // 8) % 2 == 1 and columns % 32 for columns in (width, hidden)):
             seen |= {(rows > 16) + (rows > 32)}
     assert seen == {0, 1, 2}
+
+
+def test_the_shapes_that_are_tested_take_every_way_to_dx_of_few_rows(rules):
+    from ffn_shapes import DX_OF_FEW_ROWS, THIN
+    plans = rules(DX_OF_FEW_ROWS + THIN)
+    assert all(p.back_thin for (_, rows, *_), p in zip(DX_OF_FEW_ROWS + THIN, plans) if rows <= 32)
+    assert {(rows > 16, p.dx_thin, p.dx_alone_thin) for (_, rows, *_), p in zip(DX_OF_FEW_ROWS, plans)} == {
+        (more, a, b) for more in (False, True) for a, b in ((0, 0), (0, 1), (1, 0), (1, 1))}
+    assert {p.gradients for (_, rows, *_), p in zip(DX_OF_FEW_ROWS + THIN, plans) if rows <= 32} == {1, 2}
+    # (the longest way: a wave goes through all of the hidden width for dx)
+    assert not any(p.dx_alone_thin for p in rules([(1, 1, 256, 16_000), (1, 32, 16, 1 << 20)]))
+    assert all(p.dx_thin and p.dx_alone_thin for p in rules([(n, 0, width, hidden) for n in (1, 64) for width in (1, 700) for hidden in (1, 5_000)]))

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import layer_reference as ref
-from ffn_shapes import THIN, TILES
+from ffn_shapes import DX_OF_FEW_ROWS, THIN, TILES
 from test_gpu_layers import IDS, TYPES, acts, gen, layers, params, run_ffn  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -73,3 +73,34 @@ def test_rows_far_apart(layers, rows, dtype):  # noqa: F811
     for name in got:
         ref.check(got[name], want[name], name)
     assert torch.equal(layers.dropout_forward(x, 0.3, 5, residual=dy), layers.dropout_forward(x.contiguous(), 0.3, 5, residual=dy.contiguous()))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("n,rows,width,hidden", DX_OF_FEW_ROWS)
+def test_ffn_gradients_of_few_rows(layers, n, rows, width, hidden, dtype):  # noqa: F811
+    """All gradients, dx alone, and the parameters' alone."""
+    g = gen(n, rows, width, hidden, 7)
+    x, dy = acts(g, n, rows, width, dtype, "gap"), acts(g, n, rows, width, dtype)
+    p, grads, G, D = params(g, n, 3, (hidden, width), (hidden, width), (width, hidden), spread=width ** -0.5)
+    want = ref.gated_ffn(x, *p, "silu", dy)
+    y, saved = layers.gated_ffn_forward(x, *p, save=True)
+    dx = layers.gated_ffn_backward(dy, x, *p, saved, *grads)
+    for name, got in (("y", y), ("dx", dx), ("dgate", grads[0]), ("dup", grads[1]), ("ddown", grads[2])):
+        ref.check(got, want[name], name)
+    first = [t.clone() for t in grads]
+    ref.check(layers.gated_ffn_backward(dy, x, *p, saved), want["dx"], "dx alone")
+    assert torch.equal(layers.gated_ffn_backward(dy, x, *p, saved, None, grads[1], None, accumulate=True), dx)
+    assert torch.equal(grads[0], first[0]) and torch.equal(grads[1], 2 * first[1]) and torch.equal(grads[2], first[2])
+    assert layers.gated_ffn_backward(dy, x, *p, saved, *grads, want_dx=False) is None
+    assert all(torch.equal(a, b) for a, b in zip(grads, first))
+    assert (G[:, :3] == -7.0).all() and (G[:, D - 3:] == -7.0).all()
+
+
+def test_ffn_no_rows_of_many_particles(layers):  # noqa: F811
+    p, grads, G, _ = params(gen(42), 40, 0, (400, 300), (400, 300), (300, 400))
+    x = torch.empty(40, 0, 300, device="cuda")
+    y, saved = layers.gated_ffn_forward(x, *p, save=True)
+    assert layers.gated_ffn_backward(x, x, *p, saved, *grads, accumulate=True).shape == x.shape
+    assert (G == -7.0).all()
+    layers.gated_ffn_backward(x, x, *p, saved, *grads)
+    assert all((v == 0).all() for v in grads)
