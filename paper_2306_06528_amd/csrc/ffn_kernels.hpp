@@ -12,7 +12,7 @@
 // the accuracy of fp32 products at 2.5 PFLOP/s / 6 (5, 3), where the fp32 matrix instructions end at 157 TFLOP/s; and
 // since each part is read from LDS once for several products, LDS keeps up with half the traffic a
 // plain bf16 product needs.  The matrix cores bound the large products: 8 x 4,096 x 1,024 x 2,730 bf16, forward and backward, are 6.60 TFLOP
-// of theirs and take 5.51 ms, 1,198 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,156 on the same card).
+// of theirs and take 5.65 to 5.76 ms, 1,145 to 1,170 TFLOP/s (a library's 8,192^3 bf16 product reaches 1,120 to 1,155 on the same card).
 #pragma once
 #include "ffn_rules.hpp"
 #include "layer_common.hpp"

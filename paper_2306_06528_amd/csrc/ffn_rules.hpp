@@ -12,7 +12,8 @@ inline int64_t hidden_ld(int64_t hidden) { return (hidden + 31) / 32 * 32; } // 
 inline int64_t tiles(int64_t size, int tile) { return (size + tile - 1) / tile; }
 
 // ---------------------------------------------------------------------------------------------
-// Which tiles, and into how many parts the columns go: by sizes alone, the same for every type
+// Which tiles, and into how many parts the columns go: by sizes alone, the same for every type.  (The smallest tiles of g, u and dh take 164 registers for
+// bf16 activations, 192 for fp32, so half as many more workgroups run at a time: the rule reckons with fp32.)
 // ---------------------------------------------------------------------------------------------
 enum TileKind { kLarge, kSmall, kTiny, kTileKinds };
 struct KindOf {
@@ -34,13 +35,13 @@ struct Rates {
 };
 // g and u, dh: at 15 shapes (1 to 40 particles of 64 to 16,000 rows, 64 to 1,024 wide) this finds the fastest or one within 5 % of it.
 constexpr Rates kUsual = {{1.0, 0.6, 0.35}, 0.6, 4.0, 0.0, 1.0}; // (never in parts)
-// y = h down^T: the one product whose operands both lie along the columns, h of three parts.  Small tiles cost more there (at 15 shapes, 1 to 40 particles
-// of 64 to 16,000 rows, 64 to 1,024 wide, this finds the fastest or one within 5 % of it; with the usual ones forward took 8 x 1,576 x 384 x
-// 1,024 bf16 146 us for 134, 2 x 3,000 x 768 x 2,048 fp32 345 for 299).
+// y = h down^T: the one product whose operands both lie along the columns, both of three parts.  Small tiles cost more there (of 15 shapes, 1 to 40 particles
+// of 64 to 16,000 rows, 64 to 1,024 wide, this finds the fastest or one within 5 % of it at 14 and takes 7 % more at one; with the usual ones forward would take 8 x 1,576 x 384 x
+// 1,024 bf16 166 us for 155, 2 x 3,000 x 768 x 2,048 fp32 351 for 297).
 constexpr Rates kOfDown = {{1.0, 0.6, 0.5}, 0.8, 3.0, 0.6, 16e6};
 // The gradients, tiles of dx and of the parameters in one launch: workgroups of other lengths side by side, results of four bytes each.  Of all kinds
 // and parts at 27 shapes (1 to 64 particles of 50 to 16,000 rows, 48 to 1,024 wide) this finds the fastest or one within 5 % of it at 23 and
-// never takes more than 20 % more; with the usual rates and kOfDown's reductions these would be 17 and 22 %.
+// never takes more than 17 % more.
 constexpr Rates kOfGradients = {{1.0, 0.62, 0.4}, 0.9, 10.0, 0.3, 6e6};
 inline double launch_cost(const Rates &r, TileKind kind, int64_t workgroups, double work, double longest)
 {

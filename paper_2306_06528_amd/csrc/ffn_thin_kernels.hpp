@@ -72,7 +72,7 @@ template <class T> struct ThinRows {
 constexpr int kSlot = 16 * kTileK / 4; // one operand, in 16 bytes
 
 // Forward with up to 16 rows three workgroups fit a CU, which the compiler has to be told, if a wave has one step of gate and up on its way, or two
-// of down: 16 x 1 rows, 256 x 683 fp32 9.8 us; two workgroups and twice the steps 10.9 (8 x 5 rows, 1,024 x 2,731 bf16 55 both, 1 x 8 rows, 4,096 x
+// of down (whether the grid has so many is not looked at): 16 x 1 rows, 256 x 683 fp32 9.8 us; two workgroups and twice the steps 10.9 (8 x 5 rows, 1,024 x 2,731 bf16 55 both, 1 x 8 rows, 4,096 x
 // 11,008 110 and 106).
 #define SVGD_THIN_KERNEL __global__ __launch_bounds__(kThinBlock) __attribute__((amdgpu_waves_per_eu(JB == 1 ? 6 : 2)))
 
