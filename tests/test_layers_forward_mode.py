@@ -60,3 +60,18 @@ def test_what_is_kept(monkeypatch, enabled):
 def test_tangents_are_refused_on_the_gpu():
     from paper_2306_06528_amd import layers
     check_refused(layers, torch.ones(2, 3, 4, device="cuda"))
+
+
+def test_tangents_of_function_transforms_are_refused(monkeypatch):
+    from paper_2306_06528_amd import layers
+    monkeypatch.setattr(layers, "dropout_forward", lambda x, p, seed, call, residual, counter: x * 2)
+
+    def quiet(x):
+        with torch.no_grad():
+            return layers.dropout(x, 0.5, 1)
+
+    x = torch.ones(2, 3, 4)
+    assert torch.equal(quiet(x), 2 * x)
+    for f in (quiet, lambda t: layers.dropout(t, 0.5, 1)):
+        with pytest.raises((NotImplementedError, RuntimeError)):
+            torch.func.jvp(f, (x,), (x,))
