@@ -1,0 +1,441 @@
+// Attention, backward, without atomics: one kernel has rows of its own and streams keys and values past them (dq, and the slopes' gradients row by row), the other has keys of its own and
+// streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse.
+//     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
+// P and dz are rounded to the activations' type for the products with do, k and q (BlockScale: fp16), as o and the gradients themselves are.
+#pragma once
+#include "attention_common.hpp"
+
+namespace svgd {
+
+// delta of every row: 16 lanes each.
+template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel(AttnArgs a, Heads<const T> o, Heads<const T> d_o, float *delta)
+{
+    const int64_t k = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), lines = (int64_t)a.n * a.batch * a.t * a.heads;
+    if (k >= lines) return;
+    const int h = (int)(k % a.heads);
+    const int64_t token = k / a.heads;
+    const int i = (int)(token % a.t), b = (int)(token / a.t % a.batch), particle = (int)(token / a.t / a.batch);
+    const int c = 8 * (threadIdx.x & 15);
+    const Frag<T> x = load_frag(o.at(particle, b, h) + i * o.token + c, a.dim - c), y = load_frag(d_o.at(particle, b, h) + i * d_o.token + c, a.dim - c);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += (float)x[e] * (float)y[e];
+    sum = row_sum(sum);
+    if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
+}
+
+// The exponent (of 2) of a score, and 1 - tanh^2.
+template <class T> __device__ __forceinline__ float modified(const AttnArgs &a, float score, float slope, float distance, float &damp)
+{
+    float z = score * a.scale;
+    if (a.cap > 0.f) {
+        const float t = tanh_of<T>(z / a.cap);
+        damp = 1.f - t * t;
+        z = a.cap * t;
+    }
+    return (z - slope * distance) * kLog2e;
+}
+
+template <class T, int KD, int QB, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+                                                                                                              const float *lse, const float *delta, Heads<T> dq, float *slope_rows)
+{
+    typedef Tile64<T, KD> TL;
+    __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
+    __shared__ int red[4], key_documents[2][kTileRows];
+    const AttnBlock at(a);
+    if (!at.any) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int tile = a.causal ? a.tiles - 1 - at.tile : at.tile;
+    const int first = tile * (16 * QB * kAttnWaves), own = first + wave * 16 * QB;
+    const Masks masks(a, at.batch);
+    const float mul = MOD ? 1.f : a.scale * kLog2e;
+
+    Frag<T> qf[QB][KD], df[QB][KD];
+    int limit[QB], position[QB], document[QB];
+    float slope[QB], log[QB], del[QB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = min(own + 16 * b + (lane & 15), a.rows - 1), i = a.query(r), h = at.head * a.group + r - i * a.group;
+        const T *const p = q.at(at.particle, at.batch, h) + i * q.token, *const d = d_o.at(at.particle, at.batch, h) + i * d_o.token;
+#pragma unroll
+        for (int s = 0; s < KD; ++s) {
+            qf[b][s] = load_frag(p + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+            df[b][s] = load_frag(d + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+        }
+        position[b] = masks.start + i;
+        limit[b] = masks.end(a, position[b]);
+        document[b] = masks.document(a, position[b]);
+        slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + h] : 0.f;
+        const int64_t line = a.line(at.particle, at.batch, h, i);
+        log[b] = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e; // (a row that sees nothing: every probability 0)
+        del[b] = delta[line];
+    }
+    const int last_row = min(first + 16 * QB * kAttnWaves, a.rows) - 1;
+    const int p0 = masks.start + a.query(first), p1 = masks.start + a.query(last_row);
+    int lo = 0, hi = masks.documents ? (p1 < 0 || p0 >= a.s ? 0 : masks.end(a, min(p1, a.s - 1))) : masks.end(a, p1);
+    const int free_keys = masks.documents ? 0 : masks.end(a, p0);
+    if (masks.documents) narrow(masks.documents, p0, p1, a.s, red, lo, hi);
+    const int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
+    const int wave_row = min(own + 16 * QB, a.rows) - 1;
+    const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
+
+    f32x4 acc[2 * KD][QB];
+    float sum_dz[QB], sum_dz_far[QB], sum_far[QB]; // of dz, dz distance and P distance
+    BlockScale bs;
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        sum_dz[b] = sum_dz_far[b] = sum_far[b] = 0.f;
+#pragma unroll
+        for (int d = 0; d < 2 * KD; ++d) acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
+    TL kt, vt;
+    int next_document = 0;
+    const auto fetch = [&](int tile_of) {
+        const int key = tile_of * kTileRows;
+        kt.load(hi - key, a.dim, [&](int i) { return ks + (key + i) * k.token; });
+        vt.load(hi - key, a.dim, [&](int i) { return vs + (key + i) * v.token; });
+        if (masks.documents && threadIdx.x < kTileRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
+    };
+    const auto stage = [&](int half) {
+        kt.store(lds + half * 2 * TL::kSize);
+        vt.store(lds + (half * 2 + 1) * TL::kSize);
+        if (masks.documents && threadIdx.x < kTileRows) key_documents[half][threadIdx.x] = next_document;
+    };
+    if (begin < end) {
+        fetch(begin);
+        stage(0);
+    }
+    __syncthreads();
+    int half = 0;
+    for (int n = begin; n < end; ++n) {
+        if (n + 1 < end) fetch(n + 1);
+        const int key0 = n * kTileRows;
+        if (key0 < wave_limit) {
+            const T *const kl = lds + half * 2 * TL::kSize, *const vl = kl + TL::kSize;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const int key = key0 + 32 * m;
+                f32x4 s[2][QB], dp[2][QB];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) s[j][b] = dp[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < KD; ++c) {
+                        const Frag<T> f = TL::rows(kl, 32 * m + 16 * j, 32 * c), e = TL::rows(vl, 32 * m + 16 * j, 32 * c);
+#pragma unroll
+                        for (int b = 0; b < QB; ++b) {
+                            s[j][b] = mma(f, qf[b][c], s[j][b]);
+                            dp[j][b] = mma(e, df[b][c], dp[j][b]);
+                        }
+                    }
+                }
+                const bool masked = key0 + kTileRows > free_keys;
+                float largest = 0.f;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at_key = key + 16 * j + 4 * g + e;
+                        const int doc = masked && masks.documents ? key_documents[half][32 * m + 16 * j + 4 * g + e] : 0;
+#pragma unroll
+                        for (int b = 0; b < QB; ++b) {
+                            float x = s[j][b][e], damp = 1.f;
+                            [[maybe_unused]] const float far = fabsf((float)(position[b] - at_key));
+                            if constexpr (MOD) x = modified<T>(a, x, slope[b], far, damp);
+                            if (masked && (at_key >= limit[b] || doc != document[b])) x = -INFINITY;
+                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
+                            float dz = p * (dp[j][b][e] - del[b]);
+                            if (masked && p == 0.f) dz = 0.f;
+                            if constexpr (MOD) {
+                                if (a.slopes) {
+                                    sum_dz[b] += dz;
+                                    sum_dz_far[b] += dz * far;
+                                    sum_far[b] += p * far;
+                                }
+                                dz *= damp;
+                            }
+                            s[j][b][e] = dz;
+                            if constexpr (sizeof(T) == 2 && !std::is_same<T, bf16_t>::value) largest = fmaxf(largest, fabsf(dz));
+                        }
+                    }
+                if constexpr (std::is_same<T, f16_t>::value) {
+                    const float factor = bs.take(largest);
+                    if (factor != 1.f) {
+#pragma unroll
+                        for (int b = 0; b < QB; ++b)
+#pragma unroll
+                            for (int d = 0; d < 2 * KD; ++d) acc[d][b] *= factor;
+                    }
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) {
+                        s[0][b] *= bs.scale;
+                        s[1][b] *= bs.scale;
+                    }
+                }
+                Frag<T> z[QB];
+#pragma unroll
+                for (int b = 0; b < QB; ++b) z[b] = as_operand<T>(s[0][b], s[1][b]);
+#pragma unroll
+                for (int d = 0; d < 2 * KD; ++d) {
+                    const Frag<T> f = TL::columns(kl, 32 * m, 16 * d);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, z[b], acc[d][b]);
+                }
+            }
+        }
+        half ^= 1;
+        if (n + 1 < end) stage(half);
+        __syncthreads();
+    }
+    const float factor = std::is_same<T, f16_t>::value ? a.scale / bs.scale : a.scale;
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = own + 16 * b + (lane & 15);
+        const int i = a.query(min(r, a.rows - 1)), h = at.head * a.group + min(r, a.rows - 1) - i * a.group;
+        if constexpr (MOD) {
+            // The sum of dz is 0 but for roundings, those of delta the largest: what they put on the sum with the distances is taken off (the probabilities add up to 1)
+            const float z = sum_over_rows(sum_dz[b]), zf = sum_over_rows(sum_dz_far[b]), f = sum_over_rows(sum_far[b]);
+            if (a.slopes && slope_rows && r < a.rows && g == 0) slope_rows[a.line(at.particle, at.batch, h, i)] = z * f - zf;
+        }
+        if (r >= a.rows || !dq.p) continue;
+        T *const out = dq.at(at.particle, at.batch, h) + i * dq.token;
+#pragma unroll
+        for (int d = 0; d < 2 * KD; ++d) {
+            const int c = 16 * d + 4 * g;
+            const float x[4] = {acc[d][b][0] * factor, acc[d][b][1] * factor, acc[d][b][2] * factor, acc[d][b][3] * factor};
+            if (c < a.dim) store_pack<T, 4>(out + c, a.dim - c, x);
+        }
+    }
+}
+
+// What a streamed row brings besides its values.
+struct RowInfo {
+    float log[kTileRows], delta[kTileRows], slope[kTileRows];
+    int limit[kTileRows], position[kTileRows], document[kTileRows];
+};
+
+template <class T, int KD, int KB, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+                                                                                                           const float *lse, const float *delta, Heads<T> dk, Heads<T> dv)
+{
+    typedef Tile64<T, KD> TL;
+    constexpr bool kHalf = std::is_same<T, f16_t>::value;
+    constexpr float kExponent = kHalf ? 14.f : 0.f; // of probabilities as operands
+    __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
+    __shared__ RowInfo infos[2];
+    __shared__ int red[4];
+    const AttnBlock at(a);
+    if (!at.any) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int first = at.tile * (16 * KB * kAttnWaves), own = first + wave * 16 * KB;
+    const Masks masks(a, at.batch);
+    const float mul = MOD ? 1.f : a.scale * kLog2e;
+
+    Frag<T> kf[KB][KD], vf[KB][KD];
+    int key[KB], document[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        key[b] = own + 16 * b + (lane & 15);
+        const bool there = key[b] < masks.length;
+        const T *const kp = k.at(at.particle, at.batch, at.head) + key[b] * k.token, *const vp = v.at(at.particle, at.batch, at.head) + key[b] * v.token;
+#pragma unroll
+        for (int s = 0; s < KD; ++s) {
+            const int left = there ? a.dim - 32 * s - 8 * g : 0;
+            kf[b][s] = load_frag(kp + 32 * s + 8 * g, left);
+            vf[b][s] = load_frag(vp + 32 * s + 8 * g, left);
+        }
+        document[b] = masks.documents && there ? masks.documents[key[b]] : 0;
+    }
+    // the rows that may see the workgroup's keys
+    int row_lo = 0, row_hi = first < masks.length ? a.rows : 0;
+    const int last_key = min(first + 16 * KB * kAttnWaves, masks.length) - 1;
+    if (a.causal && masks.prefix <= first) row_lo = (int)min((int64_t)max(first - masks.start, 0) * a.group, (int64_t)a.rows);
+    if (masks.documents && row_hi > 0) {
+        int lo = masks.start + row_lo / a.group, hi = masks.start + a.t;
+        narrow(masks.documents, first, last_key, a.s, red, lo, hi);
+        row_lo = hi > lo ? max(row_lo, (lo - masks.start) * a.group) : 0;
+        row_hi = hi > lo ? min(a.rows, (hi - masks.start) * a.group) : 0;
+    }
+    const int begin = row_lo / kTileRows, end = row_hi > row_lo ? (row_hi + kTileRows - 1) / kTileRows : begin;
+    // tiles from this row on need no mask
+    const int wave_last = own + 16 * KB - 1;
+    const int free_row = masks.documents || wave_last >= masks.length ? INT32_MAX
+                         : !a.causal || masks.prefix > wave_last      ? 0
+                                                                      : (int)min((int64_t)max(wave_last - masks.start, 0) * a.group, (int64_t)INT32_MAX);
+
+    f32x4 acc_k[2 * KD][KB], acc_v[2 * KD][KB];
+    BlockScale bs;
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int d = 0; d < 2 * KD; ++d) acc_k[d][b] = acc_v[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    TL qt, dt;
+    float next_log = 0.f, next_delta = 0.f, next_slope = 0.f;
+    int next_limit = 0, next_position = 0, next_document = 0;
+    const auto fetch = [&](int tile_of) {
+        const int row = tile_of * kTileRows;
+        qt.load(a.rows - row, a.dim, [&](int j) {
+            const int i = a.query(row + j), h = at.head * a.group + row + j - i * a.group;
+            return q.at(at.particle, at.batch, h) + i * q.token;
+        });
+        dt.load(a.rows - row, a.dim, [&](int j) {
+            const int i = a.query(row + j), h = at.head * a.group + row + j - i * a.group;
+            return d_o.at(at.particle, at.batch, h) + i * d_o.token;
+        });
+        if (threadIdx.x < kTileRows) {
+            const int r = row + (int)threadIdx.x;
+            next_log = INFINITY;
+            next_delta = next_slope = 0.f;
+            next_limit = next_position = next_document = 0;
+            if (r < a.rows) {
+                const int i = a.query(r), h = at.head * a.group + r - i * a.group;
+                const int64_t line = a.line(at.particle, at.batch, h, i);
+                next_log = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e;
+                next_delta = delta[line];
+                next_position = masks.start + i;
+                next_limit = masks.end(a, next_position);
+                next_document = masks.document(a, next_position);
+                if (MOD && a.slopes) next_slope = a.slopes[at.particle * a.slopes_stride + h];
+            }
+        }
+    };
+    const auto stage = [&](int half) {
+        qt.store(lds + half * 2 * TL::kSize);
+        dt.store(lds + (half * 2 + 1) * TL::kSize);
+        if (threadIdx.x < kTileRows) {
+            RowInfo &info = infos[half];
+            info.log[threadIdx.x] = next_log;
+            info.delta[threadIdx.x] = next_delta;
+            info.slope[threadIdx.x] = next_slope;
+            info.limit[threadIdx.x] = next_limit;
+            info.position[threadIdx.x] = next_position;
+            info.document[threadIdx.x] = next_document;
+        }
+    };
+    if (begin < end) {
+        fetch(begin);
+        stage(0);
+    }
+    __syncthreads();
+    int half = 0;
+    for (int n = begin; n < end; ++n) {
+        if (n + 1 < end) fetch(n + 1);
+        const T *const ql = lds + half * 2 * TL::kSize, *const dl = ql + TL::kSize;
+        const RowInfo &info = infos[half];
+        const bool masked = n * kTileRows < free_row;
+        if (own < masks.length)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                f32x4 s[2][KB], dp[2][KB];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) s[j][b] = dp[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < KD; ++c) {
+                        const Frag<T> f = TL::rows(ql, 32 * m + 16 * j, 32 * c), e = TL::rows(dl, 32 * m + 16 * j, 32 * c);
+#pragma unroll
+                        for (int b = 0; b < KB; ++b) {
+                            s[j][b] = mma(f, kf[b][c], s[j][b]);
+                            dp[j][b] = mma(e, vf[b][c], dp[j][b]);
+                        }
+                    }
+                }
+                float largest = 0.f;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = 32 * m + 16 * j + 4 * g;
+                    const f32x4 log = *reinterpret_cast<const f32x4 *>(&info.log[r]), del = *reinterpret_cast<const f32x4 *>(&info.delta[r]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                        for (int b = 0; b < KB; ++b) {
+                            float x = s[j][b][e], damp = 1.f;
+                            if constexpr (MOD) x = modified<T>(a, x, info.slope[r + e], fabsf((float)(info.position[r + e] - key[b])), damp);
+                            if (masked && (key[b] >= info.limit[r + e] || document[b] != info.document[r + e])) x = -INFINITY;
+                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, kExponent - log[e]));
+                            float dz = p * (dp[j][b][e] - del[e]);
+                            if (masked && p == 0.f) dz = 0.f;
+                            if constexpr (MOD) dz *= damp;
+                            s[j][b][e] = p;
+                            dp[j][b][e] = dz;
+                            if constexpr (kHalf) largest = fmaxf(largest, fabsf(dz));
+                        }
+                    }
+                }
+                if constexpr (kHalf) {
+                    const float factor = bs.take(largest);
+                    if (factor != 1.f) {
+#pragma unroll
+                        for (int b = 0; b < KB; ++b)
+#pragma unroll
+                            for (int d = 0; d < 2 * KD; ++d) acc_k[d][b] *= factor;
+                    }
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) {
+                        dp[0][b] *= bs.scale;
+                        dp[1][b] *= bs.scale;
+                    }
+                }
+                Frag<T> p[KB], z[KB];
+#pragma unroll
+                for (int b = 0; b < KB; ++b) {
+                    p[b] = as_operand<T>(s[0][b], s[1][b]);
+                    z[b] = as_operand<T>(dp[0][b], dp[1][b]);
+                }
+#pragma unroll
+                for (int d = 0; d < 2 * KD; ++d) {
+                    const Frag<T> f = TL::columns(dl, 32 * m, 16 * d), e = TL::columns(ql, 32 * m, 16 * d);
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) {
+                        acc_v[d][b] = mma(f, p[b], acc_v[d][b]);
+                        acc_k[d][b] = mma(e, z[b], acc_k[d][b]);
+                    }
+                }
+            }
+        half ^= 1;
+        if (n + 1 < end) stage(half);
+        __syncthreads();
+    }
+    const float of_k = kHalf ? a.scale * 0x1p-14f / bs.scale : a.scale, of_v = kHalf ? 0x1p-14f : 1.f;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        if (key[b] >= a.s) continue;
+        T *const to_k = dk.at(at.particle, at.batch, at.head) + key[b] * dk.token, *const to_v = dv.at(at.particle, at.batch, at.head) + key[b] * dv.token;
+#pragma unroll
+        for (int d = 0; d < 2 * KD; ++d) {
+            const int c = 16 * d + 4 * g;
+            const float x[4] = {acc_k[d][b][0] * of_k, acc_k[d][b][1] * of_k, acc_k[d][b][2] * of_k, acc_k[d][b][3] * of_k};
+            const float y[4] = {acc_v[d][b][0] * of_v, acc_v[d][b][1] * of_v, acc_v[d][b][2] * of_v, acc_v[d][b][3] * of_v};
+            if (c < a.dim && dk.p) store_pack<T, 4>(to_k + c, a.dim - c, x);
+            if (c < a.dim && dv.p) store_pack<T, 4>(to_v + c, a.dim - c, y);
+        }
+    }
+}
+
+// A slope's gradient: what its rows give, added up by one workgroup, in an order that is always the same.
+static __global__ __launch_bounds__(256) void attention_slopes_kernel(AttnArgs a, const float *slope_rows, float *dslopes, int64_t stride, bool accumulate)
+{
+    __shared__ float sums[4];
+    const int particle = blockIdx.x / a.heads, h = blockIdx.x - particle * a.heads;
+    float sum = 0.f;
+    for (int b = 0; b < a.batch; ++b) {
+        const float *const rows = slope_rows + a.line(particle, b, h, 0);
+        float part = 0.f;
+        for (int i = threadIdx.x; i < a.t; i += 256) part += rows[i];
+        sum += part;
+    }
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float *const to = dslopes + particle * stride + h;
+        const float all = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        *to = accumulate ? *to + all : all;
+    }
+}
+
+} // namespace svgd

@@ -1,0 +1,238 @@
+// Attention, forward.  A workgroup has 64 QB rows, a wave 16 QB of them; tiles of 64 keys and their values go through two halves of LDS, the next tile being on its way
+// from memory while one is worked on.  One pass with the running maximum and sum: sums are rescaled only where a maximum rises by more than 2^8.
+#pragma once
+#include "attention_common.hpp"
+
+namespace svgd {
+
+// Probabilities are rounded to the activations' type for their product with the values, relative to the running maximum: half a step of the type each, as o itself is rounded, with
+// signs as random.  fp16 ones are held 2^6 times as large, so that those down to 2^-20 keep their digits.
+template <class T> constexpr float kProbExponent = 0.f;
+template <> inline constexpr float kProbExponent<f16_t> = 6.f;
+
+// S, scores of 16 streamed keys key .. key + 3 a lane, to what is an exponent of 2 after multiplication by `mul`.
+template <class T, bool MOD> __device__ __forceinline__ float exponent_factor(const AttnArgs &a) { return MOD ? 1.f : a.scale * kLog2e; }
+
+template <class T, int KD, int QB, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1))) void attention_forward_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o,
+                                                                                                              float *lse, float *partial, float *partial_lse)
+{
+    typedef Tile64<T, KD> TL;
+    __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
+    __shared__ int red[4], key_documents[2][kTileRows];
+    const AttnBlock at(a);
+    if (!at.any) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int tile = a.causal ? a.tiles - 1 - at.tile : at.tile; // (those with the most keys first)
+    const int first = tile * (16 * QB * kAttnWaves), own = first + wave * 16 * QB;
+    const Masks masks(a, at.batch);
+    const float mul = exponent_factor<T, MOD>(a);
+
+    Frag<T> qf[QB][KD];
+    int limit[QB], position[QB], document[QB];
+    float slope[QB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = min(own + 16 * b + (lane & 15), a.rows - 1), i = a.query(r), h = r - i * a.group;
+        const T *const p = q.at(at.particle, at.batch, at.head * a.group + h) + i * q.token;
+#pragma unroll
+        for (int s = 0; s < KD; ++s) qf[b][s] = load_frag(p + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+        position[b] = masks.start + i;
+        limit[b] = masks.end(a, position[b]);
+        document[b] = masks.document(a, position[b]);
+        slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + at.head * a.group + h] : 0.f;
+    }
+    // the keys that the workgroup needs, and up to which a tile needs no mask
+    const int last_row = min(first + 16 * QB * kAttnWaves, a.rows) - 1;
+    const int p0 = masks.start + a.query(first), p1 = masks.start + a.query(last_row);
+    int lo = 0, hi = masks.documents ? (p1 < 0 || p0 >= a.s ? 0 : masks.end(a, min(p1, a.s - 1))) : masks.end(a, p1);
+    const int free_keys = masks.documents ? 0 : masks.end(a, p0); // (positions rise with the rows)
+    if (masks.documents) narrow(masks.documents, p0, p1, a.s, red, lo, hi);
+    int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
+    begin = max(begin, at.part * a.per_split);
+    end = min(end, (at.part + 1) * a.per_split);
+    const int wave_row = min(own + 16 * QB, a.rows) - 1;
+    const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
+
+    f32x4 acc[2 * KD][QB];
+    float top[QB], total[QB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        top[b] = -INFINITY;
+        total[b] = 0.f;
+#pragma unroll
+        for (int d = 0; d < 2 * KD; ++d) acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
+    TL kt, vt;
+    int next_document = 0;
+    const auto fetch = [&](int tile_of) {
+        const int key = tile_of * kTileRows;
+        kt.load(hi - key, a.dim, [&](int i) { return ks + (key + i) * k.token; });
+        vt.load(hi - key, a.dim, [&](int i) { return vs + (key + i) * v.token; });
+        if (masks.documents && threadIdx.x < kTileRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
+    };
+    const auto stage = [&](int half) {
+        kt.store(lds + half * 2 * TL::kSize);
+        vt.store(lds + (half * 2 + 1) * TL::kSize);
+        if (masks.documents && threadIdx.x < kTileRows) key_documents[half][threadIdx.x] = next_document;
+    };
+    if (begin < end) {
+        fetch(begin);
+        stage(0);
+    }
+    __syncthreads();
+    int half = 0;
+    for (int n = begin; n < end; ++n) {
+        if (n + 1 < end) fetch(n + 1);
+        const int key = n * kTileRows;
+        if (key < wave_limit) {
+            const T *const kl = lds + half * 2 * TL::kSize, *const vl = kl + TL::kSize;
+            f32x4 s[4][QB];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int b = 0; b < QB; ++b) s[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < KD; ++c) {
+                    const Frag<T> f = TL::rows(kl, 16 * j, 32 * c);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) s[j][b] = mma(f, qf[b][c], s[j][b]);
+                }
+            }
+            if constexpr (MOD) {
+                if (a.cap > 0.f) {
+                    const float in = a.scale / a.cap, out = a.cap * kLog2e;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int b = 0; b < QB; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[j][b][e] = out * tanh_of<T>(s[j][b][e] * in);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int b = 0; b < QB; ++b) s[j][b] *= a.scale * kLog2e;
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int b = 0; b < QB; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[j][b][e] -= slope[b] * kLog2e * fabsf((float)(position[b] - (key + 16 * j + 4 * g + e)));
+                }
+            }
+            if (key + kTileRows > free_keys) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at_key = key + 16 * j + 4 * g + e;
+                        const int doc = masks.documents ? key_documents[half][16 * j + 4 * g + e] : 0;
+#pragma unroll
+                        for (int b = 0; b < QB; ++b)
+                            if (at_key >= limit[b] || doc != document[b]) s[j][b][e] = -INFINITY;
+                    }
+            }
+            Frag<T> p[2][QB];
+#pragma unroll
+            for (int b = 0; b < QB; ++b) {
+                float most = s[0][b][0];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, s[j][b][e]);
+                most = max_over_rows(most);
+                if (__any(most * mul > top[b] * mul + 8.f)) {
+                    const float next = fmaxf(top[b], most);
+                    const float factor = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top[b] - next) * mul);
+                    top[b] = next;
+                    total[b] *= factor;
+#pragma unroll
+                    for (int d = 0; d < 2 * KD; ++d) acc[d][b] *= factor;
+                }
+                const float base = top[b] == -INFINITY ? 0.f : kProbExponent<T> - top[b] * mul;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[j][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][b][e], mul, base));
+                        total[b] += s[j][b][e];
+                    }
+                p[0][b] = as_operand<T>(s[0][b], s[1][b]);
+                p[1][b] = as_operand<T>(s[2][b], s[3][b]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int d = 0; d < 2 * KD; ++d) {
+                    const Frag<T> f = TL::columns(vl, 32 * j, 16 * d);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, p[j][b], acc[d][b]);
+                }
+        }
+        half ^= 1;
+        if (n + 1 < end) stage(half);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = own + 16 * b + (lane & 15);
+        const float sum = sum_over_rows(total[b]);
+        if (r >= a.rows) continue;
+        const bool none = sum == 0.f;
+        const float inverse = none ? 0.f : 1.f / sum;
+        const float log = none ? -INFINITY : (top[b] * mul - kProbExponent<T> + __builtin_amdgcn_logf(sum)) * kLn2;
+        const int i = a.query(r), h = at.head * a.group + r - i * a.group;
+        const int64_t line = a.line(at.particle, at.batch, h, i), lines = (int64_t)a.n * a.batch * a.heads * a.t;
+        if (a.splits > 1) {
+            if (g == 0) partial_lse[at.part * lines + line] = log;
+            float *const out = partial + (at.part * lines + line) * (32 * KD);
+#pragma unroll
+            for (int d = 0; d < 2 * KD; ++d) *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[d][b] * inverse;
+        } else {
+            if (g == 0 && lse) lse[line] = log;
+            T *const out = o.at(at.particle, at.batch, h) + i * o.token;
+#pragma unroll
+            for (int d = 0; d < 2 * KD; ++d) {
+                const int c = 16 * d + 4 * g;
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : acc[d][b][e] * inverse;
+                if (c < a.dim) store_pack<T, 4>(out + c, a.dim - c, x);
+            }
+        }
+    }
+}
+
+// The parts' results, each weighted by its share of the sum of exponentials: a thread has four values of a row.
+template <class T> __global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a, int ld, const float *partial, const float *partial_lse, Heads<T> o, float *lse)
+{
+    const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t;
+    const int quads = ld / 4;
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, line = k / quads;
+    const int c = (int)(k - line * quads) * 4;
+    if (line >= lines || c >= a.dim) return;
+    float top = -INFINITY, total = 0.f;
+    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, partial_lse[p * lines + line]);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.splits; ++p) {
+        const float l = partial_lse[p * lines + line];
+        if (l == -INFINITY) continue;
+        const float w = __builtin_amdgcn_exp2f((l - top) * kLog2e);
+        total += w;
+        sum += w * *reinterpret_cast<const f32x4 *>(partial + (p * lines + line) * ld + c);
+    }
+    const bool none = total == 0.f;
+    const float inverse = none ? 0.f : 1.f / total;
+    const int i = (int)(line % a.t);
+    const int64_t head = line / a.t;
+    const int h = (int)(head % a.heads), b = (int)(head / a.heads % a.batch), particle = (int)(head / a.heads / a.batch);
+    const float x[4] = {sum[0] * inverse, sum[1] * inverse, sum[2] * inverse, sum[3] * inverse};
+    store_pack<T, 4>(o.at(particle, b, h) + i * o.token + c, a.dim - c, x);
+    if (c == 0 && lse) lse[line] = none ? -INFINITY : top + __builtin_amdgcn_logf(total) * kLn2;
+}
+
+} // namespace svgd

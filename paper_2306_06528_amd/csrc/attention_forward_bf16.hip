@@ -1,0 +1,3 @@
+// Attention, forward, activations of type bf16.
+#define SVGD_ATTENTION_TYPE svgd::bf16_t
+#include "attention_forward_instance.hpp"

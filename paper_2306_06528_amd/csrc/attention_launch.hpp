@@ -1,0 +1,69 @@
+// What a call of attention launches, by sizes alone.  The kernels' instances are compiled type by type (attention_*_<type>.hip).
+#pragma once
+#include "attention_common.hpp"
+
+namespace svgd {
+
+struct AttnCall {
+    AttnArgs a;
+    svgd_heads q, k, v, o, d_o, dq, dk, dv;
+    const float *lse, *delta;
+    float *lse_out, *partial, *partial_lse, *slope_rows;
+    hipStream_t stream;
+};
+
+template <class T> Heads<const T> in(const svgd_heads &h) { return {(const T *)h.data, h.particle_stride, h.batch_stride, h.token_stride, h.head_stride}; }
+template <class T> Heads<T> out(const svgd_heads &h) { return {(T *)h.data, h.particle_stride, h.batch_stride, h.token_stride, h.head_stride}; }
+
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 8; // (a launch has less than 2^32 threads)
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Blocks of 16 own rows (or keys) of a wave.
+inline int row_blocks(const AttnArgs &a) { return a.rows <= 64 ? 1 : 2; }
+inline int key_blocks(const AttnArgs &a) { return a.s <= 64 || a.dim > 64 ? 1 : 2; }
+
+// Tiles of `own` rows each of `size`, the streamed ones in `splits` parts; the workgroups' numbers.
+inline void set_grid(AttnArgs &a, int64_t size, int own, int splits)
+{
+    a.tiles = (int)ceil_div(size, own);
+    a.splits = splits;
+    a.per_split = (int)ceil_div(ceil_div(a.s, kTileRows), splits);
+    a.total = (int)((int64_t)a.n * a.batch * a.kv * a.tiles * splits);
+    a.per_die = (a.total + 7) / 8;
+}
+
+// Forward with few rows: the keys in parts.
+inline int forward_splits(const AttnArgs &a)
+{
+    const int64_t blocks = (int64_t)a.n * a.batch * a.kv * ceil_div(a.rows, 64 * row_blocks(a)), tiles = ceil_div(a.s, kTileRows);
+    if (blocks >= 512 || tiles < 8) return 1;
+    const int64_t most = tiles / 4, wanted = ceil_div(1024, blocks);
+    const int64_t splits = wanted < most ? wanted : most;
+    return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
+}
+inline int padded_dim(const AttnArgs &a) { return (a.dim + 31) / 32 * 32; }
+
+template <class F> int with_dim(int dim, F f)
+{
+    using std::integral_constant;
+    if (dim <= 32) return f(integral_constant<int, 1>{});
+    if (dim <= 64) return f(integral_constant<int, 2>{});
+    if (dim <= 96) return f(integral_constant<int, 3>{});
+    return f(integral_constant<int, 4>{});
+}
+template <class F> int with_two(int blocks, F f)
+{
+    using std::integral_constant;
+    return blocks == 1 ? f(integral_constant<int, 1>{}) : f(integral_constant<int, 2>{});
+}
+template <class F> int with_truth(bool b, F f) { return b ? f(std::true_type{}) : f(std::false_type{}); }
+
+inline bool modified_scores(const AttnArgs &a) { return a.cap > 0.f || a.slopes; }
+inline int launched_ok() { return hipGetLastError() == hipSuccess ? SVGD_OK : SVGD_ERR_DEVICE; }
+
+template <class T> int attention_forward(AttnCall &c);
+template <class T> int attention_queries(AttnCall &c);
+template <class T> int attention_keys(AttnCall &c);
+
+} // namespace svgd

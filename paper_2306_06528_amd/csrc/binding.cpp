@@ -257,7 +257,8 @@ PyObject *step_rows(PyObject *, PyObject *const *a, Py_ssize_t na)
 
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(step), METHOD(phi), METHOD(step_static), METHOD(step_rows), METHOD(layer_norm_forward), METHOD(layer_norm_backward),
-                         METHOD(gated_ffn_forward), METHOD(gated_ffn_backward), METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(gated_ffn_forward), METHOD(gated_ffn_backward), METHOD(dropout), METHOD(linear_forward), METHOD(linear_backward),
+                         METHOD(qk_norm_rotary_forward), METHOD(qk_norm_rotary_backward), METHOD(attention_forward), METHOD(attention_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

@@ -265,12 +265,12 @@ template <class TL, class T, int P> struct ColumnsOfB {
     static constexpr int kPairs = TL::kJ / 2, kAtATime = TL::kThreads / kPairs, N = (4 + kAtATime - 1) / kAtATime;
     static_assert(kAtATime >= 1, "a thread for every pair");
     const T *base;   // row 0
-    int64_t stride;  // of the buffers' rows, at most 2^20: a thread's offset fits 32 bits
+    int64_t stride;  // beyond kFarStride the slow way: a thread's offset is to fit 32 bits
     uint32_t column; // the first row of the thread's pair
     bool late, single, narrow;
     T v[N][2][8];
     __device__ __forceinline__ ColumnsOfB(const T *b, int64_t s, int64_t first, int64_t count)
-        : base(b), stride(s), single(count < 2), narrow(count < 2)
+        : base(b), stride(s), single(count < 2), narrow(count < 2 || s > kFarStride)
     {
         const int64_t j = first + row();
         late = j + 2 > count && !single;
@@ -338,8 +338,8 @@ template <int NJ> struct Acc {
     }
 };
 
-// Adds the product over the columns from begin (a multiple of kTileK) to end to acc.  Products of parts pa, pb with pa + pb beyond the last part are below 2^-24
-// (three parts; 2^-16 with two) of the whole and left out.  While the matrix cores work on a step, the next one's rows of B go to the
+// Adds the product over the columns from begin (a multiple of kTileK) to end to acc.  Products of parts pa, pb with pa + pb beyond the last of three are below 2^-24
+// of the whole and left out; of two fp16 operands all four are there.  While the matrix cores work on a step, the next one's rows of B go to the
 // other half of LDS and those of A are split into the registers of the last columns' blocks as these get free, and the rows of the
 // step after it are on their way: one barrier per step.
 // lds: 2 * PB * kPlane units; scratch: the wave's own kScratch floats.
@@ -348,7 +348,7 @@ template <class TL, int PA, int PB, class LA, class LB>
 __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_t K, Acc<TL::kBlocksJ> &acc, bf16x8 *lds, float *scratch)
 {
     if (begin >= K) return;
-    constexpr int kOrder = (PA > PB ? PA : PB) - 1, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
+    constexpr int kOrder = PA == 3 || PB == 3 ? 2 : PA + PB - 2, NJ = TL::kBlocksJ, kStage = PB * TL::kPlane;
     constexpr int kLast = NJ <= 2 ? 1 : NJ <= 4 ? 2 : PB == 3 ? 1 : 2; // columns that go block of A by block of A: as many as there are registers for
     // Whether a step's rows are fetched during the whole step before it, or while it goes on: the former where there are registers for it;
     // in large tiles not if A takes the detour through LDS (large bf16 block: hidden_grad_kernel 705 us, otherwise 727, but

@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kTeamBlock<L>) void norm_backward_kernel(NormShape 
 // Sums of a particle's partials, in the same order every time: 64 columns per workgroup, its sixteen waves take every
 // sixteenth partial, four of them in flight, and their sums are added in order.
 constexpr int kReduceWaves = 16;
-__global__ __launch_bounds__(64 * kReduceWaves) void norm_reduce_kernel(const float *partials, int blocks, int width, int column_groups, Params dweight,
+static __global__ __launch_bounds__(64 * kReduceWaves) void norm_reduce_kernel(const float *partials, int blocks, int width, int column_groups, Params dweight,
                                                                         Params dbias, bool accumulate)
 {
     __shared__ double sums[kReduceWaves][64];
