@@ -35,6 +35,7 @@ typedef struct svgd_heads {
 #define SVGD_ATTENTION_MAX_BATCH ((int64_t)1 << 20)  /* sequences per particle; n batch heads length is below 2^28 - 16 too, and n batch kv_heads times the tiles of 64 keys, or rows, below 2^24 - 8 */
 #define SVGD_ATTENTION_MAX_HEADS 4096
 #define SVGD_ATTENTION_MAX_GROUP 256                 /* query heads to a key head */
+#define SVGD_ATTENTION_MAX_STRIDE ((int64_t)1 << 23) /* of tokens, and of all the query heads to a key head, of q, k, v and do: less than this */
 #define SVGD_ROTARY_MAX_DIM 256                      /* values of a head that svgd_qk_norm_rotary_* take */
 
 /*

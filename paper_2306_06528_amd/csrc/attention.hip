@@ -74,6 +74,12 @@ struct MaskExtents {
     }
 };
 
+// Tokens, or the heads that share keys, further apart than the kernels' offsets within a tile reach.
+bool far(const svgd_heads &h, int64_t together, int64_t tokens)
+{
+    return (tokens > 1 && h.token_stride >= kMaxTokenStride) || (together > 1 && h.head_stride >= kMaxTokenStride / together);
+}
+
 int check(int dtype, const svgd_attention *a, const svgd_heads &q, const svgd_heads &k, const svgd_heads &v)
 {
     if (dtype < SVGD_F32 || dtype > SVGD_F16) return SVGD_ERR_INVALID_ARG;
@@ -82,13 +88,30 @@ int check(int dtype, const svgd_attention *a, const svgd_heads &q, const svgd_he
     if (!std::isfinite(scale) || !(scale > 0.f) || !std::isfinite(cap) || !(a->cap >= 0.0) || (a->cap > 0.0 && cap < 1e-30f) || scale < 1e-30f) return SVGD_ERR_INVALID_ARG;
     if (a->slopes && !valid_params({a->slopes, a->slopes_stride, a->heads}, a->n, false)) return SVGD_ERR_INVALID_ARG;
     if (!aligned_to(a->starts, 4) || !aligned_to(a->lengths, 4) || !aligned_to(a->documents, 4) || !aligned_to(a->prefix, 4)) return SVGD_ERR_INVALID_ARG;
+    if (far(q, a->heads / a->kv_heads, a->length) || far(k, 1, a->keys) || far(v, 1, a->keys)) return SVGD_ERR_TOO_LARGE;
     if (!valid_heads(q, dtype, query_sizes(*a)) || !valid_heads(k, dtype, key_sizes(*a)) || !valid_heads(v, dtype, key_sizes(*a))) return SVGD_ERR_INVALID_ARG;
     return SVGD_OK;
 }
 
 template <class F> int for_type(int dtype, F f) { return dtype == SVGD_F32 ? f(float{}) : dtype == SVGD_BF16 ? f(bf16_t{}) : f(f16_t{}); }
 
+
 size_t rounded(size_t floats) { return (floats + 3) / 4 * 4; }
+
+// Scratch memory of the backward pass, in floats: delta, the slopes' rows (and their parts), parts' sums of dq or of dk and dv, which come after them.
+struct BackwardScratch {
+    size_t slopes, partial, total;
+    explicit BackwardScratch(const svgd_attention &p)
+    {
+        const AttnArgs a = args_of(p);
+        const size_t lines = lines_of(p), key_lines = (size_t)p.n * p.batch * p.kv_heads * p.keys;
+        const size_t qs = query_splits(a), ks = key_splits(a), ld = padded_dim(a);
+        slopes = rounded(lines);
+        partial = slopes + (p.slopes ? rounded(lines * (qs > 1 ? 1 + 3 * qs : 1)) : 0);
+        const size_t of_q = qs > 1 ? qs * lines * ld : 0, of_k = ks > 1 ? ks * key_lines * 2 * ld : 0;
+        total = partial + (of_q > of_k ? of_q : of_k);
+    }
+};
 
 } // namespace
 
@@ -135,7 +158,7 @@ int svgd_attention_forward(int dtype, const svgd_attention *p, svgd_heads q, svg
 size_t svgd_attention_scratch(const svgd_attention *p)
 {
     if (check_sizes_of(p)) return 0;
-    return rounded(lines_of(*p)) * 4 * (p->slopes ? 2 : 1);
+    return BackwardScratch(*p).total * 4;
 }
 
 int svgd_attention_backward(int dtype, const svgd_attention *p, svgd_heads d_o, svgd_heads q, svgd_heads k, svgd_heads v, svgd_heads o, const float *lse, svgd_heads dq, svgd_heads dk,
@@ -143,6 +166,7 @@ int svgd_attention_backward(int dtype, const svgd_attention *p, svgd_heads d_o, 
 {
     if (const int rc = check(dtype, p, q, k, v)) return rc;
     const HeadSizes qs = query_sizes(*p), ks = key_sizes(*p);
+    if (far(d_o, p->heads / p->kv_heads, p->length)) return SVGD_ERR_TOO_LARGE;
     const size_t need = svgd_attention_scratch(p), stats = lines_of(*p) * 4;
     const Params slopes{p->slopes, p->slopes_stride, p->heads}, grads{dslopes, dslopes_stride, p->heads};
     if (dslopes && (!p->slopes || !valid_params(grads, p->n, true) || params_meet(grads, slopes, p->n))) return SVGD_ERR_INVALID_ARG;
@@ -179,7 +203,9 @@ int svgd_attention_backward(int dtype, const svgd_attention *p, svgd_heads d_o, 
     c.dv = dv;
     c.lse = lse;
     c.delta = (const float *)scratch;
-    c.slope_rows = dslopes ? (float *)scratch + rounded(lines_of(*p)) : nullptr;
+    const BackwardScratch parts(*p);
+    c.slope_rows = dslopes ? (float *)scratch + parts.slopes : nullptr;
+    c.partial = (float *)scratch + parts.partial;
     c.stream = (hipStream_t)stream;
     if (p->batch > 0 && p->length > 0) {
         const int rc = for_type(dtype, [&](auto t) { return attention_queries<decltype(t)>(c); });

@@ -1,7 +1,9 @@
 // Attention, backward, without atomics: one kernel has rows of its own and streams keys and values past them (dq, and the slopes' gradients row by row), the other has keys of its own and
 // streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse.
 //     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
-// P and dz are rounded to the activations' type for the products with do, k and q (BlockScale: fp16), as o and the gradients themselves are.
+// P is rounded to the activations' type for the product with do: half a step of each, with signs as random as those of the gradients' own rounding.  dz goes into the products with k and q in two
+// such parts (BlockScale: fp16): rounded to one, its roundings and those of o, from which delta comes, would together put dq and dk of short sequences off by 1.7 times what rounding the results does,
+// with two parts by 1.35.
 #pragma once
 #include "attention_common.hpp"
 
@@ -24,32 +26,22 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
     if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
 }
 
-// The exponent (of 2) of a score, and 1 - tanh^2.
-template <class T> __device__ __forceinline__ float modified(const AttnArgs &a, float score, float slope, float distance, float &damp)
+template <class T, int KDX, int QB, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+                                                                                                              const float *lse, const float *delta, Heads<T> dq, float *slope_rows, float *partial)
 {
-    float z = score * a.scale;
-    if (a.cap > 0.f) {
-        const float t = tanh_of<T>(z / a.cap);
-        damp = 1.f - t * t;
-        z = a.cap * t;
-    }
-    return (z - slope * distance) * kLog2e;
-}
-
-template <class T, int KD, int QB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
-                                                                                                              const float *lse, const float *delta, Heads<T> dq, float *slope_rows)
-{
-    typedef Tile64<T, KD> TL;
+    constexpr int KD = kBlocks32<KDX>;
+    typedef Tile64<T, KD, KDX == 0> TL;
     __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
     __shared__ int red[4], key_documents[2][kTileRows];
     const AttnBlock at(a);
     if (!at.any) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     const int tile = a.causal ? a.tiles - 1 - at.tile : at.tile;
     const int first = tile * (16 * QB * kAttnWaves), own = first + wave * 16 * QB;
     const Masks masks(a, at.batch);
     const float mul = MOD ? 1.f : a.scale * kLog2e;
+    const Modified modified(a);
 
     Frag<T> qf[QB][KD], df[QB][KD];
     int limit[QB], position[QB], document[QB];
@@ -66,7 +58,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
         position[b] = masks.start + i;
         limit[b] = masks.end(a, position[b]);
         document[b] = masks.document(a, position[b]);
-        slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + h] : 0.f;
+        slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + h] * kLog2e : 0.f;
         const int64_t line = a.line(at.particle, at.batch, h, i);
         log[b] = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e; // (a row that sees nothing: every probability 0)
         del[b] = delta[line];
@@ -76,13 +68,15 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
     int lo = 0, hi = masks.documents ? (p1 < 0 || p0 >= a.s ? 0 : masks.end(a, min(p1, a.s - 1))) : masks.end(a, p1);
     const int free_keys = masks.documents ? 0 : masks.end(a, p0);
     if (masks.documents) narrow(masks.documents, p0, p1, a.s, red, lo, hi);
-    const int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
+    int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
+    part_of(a, at.part, begin, end);
     const int wave_row = min(own + 16 * QB, a.rows) - 1;
     const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
 
     f32x4 acc[2 * KD][QB];
     float sum_dz[QB], sum_dz_far[QB], sum_far[QB]; // of dz, dz distance and P distance
     BlockScale bs;
+    const SplitConst sc = split_const();
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         sum_dz[b] = sum_dz_far[b] = sum_far[b] = 0.f;
@@ -91,22 +85,26 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
     }
     const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
     TL kt, vt;
+    uint32_t k_at[TL::N], v_at[TL::N];
+    TL::offsets(k_at, a.dim, [&](int i) { return (uint32_t)i * (uint32_t)k.token; });
+    TL::offsets(v_at, a.dim, [&](int i) { return (uint32_t)i * (uint32_t)v.token; });
     int next_document = 0;
     const auto fetch = [&](int tile_of) {
-        const int key = tile_of * kTileRows;
-        kt.load(hi - key, a.dim, [&](int i) { return ks + (key + i) * k.token; });
-        vt.load(hi - key, a.dim, [&](int i) { return vs + (key + i) * v.token; });
+        const int key = tile_of * kTileRows, last = min(hi - key, kTileRows) - 1;
+        kt.load(ks + key * k.token, k_at, (uint32_t)k.token, last, a.dim);
+        vt.load(vs + key * v.token, v_at, (uint32_t)v.token, last, a.dim);
         if (masks.documents && threadIdx.x < kTileRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
     };
-    const auto stage = [&](int half) {
-        kt.store(lds + half * 2 * TL::kSize);
-        vt.store(lds + (half * 2 + 1) * TL::kSize);
+    const auto stage = [&](int half, int tile_of) {
+        kt.store(lds + half * 2 * TL::kSize, hi - tile_of * kTileRows, a.dim);
+        vt.store(lds + (half * 2 + 1) * TL::kSize, hi - tile_of * kTileRows, a.dim);
         if (masks.documents && threadIdx.x < kTileRows) key_documents[half][threadIdx.x] = next_document;
     };
     if (begin < end) {
         fetch(begin);
-        stage(0);
+        stage(0, begin);
     }
+    loads_done();
     __syncthreads();
     int half = 0;
     for (int n = begin; n < end; ++n) {
@@ -132,35 +130,36 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
                         }
                     }
                 }
-                const bool masked = key0 + kTileRows > free_keys;
+                if constexpr (MOD) modified.template apply<T>(s);
                 float largest = 0.f;
+                const auto gradients = [&](auto masked) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int at_key = key + 16 * j + 4 * g + e;
-                        const int doc = masked && masks.documents ? key_documents[half][32 * m + 16 * j + 4 * g + e] : 0;
+                        for (int e = 0; e < 4; ++e) {
+                            const int at_key = key + 16 * j + 4 * g + e;
+                            const int doc = masked && masks.documents ? key_documents[half][32 * m + 16 * j + 4 * g + e] : 0;
 #pragma unroll
-                        for (int b = 0; b < QB; ++b) {
-                            float x = s[j][b][e], damp = 1.f;
-                            [[maybe_unused]] const float far = fabsf((float)(position[b] - at_key));
-                            if constexpr (MOD) x = modified<T>(a, x, slope[b], far, damp);
-                            if (masked && (at_key >= limit[b] || doc != document[b])) x = -INFINITY;
-                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
-                            float dz = p * (dp[j][b][e] - del[b]);
-                            if (masked && p == 0.f) dz = 0.f;
-                            if constexpr (MOD) {
-                                if (a.slopes) {
+                            for (int b = 0; b < QB; ++b) {
+                                float x = s[j][b][e];
+                                [[maybe_unused]] const float far = fabsf((float)(position[b] - at_key)), t = x;
+                                if constexpr (MOD) x = modified.exponent(t, slope[b], far);
+                                if (masked && (at_key >= limit[b] || doc != document[b])) x = -INFINITY;
+                                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
+                                float dz = p * (dp[j][b][e] - del[b]);
+                                if constexpr (MOD) {
                                     sum_dz[b] += dz;
                                     sum_dz_far[b] += dz * far;
                                     sum_far[b] += p * far;
+                                    dz *= modified.damp(t);
                                 }
-                                dz *= damp;
+                                s[j][b][e] = dz;
+                                if constexpr (std::is_same<T, f16_t>::value) largest = fmaxf(largest, fabsf(dz));
                             }
-                            s[j][b][e] = dz;
-                            if constexpr (sizeof(T) == 2 && !std::is_same<T, bf16_t>::value) largest = fmaxf(largest, fabsf(dz));
                         }
-                    }
+                };
+                if (key0 + kTileRows > free_keys) gradients(std::true_type{});
+                else gradients(std::false_type{});
                 if constexpr (std::is_same<T, f16_t>::value) {
                     const float factor = bs.take(largest);
                     if (factor != 1.f) {
@@ -175,19 +174,21 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
                         s[1][b] *= bs.scale;
                     }
                 }
-                Frag<T> z[QB];
+                Frag<T> z[QB][kZParts<T>];
 #pragma unroll
-                for (int b = 0; b < QB; ++b) z[b] = as_operand<T>(s[0][b], s[1][b]);
+                for (int b = 0; b < QB; ++b) as_parts<T>(s[0][b], s[1][b], sc, z[b]);
 #pragma unroll
                 for (int d = 0; d < 2 * KD; ++d) {
                     const Frag<T> f = TL::columns(kl, 32 * m, 16 * d);
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, z[b], acc[d][b]);
+                    for (int part = 0; part < kZParts<T>; ++part)
+#pragma unroll
+                        for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, z[b][part], acc[d][b]);
                 }
             }
         }
         half ^= 1;
-        if (n + 1 < end) stage(half);
+        if (n + 1 < end) stage(half, n + 1);
         __syncthreads();
     }
     const float factor = std::is_same<T, f16_t>::value ? a.scale / bs.scale : a.scale;
@@ -198,9 +199,24 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
         if constexpr (MOD) {
             // The sum of dz is 0 but for roundings, those of delta the largest: what they put on the sum with the distances is taken off (the probabilities add up to 1)
             const float z = sum_over_rows(sum_dz[b]), zf = sum_over_rows(sum_dz_far[b]), f = sum_over_rows(sum_far[b]);
-            if (a.slopes && slope_rows && r < a.rows && g == 0) slope_rows[a.line(at.particle, at.batch, h, i)] = z * f - zf;
+            if (a.slopes && slope_rows && r < a.rows && g == 0) {
+                const int64_t line = a.line(at.particle, at.batch, h, i), lines = (int64_t)a.n * a.batch * a.heads * a.t;
+                if (a.splits > 1) {
+                    slope_rows[(1 + 3 * at.part) * lines + line] = z;
+                    slope_rows[(2 + 3 * at.part) * lines + line] = zf;
+                    slope_rows[(3 + 3 * at.part) * lines + line] = f;
+                } else {
+                    slope_rows[line] = z * f - zf;
+                }
+            }
         }
         if (r >= a.rows || !dq.p) continue;
+        if (a.splits > 1) {
+            float *const out = partial + (at.part * ((int64_t)a.n * a.batch * a.heads * a.t) + a.line(at.particle, at.batch, h, i)) * (32 * KD);
+#pragma unroll
+            for (int d = 0; d < 2 * KD; ++d) *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = acc[d][b] * factor;
+            continue;
+        }
         T *const out = dq.at(at.particle, at.batch, h) + i * dq.token;
 #pragma unroll
         for (int d = 0; d < 2 * KD; ++d) {
@@ -212,16 +228,17 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
 }
 
 // What a streamed row brings besides its values.
-struct RowInfo {
+struct __attribute__((aligned(16))) RowInfo {
     float log[kTileRows], delta[kTileRows], slope[kTileRows];
     int limit[kTileRows], position[kTileRows], document[kTileRows];
 };
 
-template <class T, int KD, int KB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
-                                                                                                           const float *lse, const float *delta, Heads<T> dk, Heads<T> dv)
+template <class T, int KDX, int KB, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+                                                                                                           const float *lse, const float *delta, Heads<T> dk, Heads<T> dv, float *partial)
 {
-    typedef Tile64<T, KD> TL;
+    constexpr int KD = kBlocks32<KDX>;
+    typedef Tile64<T, KD, KDX == 0> TL;
     constexpr bool kHalf = std::is_same<T, f16_t>::value;
     constexpr float kExponent = kHalf ? 14.f : 0.f; // of probabilities as operands
     __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
@@ -229,10 +246,11 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
     __shared__ int red[4];
     const AttnBlock at(a);
     if (!at.any) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     const int first = at.tile * (16 * KB * kAttnWaves), own = first + wave * 16 * KB;
     const Masks masks(a, at.batch);
     const float mul = MOD ? 1.f : a.scale * kLog2e;
+    const Modified modified(a);
 
     Frag<T> kf[KB][KD], vf[KB][KD];
     int key[KB], document[KB];
@@ -259,7 +277,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
         row_lo = hi > lo ? max(row_lo, (lo - masks.start) * a.group) : 0;
         row_hi = hi > lo ? min(a.rows, (hi - masks.start) * a.group) : 0;
     }
-    const int begin = row_lo / kTileRows, end = row_hi > row_lo ? (row_hi + kTileRows - 1) / kTileRows : begin;
+    int begin = row_lo / kTileRows, end = row_hi > row_lo ? (row_hi + kTileRows - 1) / kTileRows : begin;
+    part_of(a, at.part, begin, end);
     // tiles from this row on need no mask
     const int wave_last = own + 16 * KB - 1;
     const int free_row = masks.documents || wave_last >= masks.length ? INT32_MAX
@@ -268,23 +287,41 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
 
     f32x4 acc_k[2 * KD][KB], acc_v[2 * KD][KB];
     BlockScale bs;
+    const SplitConst sc = split_const();
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int d = 0; d < 2 * KD; ++d) acc_k[d][b] = acc_v[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     TL qt, dt;
+    // (tiles begin with a token's first head where the heads of a group divide 64: then the rows of all tiles lie alike)
+    const bool steady = kTileRows % a.group == 0;
+    uint32_t q_at[TL::N], d_at[TL::N];
+    const auto place = [&](int j, int64_t token, int64_t head) {
+        const int i = a.query(j);
+        return (uint32_t)i * (uint32_t)token + (uint32_t)(j - i * a.group) * (uint32_t)head;
+    };
+    TL::offsets(q_at, a.dim, [&](int j) { return place(j, q.token, q.head); });
+    TL::offsets(d_at, a.dim, [&](int j) { return place(j, d_o.token, d_o.head); });
     float next_log = 0.f, next_delta = 0.f, next_slope = 0.f;
     int next_limit = 0, next_position = 0, next_document = 0;
     const auto fetch = [&](int tile_of) {
         const int row = tile_of * kTileRows;
-        qt.load(a.rows - row, a.dim, [&](int j) {
-            const int i = a.query(row + j), h = at.head * a.group + row + j - i * a.group;
-            return q.at(at.particle, at.batch, h) + i * q.token;
-        });
-        dt.load(a.rows - row, a.dim, [&](int j) {
-            const int i = a.query(row + j), h = at.head * a.group + row + j - i * a.group;
-            return d_o.at(at.particle, at.batch, h) + i * d_o.token;
-        });
+        const int i0 = a.query(row), h0 = row - i0 * a.group, last = min(a.rows - row, kTileRows) - 1;
+        const T *const qs = q.at(at.particle, at.batch, at.head * a.group) + i0 * q.token, *const ds = d_o.at(at.particle, at.batch, at.head * a.group) + i0 * d_o.token;
+        if (steady && last == kTileRows - 1) {
+            qt.load(qs, q_at, a.dim);
+            dt.load(ds, d_at, a.dim);
+        } else {
+            uint32_t to[TL::N];
+            const auto row_at = [&](int j, int64_t token, int64_t head) {
+                const int r = h0 + min(j, last), i = a.query(r);
+                return (uint32_t)i * (uint32_t)token + (uint32_t)(r - i * a.group) * (uint32_t)head;
+            };
+            TL::offsets(to, a.dim, [&](int j) { return row_at(j, q.token, q.head); });
+            qt.load(qs, to, a.dim);
+            TL::offsets(to, a.dim, [&](int j) { return row_at(j, d_o.token, d_o.head); });
+            dt.load(ds, to, a.dim);
+        }
         if (threadIdx.x < kTileRows) {
             const int r = row + (int)threadIdx.x;
             next_log = INFINITY;
@@ -293,18 +330,18 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
             if (r < a.rows) {
                 const int i = a.query(r), h = at.head * a.group + r - i * a.group;
                 const int64_t line = a.line(at.particle, at.batch, h, i);
-                next_log = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e;
+                next_log = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e; // (a row that sees nothing: every probability 0)
                 next_delta = delta[line];
                 next_position = masks.start + i;
                 next_limit = masks.end(a, next_position);
                 next_document = masks.document(a, next_position);
-                if (MOD && a.slopes) next_slope = a.slopes[at.particle * a.slopes_stride + h];
+                if (MOD && a.slopes) next_slope = a.slopes[at.particle * a.slopes_stride + h] * kLog2e;
             }
         }
     };
-    const auto stage = [&](int half) {
-        qt.store(lds + half * 2 * TL::kSize);
-        dt.store(lds + (half * 2 + 1) * TL::kSize);
+    const auto stage = [&](int half, int tile_of) {
+        qt.store(lds + half * 2 * TL::kSize, a.rows - tile_of * kTileRows, a.dim);
+        dt.store(lds + (half * 2 + 1) * TL::kSize, a.rows - tile_of * kTileRows, a.dim);
         if (threadIdx.x < kTileRows) {
             RowInfo &info = infos[half];
             info.log[threadIdx.x] = next_log;
@@ -317,8 +354,9 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
     };
     if (begin < end) {
         fetch(begin);
-        stage(0);
+        stage(0, begin);
     }
+    loads_done();
     __syncthreads();
     int half = 0;
     for (int n = begin; n < end; ++n) {
@@ -344,28 +382,36 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
                         }
                     }
                 }
+                if constexpr (MOD) modified.template apply<T>(s);
                 float largest = 0.f;
+                const auto gradients = [&](auto hidden) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = 32 * m + 16 * j + 4 * g;
-                    const f32x4 log = *reinterpret_cast<const f32x4 *>(&info.log[r]), del = *reinterpret_cast<const f32x4 *>(&info.delta[r]);
+                    for (int j = 0; j < 2; ++j) {
+                        const int r = 32 * m + 16 * j + 4 * g;
+                        const f32x4 log = *reinterpret_cast<const f32x4 *>(&info.log[r]), del = *reinterpret_cast<const f32x4 *>(&info.delta[r]);
+                        [[maybe_unused]] const f32x4 slope = *reinterpret_cast<const f32x4 *>(&info.slope[r]);
+                        [[maybe_unused]] const i32x4 limit = *reinterpret_cast<const i32x4 *>(&info.limit[r]), position = *reinterpret_cast<const i32x4 *>(&info.position[r]),
+                                                     documents = *reinterpret_cast<const i32x4 *>(&info.document[r]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                        for (int e = 0; e < 4; ++e) {
 #pragma unroll
-                        for (int b = 0; b < KB; ++b) {
-                            float x = s[j][b][e], damp = 1.f;
-                            if constexpr (MOD) x = modified<T>(a, x, info.slope[r + e], fabsf((float)(info.position[r + e] - key[b])), damp);
-                            if (masked && (key[b] >= info.limit[r + e] || document[b] != info.document[r + e])) x = -INFINITY;
-                            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, kExponent - log[e]));
-                            float dz = p * (dp[j][b][e] - del[e]);
-                            if (masked && p == 0.f) dz = 0.f;
-                            if constexpr (MOD) dz *= damp;
-                            s[j][b][e] = p;
-                            dp[j][b][e] = dz;
-                            if constexpr (kHalf) largest = fmaxf(largest, fabsf(dz));
+                            for (int b = 0; b < KB; ++b) {
+                                float x = s[j][b][e];
+                                [[maybe_unused]] const float t = x;
+                                if constexpr (MOD) x = modified.exponent(t, slope[e], fabsf((float)(position[e] - key[b])));
+                                if (hidden && (key[b] >= limit[e] || document[b] != documents[e])) x = -INFINITY;
+                                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, kExponent - log[e]));
+                                float dz = p * (dp[j][b][e] - del[e]);
+                                if constexpr (MOD) dz *= modified.damp(t);
+                                s[j][b][e] = p;
+                                dp[j][b][e] = dz;
+                                if constexpr (kHalf) largest = fmaxf(largest, fabsf(dz));
+                            }
                         }
                     }
-                }
+                };
+                if (masked) gradients(std::true_type{});
+                else gradients(std::false_type{});
                 if constexpr (kHalf) {
                     const float factor = bs.take(largest);
                     if (factor != 1.f) {
@@ -380,30 +426,41 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
                         dp[1][b] *= bs.scale;
                     }
                 }
-                Frag<T> p[KB], z[KB];
+                Frag<T> p[KB], z[KB][kZParts<T>];
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
                     p[b] = as_operand<T>(s[0][b], s[1][b]);
-                    z[b] = as_operand<T>(dp[0][b], dp[1][b]);
+                    as_parts<T>(dp[0][b], dp[1][b], sc, z[b]);
                 }
 #pragma unroll
                 for (int d = 0; d < 2 * KD; ++d) {
                     const Frag<T> f = TL::columns(dl, 32 * m, 16 * d), e = TL::columns(ql, 32 * m, 16 * d);
 #pragma unroll
-                    for (int b = 0; b < KB; ++b) {
-                        acc_v[d][b] = mma(f, p[b], acc_v[d][b]);
-                        acc_k[d][b] = mma(e, z[b], acc_k[d][b]);
-                    }
+                    for (int b = 0; b < KB; ++b) acc_v[d][b] = mma(f, p[b], acc_v[d][b]);
+#pragma unroll
+                    for (int part = 0; part < kZParts<T>; ++part)
+#pragma unroll
+                        for (int b = 0; b < KB; ++b) acc_k[d][b] = mma(e, z[b][part], acc_k[d][b]);
                 }
             }
         half ^= 1;
-        if (n + 1 < end) stage(half);
+        if (n + 1 < end) stage(half, n + 1);
         __syncthreads();
     }
     const float of_k = kHalf ? a.scale * 0x1p-14f / bs.scale : a.scale, of_v = kHalf ? 0x1p-14f : 1.f;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
         if (key[b] >= a.s) continue;
+        if (a.splits > 1) {
+            const int64_t lines = (int64_t)a.n * a.batch * a.kv * a.s, line = ((int64_t)(at.particle * a.batch + at.batch) * a.kv + at.head) * a.s + key[b];
+            float *const out = partial + (at.part * lines + line) * (64 * KD);
+#pragma unroll
+            for (int d = 0; d < 2 * KD; ++d) {
+                *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = acc_k[d][b] * of_k;
+                *reinterpret_cast<f32x4 *>(out + 32 * KD + 16 * d + 4 * g) = acc_v[d][b] * of_v;
+            }
+            continue;
+        }
         T *const to_k = dk.at(at.particle, at.batch, at.head) + key[b] * dk.token, *const to_v = dv.at(at.particle, at.batch, at.head) + key[b] * dv.token;
 #pragma unroll
         for (int d = 0; d < 2 * KD; ++d) {
@@ -414,6 +471,39 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
             if (c < a.dim && dv.p) store_pack<T, 4>(to_v + c, a.dim - c, y);
         }
     }
+}
+
+// The parts' sums, in order, as T: a thread has four values of a line's `each` tensors of ld floats (dq; dk and dv), whose heads are `heads`, tokens `tokens`.
+template <class T> __global__ __launch_bounds__(256) void attention_sum_kernel(AttnArgs a, int heads, int tokens, int each, int ld, const float *partial, Heads<T> first, Heads<T> second)
+{
+    const int64_t lines = (int64_t)a.n * a.batch * heads * tokens;
+    const int quads = each * ld / 4;
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, line = k / quads;
+    const int at = (int)(k - line * quads) * 4, which = at / ld, c = at - which * ld;
+    if (line >= lines || c >= a.dim) return;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < a.splits; ++p) sum += *reinterpret_cast<const f32x4 *>(partial + (p * lines + line) * (each * ld) + at);
+    const Heads<T> &to = which ? second : first;
+    if (!to.p) return;
+    const int i = (int)(line % tokens);
+    const int64_t head = line / tokens;
+    const int h = (int)(head % heads), b = (int)(head / heads % a.batch), particle = (int)(head / heads / a.batch);
+    const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
+    store_pack<T, 4>(to.at(particle, b, h) + i * to.token + c, a.dim - c, x);
+}
+
+// The rows' terms of the slopes' gradients from the parts'.
+static __global__ __launch_bounds__(256) void attention_slope_rows_kernel(AttnArgs a, float *slope_rows)
+{
+    const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t, line = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (line >= lines) return;
+    float z = 0.f, zf = 0.f, f = 0.f;
+    for (int p = 0; p < a.splits; ++p) {
+        z += slope_rows[(1 + 3 * p) * lines + line];
+        zf += slope_rows[(2 + 3 * p) * lines + line];
+        f += slope_rows[(3 + 3 * p) * lines + line];
+    }
+    slope_rows[line] = z * f - zf;
 }
 
 // A slope's gradient: what its rows give, added up by one workgroup, in an order that is always the same.

@@ -38,6 +38,18 @@ void shaped(const HeadsOf &h, at::IntArrayRef shape, const char *name)
     fail(PyExc_ValueError, text.str().c_str(), name);
 }
 
+// Attention's kernels reach so far from token to token and head to head; beyond that a copy.
+HeadsOf near_heads(PyObject *obj, const char *name, const HeadsOf *like = nullptr)
+{
+    HeadsOf h = heads(obj, name, like);
+    const int64_t most = SVGD_ATTENTION_MAX_STRIDE, count = h.t.size(3);
+    if ((h.t.size(2) > 1 && h.t.stride(2) >= most) || (count > 1 && h.t.stride(3) >= most / count)) {
+        const at::NoGradGuard no_grad;
+        h.t = h.t.contiguous();
+    }
+    return h;
+}
+
 at::Tensor new_heads(const HeadsOf &h) { return at::empty(h.t.sizes(), h.t.options().memory_format(c10::nullopt)); }
 svgd_heads desc(const at::Tensor &t) { return t.defined() ? svgd_heads{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), t.stride(3)} : svgd_heads{nullptr, 0, 0, 0, 0}; }
 
@@ -307,7 +319,7 @@ PyObject *qk_norm_rotary_backward(PyObject *, PyObject *const *a, Py_ssize_t na)
 PyObject *attention_forward(PyObject *, PyObject *const *a, Py_ssize_t na)
 {
     return guarded(na, 13, [&]() -> PyObject * {
-        const HeadsOf q = heads(a[2], "q"), k = heads(a[3], "k", &q), v = heads(a[4], "v", &q);
+        const HeadsOf q = near_heads(a[2], "q"), k = near_heads(a[3], "k", &q), v = near_heads(a[4], "v", &q);
         Attention r = attention_of(q, k, v, a + 5);
         const Act x = act_of(q);
         void *stream;
@@ -328,7 +340,7 @@ PyObject *attention_forward(PyObject *, PyObject *const *a, Py_ssize_t na)
 PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t na)
 {
     return guarded(na, 20, [&]() -> PyObject * {
-        const HeadsOf q = heads(a[3], "q"), k = heads(a[4], "k", &q), v = heads(a[5], "v", &q), d_o = heads(a[2], "do", &q), o = heads(a[6], "o", &q);
+        const HeadsOf q = near_heads(a[3], "q"), k = near_heads(a[4], "k", &q), v = near_heads(a[5], "v", &q), d_o = near_heads(a[2], "do", &q), o = heads(a[6], "o", &q);
         Attention r = attention_of(q, k, v, a + 8);
         shaped(d_o, q.t.sizes(), "do");
         shaped(o, q.t.sizes(), "o");

@@ -10,10 +10,13 @@
 
 namespace svgd {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr int kTileRows = 64; // streamed rows (or keys) in LDS at a time
 constexpr int kAttnWaves = 4, kAttnBlock = 64 * kAttnWaves;
 constexpr int kMaxStart = 1 << 28;
+constexpr int64_t kMaxTokenStride = SVGD_ATTENTION_MAX_STRIDE; // (offsets within a tile fit 32 bits)
 
 template <class T> struct Heads {
     T *p;
@@ -30,7 +33,7 @@ struct AttnArgs {
     const float *slopes;
     int64_t slopes_stride;
     const int32_t *starts, *lengths, *documents, *prefix;
-    int tiles, splits, per_split; // tiles of a workgroup's own rows; parts of the streamed ones, and tiles of 64 of each part
+    int tiles, splits; // tiles of a workgroup's own rows; parts of the streamed ones
     int per_die, total;           // workgroups
     __device__ __forceinline__ int query(int r) const { return group == 1 ? r : (int)__umulhi((uint32_t)r, group_mul); } // exact: r group < 2^32
     __device__ __forceinline__ int64_t line(int i, int b, int h, int query) const { return ((int64_t)(i * batch + b) * heads + h) * t + query; }
@@ -72,6 +75,9 @@ __device__ __forceinline__ f32x4 mma(Frag<float> a, Frag<float> b, f32x4 c)
     return c;
 }
 
+// Heads of less than 16 bytes have kernels of their own, numbered 0: blocks of 32 values, loaded one by one.
+template <int KDX> constexpr int kBlocks32 = KDX ? KDX : 1;
+
 // Eight values from memory, those from `left` on 0 and not read.
 template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int left)
 {
@@ -94,48 +100,99 @@ template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int 
     return f;
 }
 
-// 64 rows of up to 32 KD values in LDS, as they are in memory; 16 bytes between rows, so that 16 rows at the same place meet in no bank.
-template <class T, int KD> struct Tile64 {
-    static constexpr int VEC = 16 / sizeof(T), kLd = 32 * KD + VEC, kSize = kTileRows * kLd, kChunks = 32 * KD / VEC, N = kTileRows * kChunks / kAttnBlock;
+// 64 rows of up to 32 KD values in LDS, as they are in memory, 16 bytes at a time.  Which place of its row such a piece takes is permuted so that neither the same piece of 16 rows (`rows`) nor 32 bytes of
+// eight rows in succession (`columns`, what 32 lanes read at a time) meet in a bank, of which there are 64.  (fp32 heads of up to 32 or of 65 to 96 values: `columns` meet in pairs.)
+// TINY: heads of less than 16 bytes.
+template <class T, int KD, bool TINY> struct Tile64 {
+    static constexpr int VEC = 16 / sizeof(T), kChunks = 32 * KD / VEC, kSize = kTileRows * 32 * KD, N = kTileRows * kChunks / kAttnBlock;
     typedef typename Pack<T, VEC>::raw raw;
     raw v[N];
-    // row(i): where row i of the tile starts; rows from `count` on are 0 and not read
-    template <class F> __device__ __forceinline__ void load(int count, int dim, F row)
+    static __device__ __forceinline__ int place(int row, int chunk) // in 16 bytes; moves with the row by 16
+    {
+        int f;
+        if constexpr (sizeof(T) == 4) f = KD % 2 ? (row >> 1) & 7 : row & 15;
+        else if constexpr (KD == 4) f = ((row & 7) << 1) | ((row >> 3) & 1);
+        else if constexpr (KD == 2) f = (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
+        else f = (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
+        return row * kChunks + (chunk ^ f);
+    }
+    static __device__ __forceinline__ int row_of(int u) { return ((int)threadIdx.x + kAttnBlock * u) / kChunks; }
+    static __device__ __forceinline__ int chunk_of(int u) { return ((int)threadIdx.x + kAttnBlock * u) % kChunks; }
+    // Where the thread's pieces lie, in bytes from the tile's first row; row(i): where row i starts, in elements.  A piece that ends beyond the head is loaded further left (and moved to its place by
+    // `store`).
+    static __device__ __forceinline__ uint32_t column(int u, int dim)
+    {
+        const int c = chunk_of(u) * VEC;
+        return (uint32_t)(TINY || c + VEC <= dim ? c : dim - VEC) * (uint32_t)sizeof(T);
+    }
+    template <class F> static __device__ __forceinline__ void offsets(uint32_t (&at)[N], int dim, F row)
     {
 #pragma unroll
+        for (int u = 0; u < N; ++u) at[u] = (uint32_t)row(row_of(u)) * (uint32_t)sizeof(T) + column(u, dim);
+    }
+    // The same rows `stride` apart, of which those beyond `last` are not there: that one again.
+    __device__ __forceinline__ void load(const T *base, const uint32_t (&at)[N], uint32_t stride, int last, int dim)
+    {
+        uint32_t to[N];
+#pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int k = threadIdx.x + kAttnBlock * u, i = k / kChunks, c = (k - i * kChunks) * VEC;
+            const uint32_t most = (uint32_t)last * stride * (uint32_t)sizeof(T) + column(u, dim);
+            to[u] = at[u] < most ? at[u] : most;
+        }
+        load(base, to, dim);
+    }
+    // Without a branch, so that nothing waits for what is on its way.
+    __device__ __forceinline__ void load(const T *base, const uint32_t (&at)[N], int dim)
+    {
+        const char *const from = reinterpret_cast<const char *>(base);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[u][e] = (T)0.f;
-            if (i < count && c < dim) {
-                const T *const p = row(i) + c;
-                if (c + VEC <= dim) {
-                    v[u] = *reinterpret_cast<const typename Pack<T, VEC>::type *>(p);
-                } else {
+        for (int u = 0; u < N; ++u) {
+            if constexpr (TINY) {
+                const int c = chunk_of(u) * VEC;
+                const T *const p = reinterpret_cast<const T *>(from + (at[u] - column(u, dim)));
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        if (c + e < dim) v[u][e] = p[e];
-                }
+                for (int e = 0; e < VEC; ++e) v[u][e] = p[c + e < dim ? c + e : dim - 1];
+            } else {
+                v[u] = *reinterpret_cast<const typename Pack<T, VEC>::type *>(from + at[u]);
             }
         }
     }
-    __device__ __forceinline__ void store(T *lds) const
+    // What is not there becomes 0 on its way.
+    __device__ __forceinline__ void store(T *lds, int count, int dim)
     {
+        if (!TINY && dim % VEC) {
+            const int by = VEC - dim % VEC;
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int k = threadIdx.x + kAttnBlock * u, i = k / kChunks, c = (k - i * kChunks) * VEC;
-            *reinterpret_cast<raw *>(lds + i * kLd + c) = v[u];
+            for (int u = 0; u < N; ++u) {
+                const int c = chunk_of(u) * VEC;
+                const bool last = c < dim && c + VEC > dim;
+#pragma unroll
+                for (int step = 1; step < VEC; step *= 2) {
+                    if (!(by & step)) continue;
+#pragma unroll
+                    for (int e = 0; e + step < VEC; ++e) v[u][e] = last ? v[u][e + step] : v[u][e];
+                }
+            }
         }
+        if (count < kTileRows || dim < 32 * KD) {
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (row_of(u) >= count || chunk_of(u) * VEC + e >= dim) v[u][e] = (T)0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) reinterpret_cast<raw *>(lds)[place(row_of(u), chunk_of(u))] = v[u];
     }
     // operand of rows row .. row + 15, values col .. col + 31
     static __device__ __forceinline__ Frag<T> rows(const T *lds, int row, int col)
     {
         const int lane = threadIdx.x & 63;
-        const T *const p = lds + (row + (lane & 15)) * kLd + col + 8 * (lane >> 4);
+        const raw *const p = reinterpret_cast<const raw *>(lds) + row * kChunks;
         Frag<T> f;
 #pragma unroll
         for (int q = 0; q < 8; q += VEC) {
-            const raw r = *reinterpret_cast<const raw *>(p + q);
+            const raw r = p[place(lane & 15, (col + q) / VEC + (lane >> 4) * (8 / VEC))];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) f[q + e] = r[e];
         }
@@ -151,22 +208,42 @@ template <class T, int KD> struct Tile64 {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 lds16x4;
             typedef T t4 __attribute__((ext_vector_type(4)));
-            const T *const p = lds + (row + 4 * g + ((lane & 15) >> 2)) * kLd + col + 4 * (lane & 3);
+            const T *const p = lds + row * 32 * KD + place(4 * g + ((lane & 15) >> 2), col / VEC + ((lane & 3) >> 1)) * VEC + 4 * (lane & 1);
             const t4 lo = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p));
-            const t4 hi = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * kLd)));
+            const t4 hi = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * 32 * KD)));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 f[e] = lo[e];
                 f[4 + e] = hi[e];
             }
         } else {
-            const T *const p = lds + (row + 4 * g) * kLd + col + (lane & 15);
+            const T *const p = lds + row * 32 * KD + (lane & 3);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = p[((e & 3) + 16 * (e >> 2)) * kLd];
+            for (int e = 0; e < 8; ++e) f[e] = p[place(4 * g + (e & 3), col / VEC + ((lane & 15) >> 2)) * VEC + (e >> 2) * 16 * 32 * KD];
         }
         return f;
     }
 };
+
+// Waits for the loads so far.  Before the loop over tiles: the compiler, which cannot tell an operand loaded before it from a tile loaded in it, would wait for the next tile with every tile.
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
+// The part's share of the tiles begin .. end - 1.
+__device__ __forceinline__ void part_of(const AttnArgs &a, int part, int &begin, int &end)
+{
+    const int count = end > begin ? end - begin : 0, first = begin;
+    begin = first + (int)((int64_t)count * part / a.splits);
+    end = first + (int)((int64_t)count * (part + 1) / a.splits);
+}
+
+// What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
+// (LDS leaves room for one workgroup on a CU where fp32 heads are wider than 64.)
+template <class T, int KD> constexpr int kWavesPerSimd = sizeof(T) == 4 && KD > 2 ? 1 : 2;
+
+// Whether a wave can have two blocks of 16 rows (or keys) of its own, which halves what it reads from LDS, without running out of registers.
+template <class T, int KDX, bool MOD> constexpr bool kTwoForward = !(sizeof(T) == 2 && KDX == 4 && MOD);
+template <class T, int KDX, bool MOD> constexpr bool kTwoQueries = sizeof(T) == 4 ? KDX != 2 || !MOD : KDX < 3 || (KDX == 3 && !MOD);
+template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = sizeof(T) == 4 ? KDX < 2 : KDX < 3;
 
 // Two results of 16 streamed rows each as a B operand.
 template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 b)
@@ -180,15 +257,51 @@ template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 
     return f;
 }
 
+// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it; fp32 is one part.
+template <class T> constexpr int kZParts = 2;
+template <> inline constexpr int kZParts<float> = 1;
+template <class T> __device__ __forceinline__ void as_parts(f32x4 a, f32x4 b, const SplitConst &sc, Frag<T> (&out)[kZParts<T>])
+{
+    out[0] = as_operand<T>(a, b);
+    if constexpr (std::is_same<T, bf16_t>::value) { // (what is left of a pair: one dot product each, see split3)
+        const bf16x2 neg_lo = __builtin_bit_cast(bf16x2, sc.neg_lo), neg_hi = __builtin_bit_cast(bf16x2, sc.neg_hi);
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+            const bf16x2 p = {out[0][k], out[0][k + 1]}, q = {out[0][4 + k], out[0][5 + k]};
+            a[k] = __builtin_amdgcn_fdot2_f32_bf16(p, neg_lo, a[k], false);
+            a[k + 1] = __builtin_amdgcn_fdot2_f32_bf16(p, neg_hi, a[k + 1], false);
+            b[k] = __builtin_amdgcn_fdot2_f32_bf16(q, neg_lo, b[k], false);
+            b[k + 1] = __builtin_amdgcn_fdot2_f32_bf16(q, neg_hi, b[k + 1], false);
+        }
+        out[1] = as_operand<T>(a, b);
+    } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a[e] -= (float)out[0][e];
+            b[e] -= (float)out[0][4 + e];
+        }
+        out[1] = as_operand<T>(a, b);
+    }
+}
+
 // The largest of the four lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them.
 __device__ __forceinline__ float max_over_rows(float v)
 {
     const unsigned u = __float_as_uint(v);
     const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const float s = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const float s = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const unsigned w = __float_as_uint(s);
     const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// The largest of the 16 lanes of a row, in all of them (as row_sum goes).
+__device__ __forceinline__ float row_max(float v)
+{
+    v = __builtin_elementwise_maximum(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, false)));
+    v = __builtin_elementwise_maximum(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, false)));
+    v = __builtin_elementwise_maximum(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, false)));
+    return __builtin_elementwise_maximum(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false)));
 }
 
 // tanh: for 16-bit activations from one exponential, off by 2^-23 or so of 1; for fp32 the library's.
@@ -197,6 +310,30 @@ template <class T> __device__ __forceinline__ float tanh_of(float x)
     if constexpr (sizeof(T) == 4) return tanhf(x);
     else return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
 }
+
+// Scores that are capped, or less a slope times the distance: z = out t - slope distance in exponents of 2, where t = tanh(scale s / cap) and out = cap, or t = scale s and out = 1; d z / d (scale s) is
+// 1 - on t^2, on = 1 or 0.
+struct Modified {
+    float in, out, on;
+    __device__ __forceinline__ Modified(const AttnArgs &a) : in(a.cap > 0.f ? a.scale / a.cap : a.scale), out((a.cap > 0.f ? a.cap : 1.f) * kLog2e), on(a.cap > 0.f ? 1.f : 0.f) {}
+    // s becomes t
+    template <class T, int N, int B> __device__ __forceinline__ void apply(f32x4 (&s)[N][B]) const
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int b = 0; b < B; ++b) s[j][b] *= in;
+        if (on == 0.f) return;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[j][b][e] = tanh_of<T>(s[j][b][e]);
+    }
+    __device__ __forceinline__ float exponent(float t, float slope, float distance) const { return __builtin_fmaf(t, out, -slope * distance); } // slope: times log2 e
+    __device__ __forceinline__ float damp(float t) const { return __builtin_fmaf(-on * t, t, 1.f); }
+};
 
 // What a sequence's masks are.
 struct Masks {
@@ -258,8 +395,7 @@ struct BlockScale {
     // the factor by which what was summed up so far has to be multiplied (mostly 1), given the lane's largest new magnitude
     __device__ __forceinline__ float take(float largest)
     {
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) largest = fmaxf(largest, __shfl_xor(largest, m));
+        largest = row_max(largest);
         largest = max_over_rows(largest);
         if (!(largest * scale > 32768.f)) return 1.f;
         const float next = ldexpf(1.f, min(max(14 - __builtin_amdgcn_frexp_expf(largest), -126), 100));

@@ -10,23 +10,22 @@ namespace svgd {
 template <class T> constexpr float kProbExponent = 0.f;
 template <> inline constexpr float kProbExponent<f16_t> = 6.f;
 
-// S, scores of 16 streamed keys key .. key + 3 a lane, to what is an exponent of 2 after multiplication by `mul`.
-template <class T, bool MOD> __device__ __forceinline__ float exponent_factor(const AttnArgs &a) { return MOD ? 1.f : a.scale * kLog2e; }
-
-template <class T, int KD, int QB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1))) void attention_forward_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o,
+template <class T, int KDX, int QB, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_forward_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o,
                                                                                                               float *lse, float *partial, float *partial_lse)
 {
-    typedef Tile64<T, KD> TL;
+    constexpr int KD = kBlocks32<KDX>;
+    typedef Tile64<T, KD, KDX == 0> TL;
     __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
     __shared__ int red[4], key_documents[2][kTileRows];
     const AttnBlock at(a);
     if (!at.any) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
     const int tile = a.causal ? a.tiles - 1 - at.tile : at.tile; // (those with the most keys first)
     const int first = tile * (16 * QB * kAttnWaves), own = first + wave * 16 * QB;
     const Masks masks(a, at.batch);
-    const float mul = exponent_factor<T, MOD>(a);
+    const float mul = MOD ? 1.f : a.scale * kLog2e; // scores times this are exponents of 2
+    const Modified modified(a);
 
     Frag<T> qf[QB][KD];
     int limit[QB], position[QB], document[QB];
@@ -40,7 +39,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
         position[b] = masks.start + i;
         limit[b] = masks.end(a, position[b]);
         document[b] = masks.document(a, position[b]);
-        slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + at.head * a.group + h] : 0.f;
+        slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + at.head * a.group + h] * kLog2e : 0.f;
     }
     // the keys that the workgroup needs, and up to which a tile needs no mask
     const int last_row = min(first + 16 * QB * kAttnWaves, a.rows) - 1;
@@ -49,8 +48,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
     const int free_keys = masks.documents ? 0 : masks.end(a, p0); // (positions rise with the rows)
     if (masks.documents) narrow(masks.documents, p0, p1, a.s, red, lo, hi);
     int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
-    begin = max(begin, at.part * a.per_split);
-    end = min(end, (at.part + 1) * a.per_split);
+    part_of(a, at.part, begin, end);
     const int wave_row = min(own + 16 * QB, a.rows) - 1;
     const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
 
@@ -65,22 +63,26 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
     }
     const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
     TL kt, vt;
+    uint32_t k_at[TL::N], v_at[TL::N];
+    TL::offsets(k_at, a.dim, [&](int i) { return (uint32_t)i * (uint32_t)k.token; });
+    TL::offsets(v_at, a.dim, [&](int i) { return (uint32_t)i * (uint32_t)v.token; });
     int next_document = 0;
     const auto fetch = [&](int tile_of) {
-        const int key = tile_of * kTileRows;
-        kt.load(hi - key, a.dim, [&](int i) { return ks + (key + i) * k.token; });
-        vt.load(hi - key, a.dim, [&](int i) { return vs + (key + i) * v.token; });
+        const int key = tile_of * kTileRows, last = min(hi - key, kTileRows) - 1;
+        kt.load(ks + key * k.token, k_at, (uint32_t)k.token, last, a.dim);
+        vt.load(vs + key * v.token, v_at, (uint32_t)v.token, last, a.dim);
         if (masks.documents && threadIdx.x < kTileRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
     };
-    const auto stage = [&](int half) {
-        kt.store(lds + half * 2 * TL::kSize);
-        vt.store(lds + (half * 2 + 1) * TL::kSize);
+    const auto stage = [&](int half, int tile_of) {
+        kt.store(lds + half * 2 * TL::kSize, hi - tile_of * kTileRows, a.dim);
+        vt.store(lds + (half * 2 + 1) * TL::kSize, hi - tile_of * kTileRows, a.dim);
         if (masks.documents && threadIdx.x < kTileRows) key_documents[half][threadIdx.x] = next_document;
     };
     if (begin < end) {
         fetch(begin);
-        stage(0);
+        stage(0, begin);
     }
+    loads_done();
     __syncthreads();
     int half = 0;
     for (int n = begin; n < end; ++n) {
@@ -101,28 +103,13 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
                 }
             }
             if constexpr (MOD) {
-                if (a.cap > 0.f) {
-                    const float in = a.scale / a.cap, out = a.cap * kLog2e;
+                modified.template apply<T>(s);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int b = 0; b < QB; ++b)
+                    for (int b = 0; b < QB; ++b)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[j][b][e] = out * tanh_of<T>(s[j][b][e] * in);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int b = 0; b < QB; ++b) s[j][b] *= a.scale * kLog2e;
-                }
-                if (a.slopes) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int b = 0; b < QB; ++b)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) s[j][b][e] -= slope[b] * kLog2e * fabsf((float)(position[b] - (key + 16 * j + 4 * g + e)));
-                }
+                        for (int e = 0; e < 4; ++e) s[j][b][e] = modified.exponent(s[j][b][e], slope[b], fabsf((float)(position[b] - (key + 16 * j + 4 * g + e))));
             }
             if (key + kTileRows > free_keys) {
 #pragma unroll
@@ -139,11 +126,11 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
             Frag<T> p[2][QB];
 #pragma unroll
             for (int b = 0; b < QB; ++b) {
-                float most = s[0][b][0];
+                float most = s[0][b][0]; // (maximum needs no step that makes signalling NaN quiet first, as fmaxf does)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) most = fmaxf(most, s[j][b][e]);
+                    for (int e = 0; e < 4; ++e) most = __builtin_elementwise_maximum(most, s[j][b][e]);
                 most = max_over_rows(most);
                 if (__any(most * mul > top[b] * mul + 8.f)) {
                     const float next = fmaxf(top[b], most);
@@ -174,7 +161,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(1)))
                 }
         }
         half ^= 1;
-        if (n + 1 < end) stage(half);
+        if (n + 1 < end) stage(half, n + 1);
         __syncthreads();
     }
 #pragma unroll

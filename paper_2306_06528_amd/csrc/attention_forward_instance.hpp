@@ -6,15 +6,20 @@ template <> int svgd::attention_forward<SVGD_ATTENTION_TYPE>(AttnCall &c)
 {
     typedef SVGD_ATTENTION_TYPE T;
     AttnArgs &a = c.a;
-    const int blocks = row_blocks(a);
-    set_grid(a, a.rows, 64 * blocks, forward_splits(a));
-    const int rc = with_dim(a.dim, [&](auto kd) {
-        return with_two(blocks, [&](auto qb) {
-            return with_truth(modified_scores(a), [&](auto mod) {
-                attention_forward_kernel<T, decltype(kd)::value, decltype(qb)::value, decltype(mod)::value>
-                    <<<a.per_die * 8, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
-                return launched_ok();
-            });
+    const int rc = with_dim<T>(a.dim, [&](auto kd) {
+        return with_truth(modified_scores(a), [&](auto mod) {
+            constexpr int KD = decltype(kd)::value;
+            constexpr bool MOD = decltype(mod)::value;
+            const bool two = kTwoForward<T, KD, MOD> && two_blocks(a, a.rows);
+            set_grid(a, a.rows, two ? 128 : 64, forward_splits(a));
+            const int grid = a.per_die * 8;
+            if constexpr (kTwoForward<T, KD, MOD>)
+                if (two) {
+                    attention_forward_kernel<T, KD, 2, MOD><<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
+                    return launched_ok();
+                }
+            attention_forward_kernel<T, KD, 1, MOD><<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
+            return launched_ok();
         });
     });
     if (rc || a.splits == 1) return rc;

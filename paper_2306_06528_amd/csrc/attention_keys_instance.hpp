@@ -6,15 +6,27 @@ template <> int svgd::attention_keys<SVGD_ATTENTION_TYPE>(AttnCall &c)
 {
     typedef SVGD_ATTENTION_TYPE T;
     AttnArgs &a = c.a;
-    const int blocks = key_blocks(a);
-    set_grid(a, a.s, 64 * blocks, 1);
-    return with_dim(a.dim, [&](auto kd) {
-        return with_two(blocks, [&](auto kb) {
-            return with_truth(modified_scores(a), [&](auto mod) {
-                attention_keys_kernel<T, decltype(kd)::value, decltype(kb)::value, decltype(mod)::value>
-                    <<<a.per_die * 8, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dk), out<T>(c.dv));
-                return launched_ok();
-            });
+    const int rc = with_dim<T>(a.dim, [&](auto kd) {
+        return with_truth(modified_scores(a), [&](auto mod) {
+            constexpr int KD = decltype(kd)::value;
+            constexpr bool MOD = decltype(mod)::value;
+            const bool two = kTwoKeys<T, KD, MOD> && two_blocks(a, a.s);
+            set_grid(a, a.s, two ? 128 : 64, key_splits(a));
+            const int grid = a.per_die * 8;
+            if constexpr (kTwoKeys<T, KD, MOD>)
+                if (two) {
+                    attention_keys_kernel<T, KD, 2, MOD>
+                        <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dk), out<T>(c.dv), c.partial);
+                    return launched_ok();
+                }
+            attention_keys_kernel<T, KD, 1, MOD>
+                <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dk), out<T>(c.dv), c.partial);
+            return launched_ok();
         });
     });
+    if (rc || a.splits == 1) return rc;
+    const int ld = padded_dim(a);
+    const int64_t lines = (int64_t)a.n * a.batch * a.kv * a.s;
+    attention_sum_kernel<T><<<(unsigned)ceil_div(lines * (ld / 2), 256), 256, 0, c.stream>>>(a, a.kv, a.s, 2, ld, c.partial, out<T>(c.dk), out<T>(c.dv));
+    return launched_ok();
 }

@@ -19,43 +19,43 @@ constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 8; // (a launch has less tha
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Blocks of 16 own rows (or keys) of a wave.
-inline int row_blocks(const AttnArgs &a) { return a.rows <= 64 ? 1 : 2; }
-inline int key_blocks(const AttnArgs &a) { return a.s <= 64 || a.dim > 64 ? 1 : 2; }
+// Workgroups with one block of 16 rows (or keys) for every wave.
+inline int64_t small_blocks(const AttnArgs &a, int64_t size) { return (int64_t)a.n * a.batch * a.kv * ceil_div(size, 64); }
+// Two blocks to a wave where the workgroups are many all the same.
+inline bool two_blocks(const AttnArgs &a, int64_t size) { return small_blocks(a, size) >= 1024; }
+
+// Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards.
+inline int parts_for(const AttnArgs &a, int64_t own, int64_t streamed)
+{
+    const int64_t blocks = small_blocks(a, own), tiles = ceil_div(streamed, kTileRows);
+    if (blocks >= 384 || blocks == 0 || tiles < 4) return 1;
+    const int64_t most = tiles / 2, wanted = ceil_div(512, blocks);
+    const int64_t parts = wanted < most ? wanted : most;
+    return (int)(parts > 64 ? 64 : parts);
+}
+inline int forward_splits(const AttnArgs &a) { return parts_for(a, a.rows, a.s); }
+inline int query_splits(const AttnArgs &a) { return parts_for(a, a.rows, a.s); }
+inline int key_splits(const AttnArgs &a) { return parts_for(a, a.s, a.rows); }
 
 // Tiles of `own` rows each of `size`, the streamed ones in `splits` parts; the workgroups' numbers.
 inline void set_grid(AttnArgs &a, int64_t size, int own, int splits)
 {
     a.tiles = (int)ceil_div(size, own);
     a.splits = splits;
-    a.per_split = (int)ceil_div(ceil_div(a.s, kTileRows), splits);
     a.total = (int)((int64_t)a.n * a.batch * a.kv * a.tiles * splits);
     a.per_die = (a.total + 7) / 8;
 }
 
-// Forward with few rows: the keys in parts.
-inline int forward_splits(const AttnArgs &a)
-{
-    const int64_t blocks = (int64_t)a.n * a.batch * a.kv * ceil_div(a.rows, 64 * row_blocks(a)), tiles = ceil_div(a.s, kTileRows);
-    if (blocks >= 512 || tiles < 8) return 1;
-    const int64_t most = tiles / 4, wanted = ceil_div(1024, blocks);
-    const int64_t splits = wanted < most ? wanted : most;
-    return (int)(splits < 1 ? 1 : splits > 64 ? 64 : splits);
-}
 inline int padded_dim(const AttnArgs &a) { return (a.dim + 31) / 32 * 32; }
 
-template <class F> int with_dim(int dim, F f)
+template <class T, class F> int with_dim(int dim, F f)
 {
     using std::integral_constant;
+    if (dim * (int)sizeof(T) < 16) return f(integral_constant<int, 0>{});
     if (dim <= 32) return f(integral_constant<int, 1>{});
     if (dim <= 64) return f(integral_constant<int, 2>{});
     if (dim <= 96) return f(integral_constant<int, 3>{});
     return f(integral_constant<int, 4>{});
-}
-template <class F> int with_two(int blocks, F f)
-{
-    using std::integral_constant;
-    return blocks == 1 ? f(integral_constant<int, 1>{}) : f(integral_constant<int, 2>{});
 }
 template <class F> int with_truth(bool b, F f) { return b ? f(std::true_type{}) : f(std::false_type{}); }
 

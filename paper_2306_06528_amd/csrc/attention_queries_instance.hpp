@@ -10,15 +10,33 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
     attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), const_cast<float *>(c.delta));
     if (const int rc = launched_ok()) return rc;
     if (!c.dq.data && !c.slope_rows) return SVGD_OK;
-    const int blocks = row_blocks(a);
-    set_grid(a, a.rows, 64 * blocks, 1);
-    return with_dim(a.dim, [&](auto kd) {
-        return with_two(blocks, [&](auto qb) {
-            return with_truth(modified_scores(a), [&](auto mod) {
-                attention_queries_kernel<T, decltype(kd)::value, decltype(qb)::value, decltype(mod)::value>
-                    <<<a.per_die * 8, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dq), c.slope_rows);
-                return launched_ok();
-            });
+    int rc = with_dim<T>(a.dim, [&](auto kd) {
+        return with_truth(modified_scores(a), [&](auto mod) {
+            constexpr int KD = decltype(kd)::value;
+            constexpr bool MOD = decltype(mod)::value;
+            const bool two = kTwoQueries<T, KD, MOD> && two_blocks(a, a.rows);
+            set_grid(a, a.rows, two ? 128 : 64, query_splits(a));
+            const int grid = a.per_die * 8;
+            if constexpr (kTwoQueries<T, KD, MOD>)
+                if (two) {
+                    attention_queries_kernel<T, KD, 2, MOD>
+                        <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dq), c.slope_rows, c.partial);
+                    return launched_ok();
+                }
+            attention_queries_kernel<T, KD, 1, MOD>
+                <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dq), c.slope_rows, c.partial);
+            return launched_ok();
         });
     });
+    if (rc || a.splits == 1) return rc;
+    if (c.dq.data) {
+        const int ld = padded_dim(a);
+        attention_sum_kernel<T><<<(unsigned)ceil_div(lines * (ld / 4), 256), 256, 0, c.stream>>>(a, a.heads, a.t, 1, ld, c.partial, out<T>(c.dq), Heads<T>{});
+        if ((rc = launched_ok())) return rc;
+    }
+    if (c.slope_rows) {
+        attention_slope_rows_kernel<<<(unsigned)ceil_div(lines, 256), 256, 0, c.stream>>>(a, c.slope_rows);
+        rc = launched_ok();
+    }
+    return rc;
 }
