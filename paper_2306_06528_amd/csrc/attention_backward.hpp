@@ -9,7 +9,7 @@
 
 namespace svgd {
 
-// delta of every row: 16 lanes each.
+// delta of every row, 16 lanes each, where the kernel that has queries of its own, which makes it otherwise, is not wanted.
 template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel(AttnArgs a, Heads<const T> o, Heads<const T> d_o, float *delta)
 {
     const int64_t k = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), lines = (int64_t)a.n * a.batch * a.t * a.heads;
@@ -28,7 +28,7 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
 
 template <class T, int KDX, int QB, bool MOD>
 __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
-                                                                                                              const float *lse, const float *delta, Heads<T> dq, float *slope_rows, float *partial)
+                                                                                                              Heads<const T> o, const float *lse, float *delta, Heads<T> dq, float *slope_rows, float *partial)
 {
     constexpr int KD = kBlocks32<KDX>;
     typedef Tile64<T, KD, KDX == 0> TL;
@@ -61,7 +61,16 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         slope[b] = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + h] * kLog2e : 0.f;
         const int64_t line = a.line(at.particle, at.batch, h, i);
         log[b] = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e; // (a row that sees nothing: every probability 0)
-        del[b] = delta[line];
+        const T *const op = o.at(at.particle, at.batch, h) + i * o.token;
+        del[b] = 0.f;
+#pragma unroll
+        for (int s = 0; s < KD; ++s) {
+            const Frag<T> f = load_frag(op + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) del[b] += (float)f[e] * (float)df[b][s][e];
+        }
+        del[b] = sum_over_rows(del[b]);
+        if (g == 0 && at.part == 0 && own + 16 * b + (lane & 15) < a.rows) delta[line] = del[b];
     }
     const int last_row = min(first + 16 * QB * kAttnWaves, a.rows) - 1;
     const int p0 = masks.start + a.query(first), p1 = masks.start + a.query(last_row);

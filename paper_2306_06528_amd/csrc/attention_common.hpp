@@ -39,22 +39,27 @@ struct AttnArgs {
     __device__ __forceinline__ int64_t line(int i, int b, int h, int query) const { return ((int64_t)(i * batch + b) * heads + h) * t + query; }
 };
 
-// Which particle, sequence, key head, tile and part a workgroup has.  Workgroups go round the eight dies in turn; a die gets tiles that follow one another, which share keys in its L2.
+// Which particle, sequence, key head, tile and part a workgroup has.  Workgroups go round the eight dies in turn; a die gets ones that follow one another.  Four heads, whose keys meet in its L2, take turns
+// tile by tile, so that of causal ones the longest of four heads come first and the shortest last: head after head the last head's longest would be left over at the end.
 struct AttnBlock {
+    static constexpr int kHeads = 4;
     int particle, batch, head, tile, part;
     bool any;
     __device__ __forceinline__ AttnBlock(const AttnArgs &a)
     {
-        int id = (int)(blockIdx.x & 7) * a.per_die + (int)(blockIdx.x >> 3);
+        const int id = (int)(blockIdx.x & 7) * a.per_die + (int)(blockIdx.x >> 3);
         any = id < a.total;
-        part = id % a.splits;
-        id /= a.splits;
-        tile = id % a.tiles;
-        id /= a.tiles;
-        head = id % a.kv;
-        id /= a.kv;
-        batch = id % a.batch;
-        particle = id / a.batch;
+        const int each = a.tiles * a.splits, heads = a.n * a.batch * a.kv;
+        const int four = id / (kHeads * each), left = id - four * (kHeads * each);
+        const int of = min(kHeads, heads - four * kHeads); // (the last heads may be fewer; beyond the last one it does not matter)
+        const int turn = left / max(of, 1);
+        int h = four * kHeads + left - turn * of;
+        tile = turn / a.splits;
+        part = turn - tile * a.splits;
+        head = h % a.kv;
+        h /= a.kv;
+        batch = h % a.batch;
+        particle = h / a.batch;
     }
 };
 
@@ -242,7 +247,6 @@ template <class T, int KD> constexpr int kWavesPerSimd = sizeof(T) == 4 && KD > 
 
 // Whether a wave can have two blocks of 16 rows (or keys) of its own, which halves what it reads from LDS, without running out of registers.
 template <class T, int KDX, bool MOD> constexpr bool kTwoForward = !(sizeof(T) == 2 && KDX == 4 && MOD);
-template <class T, int KDX, bool MOD> constexpr bool kTwoQueries = sizeof(T) == 4 ? KDX != 2 || !MOD : KDX < 3 || (KDX == 3 && !MOD);
 template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = sizeof(T) == 4 ? KDX < 2 : KDX < 3;
 
 // Two results of 16 streamed rows each as a B operand.

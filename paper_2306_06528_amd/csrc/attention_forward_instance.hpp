@@ -10,8 +10,8 @@ template <> int svgd::attention_forward<SVGD_ATTENTION_TYPE>(AttnCall &c)
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
-            const bool two = kTwoForward<T, KD, MOD> && two_blocks(a, a.rows);
-            set_grid(a, a.rows, two ? 128 : 64, forward_splits(a));
+            const bool two = kTwoForward<T, KD, MOD> && small_blocks(a, a.rows) >= kManyForward;
+            set_grid(a, a.rows, 16 * kAttnWaves * (two ? 2 : 1), forward_splits(a));
             const int grid = a.per_die * 8;
             if constexpr (kTwoForward<T, KD, MOD>)
                 if (two) {

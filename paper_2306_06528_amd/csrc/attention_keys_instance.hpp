@@ -10,8 +10,8 @@ template <> int svgd::attention_keys<SVGD_ATTENTION_TYPE>(AttnCall &c)
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
-            const bool two = kTwoKeys<T, KD, MOD> && two_blocks(a, a.s);
-            set_grid(a, a.s, two ? 128 : 64, key_splits(a));
+            const bool two = kTwoKeys<T, KD, MOD> && small_blocks(a, a.s) >= kManyKeys;
+            set_grid(a, a.s, 16 * kAttnWaves * (two ? 2 : 1), key_splits(a));
             const int grid = a.per_die * 8;
             if constexpr (kTwoKeys<T, KD, MOD>)
                 if (two) {

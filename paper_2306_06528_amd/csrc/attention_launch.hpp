@@ -20,9 +20,10 @@ constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 8; // (a launch has less tha
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Workgroups with one block of 16 rows (or keys) for every wave.
-inline int64_t small_blocks(const AttnArgs &a, int64_t size) { return (int64_t)a.n * a.batch * a.kv * ceil_div(size, 64); }
-// Two blocks to a wave where the workgroups are many all the same.
-inline bool two_blocks(const AttnArgs &a, int64_t size) { return small_blocks(a, size) >= 1024; }
+inline int64_t small_blocks(const AttnArgs &a, int64_t size) { return (int64_t)a.n * a.batch * a.kv * ceil_div(size, 16 * kAttnWaves); }
+// Two blocks to a wave where the workgroups are many all the same.  us with one and with two, 8 x 8 x 197 x 6 heads of 64 bf16 (1,536 small workgroups) and 4 x 2 x 4,096 x 16 heads of 64 causal (8,192): forward
+// 21 / 18 and 457 / 392, keys 34.7 / 40 and 999 / 915; with queries of their own, which two blocks cost more registers, 27.9 / 30.3 and 671 / 684, so always one.
+constexpr int64_t kManyForward = 1024, kManyKeys = 4096;
 
 // Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards.
 inline int parts_for(const AttnArgs &a, int64_t own, int64_t streamed)

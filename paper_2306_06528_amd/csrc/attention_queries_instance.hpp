@@ -7,24 +7,19 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
     typedef SVGD_ATTENTION_TYPE T;
     AttnArgs &a = c.a;
     const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t;
-    attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), const_cast<float *>(c.delta));
-    if (const int rc = launched_ok()) return rc;
-    if (!c.dq.data && !c.slope_rows) return SVGD_OK;
+    float *const delta = const_cast<float *>(c.delta);
+    if (!c.dq.data && !c.slope_rows) {
+        attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), delta);
+        return launched_ok();
+    }
     int rc = with_dim<T>(a.dim, [&](auto kd) {
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
-            const bool two = kTwoQueries<T, KD, MOD> && two_blocks(a, a.rows);
-            set_grid(a, a.rows, two ? 128 : 64, query_splits(a));
+            set_grid(a, a.rows, 16 * kAttnWaves, query_splits(a));
             const int grid = a.per_die * 8;
-            if constexpr (kTwoQueries<T, KD, MOD>)
-                if (two) {
-                    attention_queries_kernel<T, KD, 2, MOD>
-                        <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dq), c.slope_rows, c.partial);
-                    return launched_ok();
-                }
             attention_queries_kernel<T, KD, 1, MOD>
-                <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dq), c.slope_rows, c.partial);
+                <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), in<T>(c.o), c.lse, delta, out<T>(c.dq), c.slope_rows, c.partial);
             return launched_ok();
         });
     });
