@@ -491,7 +491,15 @@ template <class T> __global__ __launch_bounds__(256) void attention_sum_kernel(A
     const int at = (int)(k - line * quads) * 4, which = at / ld, c = at - which * ld;
     if (line >= lines || c >= a.dim) return;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < a.splits; ++p) sum += *reinterpret_cast<const f32x4 *>(partial + (p * lines + line) * (each * ld) + at);
+    constexpr int U = 8; // on their way together
+    for (int p0 = 0; p0 < a.splits; p0 += U) {
+        f32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const f32x4 *>(partial + (min(p0 + u, a.splits - 1) * lines + line) * (each * ld) + at);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p0 + u < a.splits) sum += x[u];
+    }
     const Heads<T> &to = which ? second : first;
     if (!to.p) return;
     const int i = (int)(line % tokens);

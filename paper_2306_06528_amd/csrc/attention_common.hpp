@@ -105,11 +105,12 @@ template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int 
     return f;
 }
 
-// 64 rows of up to 32 KD values in LDS, as they are in memory, 16 bytes at a time.  Which place of its row such a piece takes is permuted so that neither the same piece of 16 rows (`rows`) nor 32 bytes of
+// Rows of up to 32 KD values in LDS, as they are in memory, 16 bytes at a time.  Which place of its row such a piece takes is permuted so that neither the same piece of 16 rows (`rows`) nor 32 bytes of
 // eight rows in succession (`columns`, what 32 lanes read at a time) meet in a bank, of which there are 64.  (fp32 heads of up to 32 or of 65 to 96 values: `columns` meet in pairs.)
 // TINY: heads of less than 16 bytes.
-template <class T, int KD, bool TINY> struct Tile64 {
-    static constexpr int VEC = 16 / sizeof(T), kChunks = 32 * KD / VEC, kSize = kTileRows * 32 * KD, N = kTileRows * kChunks / kAttnBlock;
+// ROWS rows, brought by THREADS threads, neighbours in the workgroup.
+template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
+    static constexpr int VEC = 16 / sizeof(T), kChunks = 32 * KD / VEC, kSize = ROWS * 32 * KD, N = ROWS * kChunks / THREADS;
     typedef typename Pack<T, VEC>::raw raw;
     raw v[N];
     static __device__ __forceinline__ int place(int row, int chunk) // in 16 bytes; moves with the row by 16
@@ -121,8 +122,8 @@ template <class T, int KD, bool TINY> struct Tile64 {
         else f = (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
         return row * kChunks + (chunk ^ f);
     }
-    static __device__ __forceinline__ int row_of(int u) { return ((int)threadIdx.x + kAttnBlock * u) / kChunks; }
-    static __device__ __forceinline__ int chunk_of(int u) { return ((int)threadIdx.x + kAttnBlock * u) % kChunks; }
+    static __device__ __forceinline__ int row_of(int u) { return ((int)(threadIdx.x & (THREADS - 1)) + THREADS * u) / kChunks; }
+    static __device__ __forceinline__ int chunk_of(int u) { return ((int)(threadIdx.x & (THREADS - 1)) + THREADS * u) % kChunks; }
     // Where the thread's pieces lie, in bytes from the tile's first row; row(i): where row i starts, in elements.  A piece that ends beyond the head is loaded further left (and moved to its place by
     // `store`).
     static __device__ __forceinline__ uint32_t column(int u, int dim)
@@ -158,7 +159,9 @@ template <class T, int KD, bool TINY> struct Tile64 {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[u][e] = p[c + e < dim ? c + e : dim - 1];
             } else {
-                v[u] = *reinterpret_cast<const typename Pack<T, VEC>::type *>(from + at[u]);
+                // (a wave's own tiles are read once: 8 x 4 sequences of 4,096 to 8,192 keys, 4 heads of 128 bf16 80 us, so as what others read too 92)
+                if constexpr (THREADS == 64) v[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Pack<T, VEC>::type *>(from + at[u]));
+                else v[u] = *reinterpret_cast<const typename Pack<T, VEC>::type *>(from + at[u]);
             }
         }
     }
@@ -179,7 +182,7 @@ template <class T, int KD, bool TINY> struct Tile64 {
                 }
             }
         }
-        if (count < kTileRows || dim < 32 * KD) {
+        if (count < ROWS || dim < 32 * KD) {
 #pragma unroll
             for (int u = 0; u < N; ++u)
 #pragma unroll
@@ -240,6 +243,8 @@ __device__ __forceinline__ void part_of(const AttnArgs &a, int part, int &begin,
     begin = first + (int)((int64_t)count * part / a.splits);
     end = first + (int)((int64_t)count * (part + 1) / a.splits);
 }
+
+template <class T, int KD, bool TINY> using Tile64 = Tile<T, KD, TINY, kTileRows, kAttnBlock>;
 
 // What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
 // (LDS leaves room for one workgroup on a CU where fp32 heads are wider than 64.)

@@ -10,6 +10,53 @@ namespace svgd {
 template <class T> constexpr float kProbExponent = 0.f;
 template <> inline constexpr float kProbExponent<f16_t> = 6.f;
 
+// Running maxima and sums of a wave's rows, and their sums of values, of which value 16 d + 4 (lane / 16) + e of row lane % 16 is acc[d][b][e].
+template <class T, int KD, int QB> struct Running {
+    f32x4 acc[2 * KD][QB];
+    float top[QB], total[QB]; // total: of the lane's keys
+    __device__ __forceinline__ Running()
+    {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            top[b] = -INFINITY;
+            total[b] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 2 * KD; ++d) acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // Probabilities, relative to the maximum, of NB blocks of 16 keys from their scores, which times mul are exponents of 2.
+    template <int NB> __device__ __forceinline__ void probabilities(f32x4 (&s)[NB][QB], float mul, Frag<T> (&p)[NB / 2][QB])
+    {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            float most = s[0][b][0]; // (maximum needs no step that makes signalling NaN quiet first, as fmaxf does)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = __builtin_elementwise_maximum(most, s[j][b][e]);
+            most = max_over_rows(most);
+            if (__any(most * mul > top[b] * mul + 8.f)) {
+                const float next = fmaxf(top[b], most);
+                const float factor = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top[b] - next) * mul);
+                top[b] = next;
+                total[b] *= factor;
+#pragma unroll
+                for (int d = 0; d < 2 * KD; ++d) acc[d][b] *= factor;
+            }
+            const float base = top[b] == -INFINITY ? 0.f : kProbExponent<T> - top[b] * mul;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[j][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][b][e], mul, base));
+                    total[b] += s[j][b][e];
+                }
+#pragma unroll
+            for (int j = 0; j < NB / 2; ++j) p[j][b] = as_operand<T>(s[2 * j][b], s[2 * j + 1][b]);
+        }
+    }
+};
+
 template <class T, int KDX, int QB, bool MOD>
 __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_forward_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o,
                                                                                                               float *lse, float *partial, float *partial_lse)
@@ -52,15 +99,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     const int wave_row = min(own + 16 * QB, a.rows) - 1;
     const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
 
-    f32x4 acc[2 * KD][QB];
-    float top[QB], total[QB];
-#pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        top[b] = -INFINITY;
-        total[b] = 0.f;
-#pragma unroll
-        for (int d = 0; d < 2 * KD; ++d) acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    Running<T, KD, QB> run;
     const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
     TL kt, vt;
     uint32_t k_at[TL::N], v_at[TL::N];
@@ -124,40 +163,14 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                     }
             }
             Frag<T> p[2][QB];
-#pragma unroll
-            for (int b = 0; b < QB; ++b) {
-                float most = s[0][b][0]; // (maximum needs no step that makes signalling NaN quiet first, as fmaxf does)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) most = __builtin_elementwise_maximum(most, s[j][b][e]);
-                most = max_over_rows(most);
-                if (__any(most * mul > top[b] * mul + 8.f)) {
-                    const float next = fmaxf(top[b], most);
-                    const float factor = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top[b] - next) * mul);
-                    top[b] = next;
-                    total[b] *= factor;
-#pragma unroll
-                    for (int d = 0; d < 2 * KD; ++d) acc[d][b] *= factor;
-                }
-                const float base = top[b] == -INFINITY ? 0.f : kProbExponent<T> - top[b] * mul;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[j][b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][b][e], mul, base));
-                        total[b] += s[j][b][e];
-                    }
-                p[0][b] = as_operand<T>(s[0][b], s[1][b]);
-                p[1][b] = as_operand<T>(s[2][b], s[3][b]);
-            }
+            run.probabilities(s, mul, p);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int d = 0; d < 2 * KD; ++d) {
                     const Frag<T> f = TL::columns(vl, 32 * j, 16 * d);
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, p[j][b], acc[d][b]);
+                    for (int b = 0; b < QB; ++b) run.acc[d][b] = mma(f, p[j][b], run.acc[d][b]);
                 }
         }
         half ^= 1;
@@ -167,18 +180,18 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int r = own + 16 * b + (lane & 15);
-        const float sum = sum_over_rows(total[b]);
+        const float sum = sum_over_rows(run.total[b]);
         if (r >= a.rows) continue;
         const bool none = sum == 0.f;
         const float inverse = none ? 0.f : 1.f / sum;
-        const float log = none ? -INFINITY : (top[b] * mul - kProbExponent<T> + __builtin_amdgcn_logf(sum)) * kLn2;
+        const float log = none ? -INFINITY : (run.top[b] * mul - kProbExponent<T> + __builtin_amdgcn_logf(sum)) * kLn2;
         const int i = a.query(r), h = at.head * a.group + r - i * a.group;
         const int64_t line = a.line(at.particle, at.batch, h, i), lines = (int64_t)a.n * a.batch * a.heads * a.t;
         if (a.splits > 1) {
             if (g == 0) partial_lse[at.part * lines + line] = log;
             float *const out = partial + (at.part * lines + line) * (32 * KD);
 #pragma unroll
-            for (int d = 0; d < 2 * KD; ++d) *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[d][b] * inverse;
+            for (int d = 0; d < 2 * KD; ++d) *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : run.acc[d][b] * inverse;
         } else {
             if (g == 0 && lse) lse[line] = log;
             T *const out = o.at(at.particle, at.batch, h) + i * o.token;
@@ -187,9 +200,129 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                 const int c = 16 * d + 4 * g;
                 float x[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : acc[d][b][e] * inverse;
+                for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : run.acc[d][b][e] * inverse;
                 if (c < a.dim) store_pack<T, 4>(out + c, a.dim - c, x);
             }
+        }
+    }
+}
+
+// Up to 16 rows: single tokens, or a few, over a cache.  All four waves have the same rows; each takes every fourth tile of 32 keys through a part of LDS of its own, so that none waits for another before the
+// end, when their sums are joined.  Reading keys and values once bounds it.
+constexpr int kFewKeys = 32;
+template <class T, int KDX, bool MOD>
+__global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o, float *lse, float *partial, float *partial_lse)
+{
+    constexpr int KD = kBlocks32<KDX>;
+    typedef Tile<T, KD, KDX == 0, kFewKeys, 64> TL;
+    constexpr int kJoin = 16 * (32 * KD + 4); // floats of a wave's sums: rows four floats apart from what would be one bank
+    constexpr int kPart = 2 * TL::kSize * (int)sizeof(T) > kJoin * 4 ? 2 * TL::kSize * (int)sizeof(T) : kJoin * 4;
+    __shared__ __attribute__((aligned(16))) char lds[kAttnWaves][kPart];
+    __shared__ float tops[kAttnWaves][16], totals[kAttnWaves][16];
+    const AttnBlock at(a);
+    if (!at.any) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const Masks masks(a, at.batch);
+    const float mul = MOD ? 1.f : a.scale * kLog2e;
+    const Modified modified(a);
+    const int r = min(lane & 15, a.rows - 1), i = a.query(r), h = at.head * a.group + r - i * a.group;
+    const T *const qp = q.at(at.particle, at.batch, h) + i * q.token;
+    Frag<T> qf[1][KD];
+#pragma unroll
+    for (int s = 0; s < KD; ++s) qf[0][s] = load_frag(qp + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+    const int position = masks.start + i, limit = masks.end(a, position), document = masks.document(a, position);
+    const float slope = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + h] * kLog2e : 0.f;
+    const int p0 = masks.start, p1 = masks.start + a.t - 1;
+    const int hi = masks.documents ? (p1 < 0 || p0 >= a.s ? 0 : masks.end(a, min(p1, a.s - 1))) : masks.end(a, p1);
+    const int free_keys = masks.documents ? 0 : masks.end(a, p0);
+    int begin = 0, end = (hi + kFewKeys - 1) / kFewKeys;
+    part_of(a, at.part, begin, end);
+
+    Running<T, KD, 1> run;
+    const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
+    T *const kl = reinterpret_cast<T *>(lds[wave]), *const vl = kl + TL::kSize;
+    TL kt, vt;
+    uint32_t k_at[TL::N], v_at[TL::N];
+    TL::offsets(k_at, a.dim, [&](int j) { return (uint32_t)j * (uint32_t)k.token; });
+    TL::offsets(v_at, a.dim, [&](int j) { return (uint32_t)j * (uint32_t)v.token; });
+    const auto fetch = [&](int n) {
+        const int key = n * kFewKeys, last = min(hi - key, kFewKeys) - 1;
+        kt.load(ks + key * k.token, k_at, (uint32_t)k.token, last, a.dim);
+        vt.load(vs + key * v.token, v_at, (uint32_t)v.token, last, a.dim);
+    };
+    loads_done();
+    if (begin + wave < end) fetch(begin + wave);
+    for (int n = begin + wave; n < end; n += kAttnWaves) {
+        const int key = n * kFewKeys;
+        wave_sync(); // (the tile before has been read)
+        kt.store(kl, hi - key, a.dim);
+        vt.store(vl, hi - key, a.dim);
+        wave_sync();
+        if (n + kAttnWaves < end) fetch(n + kAttnWaves);
+        f32x4 s[2][1];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            s[j][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KD; ++c) s[j][0] = mma(TL::rows(kl, 16 * j, 32 * c), qf[0][c], s[j][0]);
+        }
+        if constexpr (MOD) {
+            modified.template apply<T>(s);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[j][0][e] = modified.exponent(s[j][0][e], slope, fabsf((float)(position - (key + 16 * j + 4 * g + e))));
+        }
+        if (key + kFewKeys > free_keys) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at_key = key + 16 * j + 4 * g + e;
+                    const int doc = masks.documents ? masks.documents[min(at_key, a.s - 1)] : 0;
+                    if (at_key >= limit || doc != document) s[j][0][e] = -INFINITY;
+                }
+        }
+        Frag<T> p[1][1];
+        run.probabilities(s, mul, p);
+#pragma unroll
+        for (int d = 0; d < 2 * KD; ++d) run.acc[d][0] = mma(TL::columns(vl, 0, 16 * d), p[0][0], run.acc[d][0]);
+    }
+    // the waves' sums, in their order
+    run.total[0] = sum_over_rows(run.total[0]);
+    wave_sync();
+    float *const mine = reinterpret_cast<float *>(lds[wave]);
+    if (g == 0) {
+        tops[wave][lane] = run.top[0];
+        totals[wave][lane] = run.total[0];
+    }
+#pragma unroll
+    for (int d = 0; d < 2 * KD; ++d) *reinterpret_cast<f32x4 *>(mine + (lane & 15) * (32 * KD + 4) + 16 * d + 4 * g) = run.acc[d][0];
+    __syncthreads();
+    for (int x = threadIdx.x; x < a.rows * 8 * KD; x += kAttnBlock) {
+        const int row = x / (8 * KD), c = (x - row * 8 * KD) * 4;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) top = __builtin_elementwise_maximum(top, tops[w][row]);
+        f32x4 all = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kAttnWaves; ++w) {
+            if (totals[w][row] == 0.f) continue;
+            const float share = __builtin_amdgcn_exp2f((tops[w][row] - top) * mul);
+            sum += share * totals[w][row];
+            all += share * *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(lds[w]) + row * (32 * KD + 4) + c);
+        }
+        const bool none = sum == 0.f;
+        const float inverse = none ? 0.f : 1.f / sum, log = none ? -INFINITY : (top * mul - kProbExponent<T> + __builtin_amdgcn_logf(sum)) * kLn2;
+        const int query = a.query(row), head = at.head * a.group + row - query * a.group;
+        const int64_t line = a.line(at.particle, at.batch, head, query), lines = (int64_t)a.n * a.batch * a.heads * a.t;
+        if (a.splits > 1) {
+            if (c == 0) partial_lse[at.part * lines + line] = log;
+            *reinterpret_cast<f32x4 *>(partial + (at.part * lines + line) * (32 * KD) + c) = all * inverse;
+        } else {
+            if (c == 0 && lse) lse[line] = log;
+            const float y[4] = {all[0] * inverse, all[1] * inverse, all[2] * inverse, all[3] * inverse};
+            if (c < a.dim) store_pack<T, 4>(o.at(at.particle, at.batch, head) + query * o.token + c, a.dim - c, y);
         }
     }
 }
@@ -202,15 +335,33 @@ template <class T> __global__ __launch_bounds__(256) void attention_join_kernel(
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, line = k / quads;
     const int c = (int)(k - line * quads) * 4;
     if (line >= lines || c >= a.dim) return;
+    // eight parts at a time, so that their loads are on their way together
+    constexpr int U = 8;
     float top = -INFINITY, total = 0.f;
-    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, partial_lse[p * lines + line]);
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < a.splits; ++p) {
-        const float l = partial_lse[p * lines + line];
-        if (l == -INFINITY) continue;
-        const float w = __builtin_amdgcn_exp2f((l - top) * kLog2e);
-        total += w;
-        sum += w * *reinterpret_cast<const f32x4 *>(partial + (p * lines + line) * ld + c);
+    for (int p0 = 0; p0 < a.splits; p0 += U) {
+        float l[U];
+        f32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t p = min(p0 + u, a.splits - 1);
+            l[u] = partial_lse[p * lines + line];
+            x[u] = *reinterpret_cast<const f32x4 *>(partial + (p * lines + line) * ld + c);
+        }
+        float next = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) next = __builtin_elementwise_maximum(next, l[u]);
+        const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - next) * kLog2e);
+        total *= old;
+        sum *= old;
+        top = next;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p0 + u >= a.splits || l[u] == -INFINITY) continue;
+            const float w = __builtin_amdgcn_exp2f((l[u] - top) * kLog2e);
+            total += w;
+            sum += w * x[u];
+        }
     }
     const bool none = total == 0.f;
     const float inverse = none ? 0.f : 1.f / total;

@@ -10,6 +10,11 @@ template <> int svgd::attention_forward<SVGD_ATTENTION_TYPE>(AttnCall &c)
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
+            if (few_rows(a)) {
+                set_grid(a, a.rows, 16 * kAttnWaves, forward_splits(a));
+                attention_few_kernel<T, KD, MOD><<<a.per_die * 8, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
+                return launched_ok();
+            }
             const bool two = kTwoForward<T, KD, MOD> && small_blocks(a, a.rows) >= kManyForward;
             set_grid(a, a.rows, 16 * kAttnWaves * (two ? 2 : 1), forward_splits(a));
             const int grid = a.per_die * 8;

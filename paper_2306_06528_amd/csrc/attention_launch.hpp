@@ -34,7 +34,16 @@ inline int parts_for(const AttnArgs &a, int64_t own, int64_t streamed)
     const int64_t parts = wanted < most ? wanted : most;
     return (int)(parts > 64 ? 64 : parts);
 }
-inline int forward_splits(const AttnArgs &a) { return parts_for(a, a.rows, a.s); }
+constexpr int64_t kFewBlocks = 1024;
+inline bool few_rows(const AttnArgs &a) { return a.rows <= 16; }
+inline int forward_splits(const AttnArgs &a)
+{
+    if (!few_rows(a)) return parts_for(a, a.rows, a.s);
+    // two tiles of 32 keys for every wave at least
+    const int64_t blocks = small_blocks(a, a.rows), most = a.s / (2 * kAttnWaves * 32), wanted = ceil_div(kFewBlocks, blocks);
+    const int64_t parts = wanted < most ? wanted : most;
+    return (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+}
 inline int query_splits(const AttnArgs &a) { return parts_for(a, a.rows, a.s); }
 inline int key_splits(const AttnArgs &a) { return parts_for(a, a.s, a.rows); }
 
