@@ -54,8 +54,6 @@ int check(int dtype, const svgd_rotary *p)
 RotaryArgs args_of(const svgd_rotary &p, int64_t most)
 {
     RotaryArgs a{};
-    a.heads = p.heads;
-    a.kv = p.kv_heads;
     a.dim = p.dim;
     a.pairs = p.pairs;
     a.interleaved = p.interleaved != 0;
@@ -65,8 +63,6 @@ RotaryArgs args_of(const svgd_rotary &p, int64_t most)
     a.positions = p.positions;
     a.positions_stride = p.positions_stride;
     a.eps = (float)p.eps;
-    a.q_weight = {p.q_weight, p.q_weight_stride, p.dim};
-    a.k_weight = {p.k_weight, p.k_weight_stride, p.dim};
     const int64_t blocks = most / p.n > 1 ? most / p.n : 1;
     a.per = (a.tokens + blocks - 1) / blocks;
     if (a.per > kTokens) a.per = (a.per + kTokens - 1) / kTokens * kTokens;
@@ -74,7 +70,7 @@ RotaryArgs args_of(const svgd_rotary &p, int64_t most)
     a.blocks = (int)((a.tokens + a.per - 1) / a.per);
     return a;
 }
-constexpr int64_t kForwardBlocks = 8192, kBackwardBlocks = 2048;
+constexpr int64_t kForwardBlocks = 2048, kBackwardBlocks = 2048;
 
 struct Reads { // besides the activations
     Extent e[4];
@@ -120,7 +116,11 @@ int svgd_qk_norm_rotary_forward(int dtype, const svgd_rotary *p, svgd_heads q, s
     return for_type(dtype, [&](auto t) {
         using T = decltype(t);
         return for_team<T>(p->dim, [&](auto l) {
-            rotary_forward_kernel<T, decltype(l)::value><<<p->n * a.blocks, kRotaryBlock, 0, (hipStream_t)stream>>>(a, in<T>(q), in<T>(k), out<T>(q_out), out<T>(k_out));
+            const RotaryKinds<T> kinds{{{in<T>(q), {}, out<T>(q_out), {p->q_weight, p->q_weight_stride, p->dim}, p->heads},
+                                        {in<T>(k), {}, out<T>(k_out), {p->k_weight, p->k_weight_stride, p->dim}, p->kv_heads}}};
+            constexpr int L = decltype(l)::value;
+            if (p->dim * sizeof(T) % 16 == 0) rotary_forward_kernel<T, L, true><<<p->n * a.blocks, kRotaryBlock, 0, (hipStream_t)stream>>>(a, kinds);
+            else rotary_forward_kernel<T, L, false><<<p->n * a.blocks, kRotaryBlock, 0, (hipStream_t)stream>>>(a, kinds);
             return launched();
         });
     });
@@ -180,8 +180,11 @@ int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_
         const int rc = for_type(dtype, [&](auto t) {
             using T = decltype(t);
             return for_team<T>(p->dim, [&](auto l) {
-                rotary_backward_kernel<T, decltype(l)::value><<<p->n * a.blocks, kRotaryBlock, 0, (hipStream_t)stream>>>(a, in<T>(dq_out), in<T>(dk_out), in<T>(q), in<T>(k), out<T>(dq),
-                                                                                                                      out<T>(dk), params ? (float *)scratch : nullptr);
+                const RotaryKinds<T> kinds{{{in<T>(q), in<T>(dq_out), out<T>(dq), w[0], p->heads}, {in<T>(k), in<T>(dk_out), out<T>(dk), w[1], p->kv_heads}}};
+                constexpr int L = decltype(l)::value;
+                float *const partial = params ? (float *)scratch : nullptr;
+                if (p->dim * sizeof(T) % 16 == 0) rotary_backward_kernel<T, L, true><<<p->n * a.blocks, kRotaryBlock, 0, (hipStream_t)stream>>>(a, kinds, partial);
+                else rotary_backward_kernel<T, L, false><<<p->n * a.blocks, kRotaryBlock, 0, (hipStream_t)stream>>>(a, kinds, partial);
                 return launched();
             });
         });

@@ -10,14 +10,13 @@ constexpr int kTokens = 8, kRotaryBlock = 256;
 constexpr int kMaxPairs = SVGD_ROTARY_MAX_DIM / 2;
 
 struct RotaryArgs {
-    int heads, kv, dim, pairs, interleaved;
+    int dim, pairs, interleaved;
     int length;
     int64_t tokens; // batch length: of a particle
     const double *frequencies;
     const int64_t *positions;
     int64_t positions_stride;
     float eps;
-    Params q_weight, k_weight;
     int blocks;  // workgroups per particle
     int64_t per; // tokens of each
 };
@@ -111,14 +110,93 @@ __device__ __forceinline__ void angles(const RotaryArgs &a, int64_t first, int64
     }
 }
 
-template <class T, int L>
-__global__ __launch_bounds__(kRotaryBlock) void rotary_forward_kernel(RotaryArgs a, Heads<const T> q, Heads<const T> k, Heads<T> q_out, Heads<T> k_out)
+// What a pass reads and writes of queries (0) and of keys (1): read from the kernel's arguments by number, so that only one of them takes scalar registers at a time.
+template <class T> struct RotaryKind {
+    Heads<const T> x, dy; // backward; forward x alone
+    Heads<T> to;
+    Params weight;
+    int heads;
+};
+template <class T> struct RotaryKinds {
+    RotaryKind<T> of[2];
+};
+
+// A lane's 16 bytes of a head as they come from memory, 0 behind the head's end.  WHOLE: heads end with such a piece.
+template <class T, bool WHOLE> struct HeadPiece {
+    static constexpr int VEC = 16 / sizeof(T);
+    typename Pack<T, VEC>::raw v;
+    __device__ __forceinline__ void load(const T *head, int c, int dim)
+    {
+        if constexpr (WHOLE) {
+            v = *reinterpret_cast<const typename Pack<T, VEC>::type *>(head + (c < dim ? c : 0));
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] = head[c + e < dim ? c + e : 0];
+        }
+    }
+    __device__ __forceinline__ void get(float (&y)[VEC], int c, int dim) const
+    {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) y[e] = (WHOLE ? c : c + e) < dim ? (float)v[e] : 0.f;
+    }
+    static __device__ __forceinline__ void store(T *head, int c, int dim, const float (&y)[VEC])
+    {
+        if (c < dim) store_pack<T, VEC>(head + c, WHOLE ? VEC : dim - c, y);
+    }
+};
+
+// The heads of `count` tokens from token0 on, dealt to the teams one after the other.  From one of a team's to its next one it is `tokens` tokens and `more` heads, and at the end of a token's heads or of a
+// sequence a step back: pointers are moved on by sums (as products of 64 bits addresses took a third of the instructions).
+struct HeadTurn {
+    int items, heads, length, teams, item, tokens, more;
+    int i, t, h; // the token's number among them, of its sequence; head
+    int b;
+    __device__ __forceinline__ HeadTurn(const RotaryArgs &a, int64_t token0, int count, int heads_, int team, int teams_)
+        : items(count * heads_), heads(max(heads_, 1)), length(a.length), teams(teams_), item(team)
+    {
+        tokens = teams / heads;
+        more = teams - tokens * heads;
+        i = (uint32_t)item / (uint32_t)heads;
+        h = item - i * heads;
+        const int64_t token = token0 + i;
+        b = (int)(token / length);
+        t = (int)(token - (int64_t)b * length);
+    }
+    __device__ __forceinline__ bool any() const { return item < items; }
+};
+template <class P> struct HeadPointer {
+    P *p;
+    int64_t step, carry, wrap;
+    __device__ __forceinline__ HeadPointer(P *base, const Heads<P> &s, const HeadTurn &at)
+        : p(base + at.b * s.batch + at.t * s.token + at.h * s.head), step(at.tokens * s.token + at.more * s.head), carry(s.token - at.heads * s.head), wrap(s.batch - at.length * s.token)
+    {
+    }
+};
+template <class... Ps> __device__ __forceinline__ void next_head(HeadTurn &at, HeadPointer<Ps> &...ps)
+{
+    at.item += at.teams;
+    at.i += at.tokens;
+    at.t += at.tokens;
+    at.h += at.more;
+    ((ps.p += ps.step), ...);
+    if (at.h >= at.heads) {
+        at.h -= at.heads;
+        ++at.i;
+        ++at.t;
+        ((ps.p += ps.carry), ...);
+    }
+    while (at.t >= at.length) { // (mostly not once, kTokens times at most)
+        at.t -= at.length;
+        ((ps.p += ps.wrap), ...);
+    }
+}
+
+template <class T, int L, bool WHOLE> __global__ __launch_bounds__(kRotaryBlock) void rotary_forward_kernel(RotaryArgs a, RotaryKinds<T> kinds)
 {
     constexpr int VEC = 16 / sizeof(T), kTeams = kRotaryBlock / L;
     __shared__ __attribute__((aligned(16))) float cs[kTokens][kMaxPairs], sn[kTokens][kMaxPairs], slots[kTeams][L * VEC];
     const int particle = blockIdx.x / a.blocks, team = threadIdx.x / L, c = threadIdx.x % L * VEC;
     const int64_t first = (blockIdx.x - particle * a.blocks) * a.per, last = first + a.per < a.tokens ? first + a.per : a.tokens;
-    const bool norm = a.q_weight.p != nullptr;
     const float inverse = 1.f / (float)a.dim;
     for (int64_t token0 = first; token0 < last; token0 += kTokens) {
         __syncthreads(); // (the angles before these have been read)
@@ -127,43 +205,45 @@ __global__ __launch_bounds__(kRotaryBlock) void rotary_forward_kernel(RotaryArgs
         const int count = last - token0 < kTokens ? (int)(last - token0) : kTokens;
 #pragma unroll 1
         for (int kind = 0; kind < 2; ++kind) {
-            const Heads<const T> &from = kind ? k : q;
-            const Heads<T> &to = kind ? k_out : q_out;
-            const Params &weight = kind ? a.k_weight : a.q_weight;
-            const int heads = kind ? a.kv : a.heads;
+            const RotaryKind<T> &k = kinds.of[kind];
+            const bool norm = k.weight.p != nullptr;
             float w[VEC];
-            if (norm) load_pack<float, VEC>(weight.p + particle * weight.stride + c, a.dim - c, w);
-            for (int item = team; item < count * heads; item += kTeams) {
-                const int i = item / heads, h = item - i * heads;
-                const int64_t token = token0 + i;
-                const int b = (int)(token / a.length), t = (int)(token - (int64_t)b * a.length);
+            if (norm) load_pack<float, VEC>(k.weight.p + particle * k.weight.stride + c, a.dim - c, w);
+            // (the next head is on its way while one is worked on)
+            HeadTurn at(a, token0, count, k.heads, team, kTeams);
+            HeadPointer<const T> from(k.x.p + particle * k.x.particle, k.x, at);
+            HeadPointer<T> to(k.to.p + particle * k.to.particle, k.to, at);
+            HeadPiece<T, WHOLE> next;
+            if (at.any()) next.load(from.p, c, a.dim);
+            while (at.any()) {
                 float y[VEC];
-                load_pack<T, VEC>(from.at(particle, b, h) + t * from.token + c, a.dim - c, y);
+                next.get(y, c, a.dim);
+                const int i = at.i;
+                T *const out = to.p;
+                next_head(at, from, to);
+                if (at.any()) next.load(from.p, c, a.dim);
                 if (norm) {
                     float square = 0.f;
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) square += y[e] * y[e];
-                    const float rstd = 1.f / sqrtf(head_sum<L>(square) * inverse + a.eps);
+                    const float rstd = __builtin_amdgcn_rsqf(head_sum<L>(square) * inverse + a.eps);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) y[e] = y[e] * rstd * w[e];
                 }
                 turn<VEC>(a, y, c, slots[team], cs[i], sn[i], 1.f);
-                if (c < a.dim) store_pack<T, VEC>(to.at(particle, b, h) + t * to.token + c, a.dim - c, y);
+                HeadPiece<T, WHOLE>::store(out, c, a.dim, y);
             }
         }
     }
 }
 
 // partial: the workgroups' sums of the weights' gradients, [particle][workgroup][queries', keys'][dim]; null: not wanted
-template <class T, int L>
-__global__ __launch_bounds__(kRotaryBlock) void rotary_backward_kernel(RotaryArgs a, Heads<const T> dq_out, Heads<const T> dk_out, Heads<const T> q, Heads<const T> k, Heads<T> dq, Heads<T> dk,
-                                                                       float *partial)
+template <class T, int L, bool WHOLE> __global__ __launch_bounds__(kRotaryBlock) void rotary_backward_kernel(RotaryArgs a, RotaryKinds<T> kinds, float *partial)
 {
     constexpr int VEC = 16 / sizeof(T), kTeams = kRotaryBlock / L;
     __shared__ __attribute__((aligned(16))) float cs[kTokens][kMaxPairs], sn[kTokens][kMaxPairs], slots[kTeams][L * VEC];
     const int particle = blockIdx.x / a.blocks, team = threadIdx.x / L, c = threadIdx.x % L * VEC;
     const int64_t first = (blockIdx.x - particle * a.blocks) * a.per, last = first + a.per < a.tokens ? first + a.per : a.tokens;
-    const bool norm = a.q_weight.p != nullptr;
     const float inverse = 1.f / (float)a.dim;
     float dw[2][VEC];
 #pragma unroll
@@ -173,21 +253,32 @@ __global__ __launch_bounds__(kRotaryBlock) void rotary_backward_kernel(RotaryArg
         angles(a, token0, last, cs, sn);
         __syncthreads();
         const int count = last - token0 < kTokens ? (int)(last - token0) : kTokens;
-#pragma unroll
+#pragma unroll 1
         for (int kind = 0; kind < 2; ++kind) {
-            const Heads<const T> &dy = kind ? dk_out : dq_out, &from = kind ? k : q;
-            const Heads<T> &to = kind ? dk : dq;
-            const Params &weight = kind ? a.k_weight : a.q_weight;
-            const int heads = kind ? a.kv : a.heads;
-            float w[VEC];
-            if (norm) load_pack<float, VEC>(weight.p + particle * weight.stride + c, a.dim - c, w);
-            for (int item = team; item < count * heads; item += kTeams) {
-                const int i = item / heads, h = item - i * heads;
-                const int64_t token = token0 + i;
-                const int b = (int)(token / a.length), t = (int)(token - (int64_t)b * a.length);
+            const RotaryKind<T> &k = kinds.of[kind];
+            const bool norm = k.weight.p != nullptr, store = k.to.p != nullptr;
+            float w[VEC], d[VEC];
+            if (norm) load_pack<float, VEC>(k.weight.p + particle * k.weight.stride + c, a.dim - c, w);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[e] = kind ? dw[1][e] : dw[0][e];
+            HeadTurn at(a, token0, count, k.heads, team, kTeams);
+            HeadPointer<const T> from(k.x.p + particle * k.x.particle, k.x, at), dy(k.dy.p + particle * k.dy.particle, k.dy, at);
+            HeadPointer<T> to(k.to.p + particle * k.to.particle, k.to, at);
+            HeadPiece<T, WHOLE> next_g, next_x;
+            const auto fetch = [&] {
+                if (!at.any()) return;
+                next_g.load(dy.p, c, a.dim);
+                if (norm) next_x.load(from.p, c, a.dim);
+            };
+            fetch();
+            while (at.any()) {
                 float g[VEC], x[VEC];
-                load_pack<T, VEC>(dy.at(particle, b, h) + t * dy.token + c, a.dim - c, g);
-                if (norm) load_pack<T, VEC>(from.at(particle, b, h) + t * from.token + c, a.dim - c, x);
+                next_g.get(g, c, a.dim);
+                if (norm) next_x.get(x, c, a.dim);
+                const int i = at.i;
+                T *const out = to.p;
+                next_head(at, from, dy, to);
+                fetch();
                 turn<VEC>(a, g, c, slots[team], cs[i], sn[i], -1.f);
                 if (norm) {
                     float square = 0.f, mean = 0.f;
@@ -196,16 +287,21 @@ __global__ __launch_bounds__(kRotaryBlock) void rotary_backward_kernel(RotaryArg
                         square += x[e] * x[e];
                         mean += g[e] * w[e] * x[e];
                     }
-                    const float rstd = 1.f / sqrtf(head_sum<L>(square) * inverse + a.eps);
+                    const float rstd = __builtin_amdgcn_rsqf(head_sum<L>(square) * inverse + a.eps);
                     mean = head_sum<L>(mean) * inverse * rstd; // of a xhat
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
                         const float xhat = x[e] * rstd;
-                        dw[kind][e] += g[e] * xhat;
+                        d[e] += g[e] * xhat;
                         g[e] = rstd * (g[e] * w[e] - xhat * mean);
                     }
                 }
-                if (to.p && c < a.dim) store_pack<T, VEC>(to.at(particle, b, h) + t * to.token + c, a.dim - c, g);
+                if (store) HeadPiece<T, WHOLE>::store(out, c, a.dim, g);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                dw[0][e] = kind ? dw[0][e] : d[e];
+                dw[1][e] = kind ? d[e] : dw[1][e];
             }
         }
     }
