@@ -133,6 +133,14 @@ template <int P, int STEP> struct RowsOfA { // STEP: 2 where the groups of 8 row
             }
         }
     }
+    __device__ __forceinline__ void leave_out(int count) // the step's first `count` columns count as 0
+    {
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * (int)(threadIdx.x & 7) + e < count) v[n][e] = 0.f;
+    }
     __device__ __forceinline__ void stage(float *scratch) const
     {
         f32x4 *const s = reinterpret_cast<f32x4 *>(scratch);
@@ -189,6 +197,14 @@ template <class T, int P> struct ColumnsOfA {
                 v[e][t] = k < K ? x : (T)0.f;
             }
         }
+    }
+    __device__ __forceinline__ void leave_out(int count)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (k_of((threadIdx.x & 63) >> 4, e) < count) v[e][t] = (T)0.f;
     }
     __device__ __forceinline__ void stage(float *) const {}
     __device__ __forceinline__ void parts(int ib, const SplitConst &sc, bf16x8 (&out)[P], const float *) const
@@ -343,8 +359,10 @@ template <int NJ> struct Acc {
 // other half of LDS and those of A are split into the registers of the last columns' blocks as these get free, and the rows of the
 // step after it are on their way: one barrier per step.
 // lds: 2 * PB * kPlane units; scratch: the wave's own kScratch floats.
+// BACK: the last step, if it is not whole, begins further back, where it is, and what it has in common with the step before counts as 0: loaded like any other (otherwise value by value, behind
+// the others).
 constexpr int kScratch = 64 * kTileK; // 64 rows of a step of A; 16 rows of 68 values of C
-template <class TL, int PA, int PB, class LA, class LB>
+template <class TL, int PA, int PB, bool BACK = false, class LA, class LB>
 __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_t K, Acc<TL::kBlocksJ> &acc, bf16x8 *lds, float *scratch)
 {
     if (begin >= K) return;
@@ -377,13 +395,15 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
                     }
         }
     };
-    const int64_t whole = a.narrow || b.narrow ? begin : K / kTileK * kTileK;
+    const bool back = BACK && K >= kTileK;
+    const int64_t whole = a.narrow || b.narrow ? begin : (back ? K + kTileK - 1 : K) / kTileK * kTileK;
     if (whole > begin) {
-        const int64_t last = whole - kTileK; // (what is fetched ahead of the end is the last step again)
-        b.fetch(begin);
-        a.fetch(begin);
+        const int64_t last = back ? K - kTileK : whole - kTileK; // (what is fetched ahead of the end is the last step again)
+        b.fetch(BACK && last < begin ? last : begin);
+        a.fetch(BACK && last < begin ? last : begin);
         __syncthreads(); // (an earlier product's last step has been read)
         b.store(lds, sc);
+        if (BACK && begin + kTileK > K) a.leave_out((int)(begin + kTileK - K));
         a.stage(scratch);
 #pragma unroll
         for (int ib = 0; ib < 4; ++ib) a.parts(ib, sc, fa[ib], scratch);
@@ -400,20 +420,22 @@ __device__ __forceinline__ void tile_product(LA &a, LB &b, int64_t begin, int64_
                 b.fetch(next);
                 __builtin_amdgcn_sched_barrier(0);
                 columns(0, NJ - kLast);
+                if (BACK && k0 + kTileK > K) a.leave_out((int)(k0 + kTileK - K));
                 if constexpr (LA::kStaged) {
                     a.stage(scratch);
                     a.fetch(next);
                 }
             } else {
-                b.fetch(k0);
+                b.fetch(BACK && last < k0 ? last : k0);
                 __builtin_amdgcn_sched_barrier(0);
                 columns(0, NJ / 2 - 1);
                 b.store(lds + (kStage - stage), sc);
                 __builtin_amdgcn_sched_barrier(0);
-                a.fetch(k0);
+                a.fetch(BACK && last < k0 ? last : k0);
                 __builtin_amdgcn_sched_barrier(0);
                 columns(NJ / 2 - 1, NJ - kLast);
                 __builtin_amdgcn_sched_barrier(0);
+                if (BACK && k0 + kTileK > K) a.leave_out((int)(k0 + kTileK - K));
                 a.stage(scratch);
             }
             bf16x8 fb[kLast][PB];
@@ -705,7 +727,7 @@ template <class TA, class TB> struct WeightGrad {
     float *partial;
 };
 
-template <class TL, bool SWAPPED, class TA, class TB>
+template <class TL, bool SWAPPED, bool BACK = false, class TA, class TB>
 __device__ __forceinline__ void weight_grad_tile(const WeightGrad<TA, TB> &w, int block, bool accumulate, bf16x8 *lds, float *scratch)
 {
     constexpr int PA = kParts<TA>, PB = kParts<TB>;
@@ -723,7 +745,7 @@ __device__ __forceinline__ void weight_grad_tile(const WeightGrad<TA, TB> &w, in
     ColumnsOfA<TA, PA> a(w.a.p + particle * w.a.particle, w.a.row, iw, w.wide);
     ColumnsOfB<TL, TB, PB> b(b_rows.p + particle * b_rows.particle, b_rows.row, j0, w.high);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, PA, PB>(a, b, w.grid.begin(part), w.grid.end(part), acc, lds, scratch);
+    tile_product<TL, PA, PB, BACK>(a, b, w.grid.begin(part), w.grid.end(part), acc, lds, scratch);
     each_quad<TL, true>(acc, iw, w.wide, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
         if (j >= w.high) return;
         const int skip = (int)(first - i);
@@ -773,6 +795,7 @@ template <class T> __global__ __launch_bounds__(256) void reduce_rows_kernel(Ffn
     const int64_t each = s.n * s.rows * s.width_ld;
     const float *p = partial + line * s.width_ld + i;
     f32x4 total = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int part = 0; part < parts; ++part) total += *reinterpret_cast<const f32x4 *>(p + part * each);
     store_quad(y.p + particle * y.particle + j * y.row + i, total, 0, s.width - i);
 }
@@ -784,6 +807,7 @@ static __global__ __launch_bounds__(256) void reduce_params_kernel(int n, int64_
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, each = n * outs * size;
     if (k >= each) return;
     float total = 0.f;
+#pragma unroll 8
     for (int part = 0; part < parts; ++part) total += partial[part * each + k];
     const int64_t line = k / size, at = k - line * size, particle = line / outs;
     const Params &out = line - particle * outs ? out1 : out0;

@@ -101,7 +101,7 @@ SVGD_TILE_KERNEL void linear_forward_kernel(LinearShape s, TileGrid grid, Rows<c
     RowsOfA<3, 1> a(w + first * s.width, w, s.out - first, s.width);
     RowsOfB<TL, T, P> b(x.p + particle * x.particle + j0 * x.row, x.row, s.rows - j0);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, 3, P>(a, b, grid.begin(part), grid.end(part), acc, lds, scratch);
+    tile_product<TL, 3, P, true>(a, b, grid.begin(part), grid.end(part), acc, lds, scratch);
     const LinearEnd<T> end = to.of(s, particle);
     float *const sums = partial + ((int64_t)part * s.n + particle) * s.rows * s.out_ld;
     each_quad<TL, false>(acc, iw, s.out, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t) {
@@ -238,7 +238,7 @@ SVGD_TILE_KERNEL void linear_gradients_kernel(LinearShape s, TileGrid input, Row
     float *const scratch = scratches[wave_of_block()];
     const int block = blockIdx.x;
     if (block >= input.per_die * kDies) {
-        weight_grad_tile<TL, false>(grad, block - input.per_die * kDies, accumulate, lds, scratch);
+        weight_grad_tile<TL, false, true>(grad, block - input.per_die * kDies, accumulate, lds, scratch);
         return;
     }
     int particle, part, ti, tj;
@@ -247,7 +247,7 @@ SVGD_TILE_KERNEL void linear_gradients_kernel(LinearShape s, TileGrid input, Row
     ColumnsOfA<float, 3> a(weight.p + particle * weight.stride, s.width, iw, s.width);
     RowsOfB<TL, TD, P> b(dz.p + particle * dz.particle + j0 * dz.row, dz.row, s.rows - j0);
     Acc<TL::kBlocksJ> acc;
-    tile_product<TL, 3, P>(a, b, input.begin(part), input.end(part), acc, lds, scratch);
+    tile_product<TL, 3, P, true>(a, b, input.begin(part), input.end(part), acc, lds, scratch);
     float *const sums = dx_partial + ((int64_t)part * s.n + particle) * s.rows * s.width_ld;
     each_quad<TL, true>(acc, iw, s.width, j0, scratch, [&](int64_t i, int64_t j, f32x4 c, int64_t first) {
         if (j >= s.rows) return;

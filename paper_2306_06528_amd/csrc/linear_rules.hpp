@@ -4,13 +4,18 @@
 
 namespace svgd {
 
+// What a launch takes (ffn_rules.hpp says in what): of the kinds and of one, two or four parts at 14 shapes (1 to 32 particles of 40 to 16,000 rows, 64 to 2,000 wide), fp32 and bf16, forward finds the fastest or one
+// within 7 % of it, backward one within 14 %.  (With the rates of the feed-forward block's products 5 x 1,003 x 333 x 501 fp32 forward took 39 us, so 29; 8 x 1,576 x 384 x 1,152 fp32 backward 202 and 164.)
+constexpr Rates kOfLinear = {{1.0, 0.61, 0.42}, 1.0, 8.8, 0.1, 3.7e6};
+constexpr Rates kOfLinearGradients = {{1.0, 0.65, 0.41}, 0.8, 7.4, 2.6, 60e6};
+
 inline int64_t linear_ld(int64_t out) { return (out + 3) / 4 * 4; } // rows of z, of dz and of parts' sums start on 16 bytes
 
 struct LinearForwardPlan {
     bool thin;
     Choice tile;
     LinearForwardPlan(int n, int64_t rows, int64_t width, int64_t out)
-        : thin(rows <= kThinRows), tile(choose(kOfDown, n, out, rows, width, 1, n * rows * out))
+        : thin(rows <= kThinRows), tile(choose(kOfLinear, n, out, rows, width, 1, n * rows * out))
     {
         if (thin) tile.parts = 1;
     }
@@ -33,10 +38,10 @@ struct LinearBackwardPlan {
             if (!launchable((TileKind)kd, blocks_for(params) + blocks_for(input))) continue;
             for (int pp = 1; pp <= 32 && (pp == 1 || (rows / pp >= 4 * kTileK && params * pp <= 1024)); pp *= 2)
                 for (int ip = 1; ip <= 32 && (ip == 1 || (out / ip >= 4 * kTileK && input * ip <= 1024)); ip *= 2) {
-                    const double of_params = steps_of(kOfGradients, rows, pp), of_input = steps_of(kOfGradients, out, ip);
-                    const double c = launch_cost(kOfGradients, (TileKind)kd, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
+                    const double of_params = steps_of(kOfLinearGradients, rows, pp), of_input = steps_of(kOfLinearGradients, out, ip);
+                    const double c = launch_cost(kOfLinearGradients, (TileKind)kd, params * pp + input * ip, (double)(params * pp) * of_params + (double)(input * ip) * of_input,
                                                  of_params > of_input ? of_params : of_input) +
-                                     reduce_cost(kOfGradients, pp, n * width * out) + reduce_cost(kOfGradients, ip, n * rows * width);
+                                     reduce_cost(kOfLinearGradients, pp, n * width * out) + reduce_cost(kOfLinearGradients, ip, n * rows * width);
                     if (c < least) {
                         least = c;
                         kind = (TileKind)kd;

@@ -70,7 +70,7 @@ RotaryArgs args_of(const svgd_rotary &p, int64_t most)
     a.blocks = (int)((a.tokens + a.per - 1) / a.per);
     return a;
 }
-constexpr int64_t kForwardBlocks = 2048, kBackwardBlocks = 2048;
+constexpr int64_t kForwardBlocks = 2048, kBackwardBlocks = 768;
 
 struct Reads { // besides the activations
     Extent e[4];
