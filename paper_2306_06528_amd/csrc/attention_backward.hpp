@@ -45,7 +45,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 
     Frag<T> qf[QB][KD], df[QB][KD];
     int limit[QB], position[QB], document[QB];
-    float slope[QB], log[QB], del[QB];
+    float slope[QB], log[QB];
+    f32x4 less[QB];
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int r = min(own + 16 * b + (lane & 15), a.rows - 1), i = a.query(r), h = at.head * a.group + r - i * a.group;
@@ -62,15 +63,16 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         const int64_t line = a.line(at.particle, at.batch, h, i);
         log[b] = lse[line] == -INFINITY ? INFINITY : lse[line] * kLog2e; // (a row that sees nothing: every probability 0)
         const T *const op = o.at(at.particle, at.batch, h) + i * o.token;
-        del[b] = 0.f;
+        float del = 0.f;
 #pragma unroll
         for (int s = 0; s < KD; ++s) {
             const Frag<T> f = load_frag(op + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) del[b] += (float)f[e] * (float)df[b][s][e];
+            for (int e = 0; e < 8; ++e) del += (float)f[e] * (float)df[b][s][e];
         }
-        del[b] = sum_over_rows(del[b]);
-        if (g == 0 && at.part == 0 && own + 16 * b + (lane & 15) < a.rows) delta[line] = del[b];
+        del = sum_over_rows(del);
+        less[b] = f32x4{-del, -del, -del, -del};
+        if (g == 0 && at.part == 0 && own + 16 * b + (lane & 15) < a.rows) delta[line] = del;
     }
     const int last_row = min(first + 16 * QB * kAttnWaves, a.rows) - 1;
     const int p0 = masks.start + a.query(first), p1 = masks.start + a.query(last_row);
@@ -128,7 +130,10 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) s[j][b] = dp[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int b = 0; b < QB; ++b) {
+                        s[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        dp[j][b] = less[b]; // dP - delta, from the start
+                    }
 #pragma unroll
                     for (int c = 0; c < KD; ++c) {
                         const Frag<T> f = TL::rows(kl, 32 * m + 16 * j, 32 * c), e = TL::rows(vl, 32 * m + 16 * j, 32 * c);
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                                 if constexpr (MOD) x = modified.exponent(t, slope[b], far);
                                 if (masked && (at_key >= limit[b] || doc != document[b])) x = -INFINITY;
                                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
-                                float dz = p * (dp[j][b][e] - del[b]);
+                                float dz = p * dp[j][b][e];
                                 if constexpr (MOD) {
                                     sum_dz[b] += dz;
                                     sum_dz_far[b] += dz * far;
@@ -238,7 +243,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 
 // What a streamed row brings besides its values.
 struct __attribute__((aligned(16))) RowInfo {
-    float log[kTileRows], delta[kTileRows], slope[kTileRows];
+    float log[kTileRows], less[kTileRows], slope[kTileRows];
     int limit[kTileRows], position[kTileRows], document[kTileRows];
 };
 
@@ -248,6 +253,10 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 {
     constexpr int KD = kBlocks32<KDX>;
     typedef Tile64<T, KD, KDX == 0> TL;
+    // Two waves to a SIMD hide little of what a wave waits for: operands are asked for well before their products, where the compiler, short of registers, asks for a few at a time and waits for each (4 x 2 x 4,096
+    // x 16 heads of 64 bf16 causal 915 us, so 875; with one block of keys, three waves, the registers are worth more: 8 x 8 x 197 x 6 heads of 64 35 us, so 43).
+    constexpr bool kDeep = sizeof(T) == 2 && (KB == 2 || KD > 2);
+    constexpr int kEarly = kDeep ? (KD <= 2 ? 2 * KD : 4) : 0; // transposed operands that are asked for before the exponentials
     constexpr bool kHalf = std::is_same<T, f16_t>::value;
     constexpr float kExponent = kHalf ? 14.f : 0.f; // of probabilities as operands
     __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
@@ -354,7 +363,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         if (threadIdx.x < kTileRows) {
             RowInfo &info = infos[half];
             info.log[threadIdx.x] = next_log;
-            info.delta[threadIdx.x] = next_delta;
+            info.less[threadIdx.x] = -next_delta;
             info.slope[threadIdx.x] = next_slope;
             info.limit[threadIdx.x] = next_limit;
             info.position[threadIdx.x] = next_position;
@@ -379,25 +388,39 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                 f32x4 s[2][KB], dp[2][KB];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) s[j][b] = dp[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    Frag<T> f[KD], e[KD];
+                    const f32x4 less = *reinterpret_cast<const f32x4 *>(&info.less[32 * m + 16 * j + 4 * g]);
 #pragma unroll
                     for (int c = 0; c < KD; ++c) {
-                        const Frag<T> f = TL::rows(ql, 32 * m + 16 * j, 32 * c), e = TL::rows(dl, 32 * m + 16 * j, 32 * c);
+                        f[c] = TL::rows(ql, 32 * m + 16 * j, 32 * c);
+                        e[c] = TL::rows(dl, 32 * m + 16 * j, 32 * c);
+                    }
+                    if constexpr (kDeep)
+                        if (j == 0 || KD > 2) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int b = 0; b < KB; ++b) {
+                        s[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        dp[j][b] = less; // dP - delta, from the start
+                    }
+#pragma unroll
+                    for (int c = 0; c < KD; ++c)
 #pragma unroll
                         for (int b = 0; b < KB; ++b) {
-                            s[j][b] = mma(f, kf[b][c], s[j][b]);
-                            dp[j][b] = mma(e, vf[b][c], dp[j][b]);
+                            s[j][b] = mma(f[c], kf[b][c], s[j][b]);
+                            dp[j][b] = mma(e[c], vf[b][c], dp[j][b]);
                         }
-                    }
                 }
+                Frag<T> dc[kEarly + 1];
+#pragma unroll
+                for (int d = 0; d < kEarly; ++d) dc[d] = TL::columns(dl, 32 * m, 16 * d);
+                if constexpr (kDeep) __builtin_amdgcn_sched_barrier(0);
                 if constexpr (MOD) modified.template apply<T>(s);
                 float largest = 0.f;
                 const auto gradients = [&](auto hidden) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int r = 32 * m + 16 * j + 4 * g;
-                        const f32x4 log = *reinterpret_cast<const f32x4 *>(&info.log[r]), del = *reinterpret_cast<const f32x4 *>(&info.delta[r]);
+                        const f32x4 log = *reinterpret_cast<const f32x4 *>(&info.log[r]);
                         [[maybe_unused]] const f32x4 slope = *reinterpret_cast<const f32x4 *>(&info.slope[r]);
                         [[maybe_unused]] const i32x4 limit = *reinterpret_cast<const i32x4 *>(&info.limit[r]), position = *reinterpret_cast<const i32x4 *>(&info.position[r]),
                                                      documents = *reinterpret_cast<const i32x4 *>(&info.document[r]);
@@ -410,7 +433,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                                 if constexpr (MOD) x = modified.exponent(t, slope[e], fabsf((float)(position[e] - key[b])));
                                 if (hidden && (key[b] >= limit[e] || document[b] != documents[e])) x = -INFINITY;
                                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, kExponent - log[e]));
-                                float dz = p * (dp[j][b][e] - del[e]);
+                                float dz = p * dp[j][b][e];
                                 if constexpr (MOD) dz *= modified.damp(t);
                                 s[j][b][e] = p;
                                 dp[j][b][e] = dz;
@@ -441,15 +464,26 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                     p[b] = as_operand<T>(s[0][b], s[1][b]);
                     as_parts<T>(dp[0][b], dp[1][b], sc, z[b]);
                 }
+                constexpr int kAtOnce = !kDeep ? 1 : KD <= 2 ? 2 * KD : KD; // operands
 #pragma unroll
-                for (int d = 0; d < 2 * KD; ++d) {
-                    const Frag<T> f = TL::columns(dl, 32 * m, 16 * d), e = TL::columns(ql, 32 * m, 16 * d);
+                for (int d0 = 0; d0 < 2 * KD; d0 += kAtOnce) {
+                    Frag<T> f[kAtOnce], e[kAtOnce];
 #pragma unroll
-                    for (int b = 0; b < KB; ++b) acc_v[d][b] = mma(f, p[b], acc_v[d][b]);
+                    for (int d = 0; d < kAtOnce; ++d) {
+                        f[d] = d0 + d < kEarly ? dc[d0 + d < kEarly ? d0 + d : kEarly] : TL::columns(dl, 32 * m, 16 * (d0 + d));
+                        e[d] = TL::columns(ql, 32 * m, 16 * (d0 + d));
+                    }
+                    if constexpr (kDeep) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int part = 0; part < kZParts<T>; ++part)
+                    for (int d = 0; d < kAtOnce; ++d)
 #pragma unroll
-                        for (int b = 0; b < KB; ++b) acc_k[d][b] = mma(e, z[b][part], acc_k[d][b]);
+                        for (int b = 0; b < KB; ++b) acc_v[d0 + d][b] = mma(f[d], p[b], acc_v[d0 + d][b]);
+#pragma unroll
+                    for (int d = 0; d < kAtOnce; ++d)
+#pragma unroll
+                        for (int part = 0; part < kZParts<T>; ++part)
+#pragma unroll
+                            for (int b = 0; b < KB; ++b) acc_k[d0 + d][b] = mma(e[d], z[b][part], acc_k[d0 + d][b]);
                 }
             }
         half ^= 1;

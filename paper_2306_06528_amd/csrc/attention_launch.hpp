@@ -25,14 +25,22 @@ inline int64_t small_blocks(const AttnArgs &a, int64_t size) { return (int64_t)a
 // 21 / 18 and 457 / 392, keys 34.7 / 40 and 999 / 915; with queries of their own, which two blocks cost more registers, 27.9 / 30.3 and 671 / 684, so always one.
 constexpr int64_t kManyForward = 1024, kManyKeys = 4096;
 
-// Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards.
+// Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards: as many as make the shortest way of a workgroup's tiles, the time until its first one
+// is there (one tile's) and, with parts, the sums' own launch, times the rounds of kAtATime workgroups.  (3 x 2 x 333 x 6 heads of 40 fp32, 192 workgroups of 6 tiles: 3 parts, which make two rounds, 20 us, 2 parts 15.)
+constexpr int64_t kAtATime = 512;
 inline int parts_for(const AttnArgs &a, int64_t own, int64_t streamed)
 {
     const int64_t blocks = small_blocks(a, own), tiles = ceil_div(streamed, kTileRows);
-    if (blocks >= 384 || blocks == 0 || tiles < 4) return 1;
-    const int64_t most = tiles / 2, wanted = ceil_div(512, blocks);
-    const int64_t parts = wanted < most ? wanted : most;
-    return (int)(parts > 64 ? 64 : parts);
+    if (blocks == 0 || blocks >= kAtATime) return 1;
+    int64_t best = 1, least = tiles + 1;
+    for (int64_t parts = 2; parts <= 64 && 2 * parts <= tiles; ++parts) {
+        const int64_t cost = ceil_div(blocks * parts, kAtATime) * (ceil_div(tiles, parts) + 1) + 1;
+        if (cost < least) {
+            least = cost;
+            best = parts;
+        }
+    }
+    return (int)best;
 }
 constexpr int64_t kFewBlocks = 1024;
 inline bool few_rows(const AttnArgs &a) { return a.rows <= 16; }

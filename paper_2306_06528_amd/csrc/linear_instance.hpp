@@ -61,8 +61,9 @@ template <> int linear_backward<SVGD_LINEAR_TYPE>(const LinearCall &c, const Lin
     const bool act = c.s.activation != SVGD_NO_ACTIVATION, products = (c.dx.data && c.s.rows > 0) || c.dweight.p;
     if (c.s.rows > 0 && ((act && products) || c.dbias.p)) {
         const int groups = (int)tiles(c.s.out, 256);
-        linear_slope_kernel<T><<<c.s.n * plan.sums * groups, 256, 0, c.stream>>>(c.s, plan.sum_rows, plan.sums, groups, in<T>(c.dy), act ? c.z : nullptr, products ? dz : nullptr, sums,
-                                                                                   c.dbias, c.accumulate);
+        const int blocks = c.s.n * plan.sums * groups;
+        if (act) linear_slope_kernel<T, true><<<blocks, 256, 0, c.stream>>>(c.s, plan.sum_rows, plan.sums, groups, in<T>(c.dy), c.z, products ? dz : nullptr, sums, c.dbias, c.accumulate);
+        else linear_slope_kernel<T, false><<<blocks, 256, 0, c.stream>>>(c.s, plan.sum_rows, plan.sums, groups, in<T>(c.dy), nullptr, nullptr, sums, c.dbias, c.accumulate);
         if (const int rc = launched()) return rc;
     }
     if (c.dbias.p && (plan.sums > 1 || (c.s.rows == 0 && !c.accumulate))) { // (the sum over no rows is 0)

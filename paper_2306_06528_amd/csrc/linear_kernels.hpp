@@ -176,7 +176,7 @@ template <class T, int JB> SVGD_THIN_KERNEL void thin_linear_kernel(LinearShape 
 
 // dz (null: not wanted) of some rows, and the sums of their columns (null: not wanted) to sums[part][particle][out], or where there is one part to the bias's gradient: 64 lanes have four columns
 // each, the four waves every fourth row.
-template <class T>
+template <class T, bool ACT>
 __global__ __launch_bounds__(256) void linear_slope_kernel(LinearShape s, int64_t per, int parts, int groups, Rows<const T> dy, const float *z, float *dz, float *sums, Params dbias,
                                                            bool accumulate)
 {
@@ -190,11 +190,12 @@ __global__ __launch_bounds__(256) void linear_slope_kernel(LinearShape s, int64_
     const int left = s.out - i < 4 ? (int)(s.out - i) : 4;
     f32x4 total = {0.f, 0.f, 0.f, 0.f};
     if (left > 0) {
-#pragma unroll 2
+        constexpr int U = ACT ? 2 : 8;
+#pragma unroll U
         for (int64_t j = part * per + wave; j < last; j += 4) {
             float g[4];
             load_pack<T, 4>(dy.p + particle * dy.particle + j * dy.row + i, left, g);
-            if (z) {
+            if constexpr (ACT) {
                 const int64_t at = (particle * s.rows + j) * s.out_ld + i;
                 const f32x4 zv = *reinterpret_cast<const f32x4 *>(z + at);
                 f32x4 d;
