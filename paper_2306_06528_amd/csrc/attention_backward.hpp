@@ -18,22 +18,24 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
     const int64_t token = k / a.heads;
     const int i = (int)(token % a.t), b = (int)(token / a.t % a.batch), particle = (int)(token / a.t / a.batch);
     const int c = 8 * (threadIdx.x & 15);
-    const Frag<T> x = load_frag(o.at(particle, b, h) + i * o.token + c, a.dim - c), y = load_frag(d_o.at(particle, b, h) + i * d_o.token + c, a.dim - c);
+    const SplitConst sc = split_const();
+    const Frag<T> x = load_frag(o.at(particle, b, h) + i * o.token + c, a.dim - c, sc), y = load_frag(d_o.at(particle, b, h) + i * d_o.token + c, a.dim - c, sc);
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += (float)x[e] * (float)y[e];
+    for (int e = 0; e < 8; ++e) sum += value_of<T>(x, e) * value_of<T>(y, e);
     sum = row_sum(sum);
     if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
 }
 
 template <class T, int KDX, int QB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
                                                                                                               Heads<const T> o, const float *lse, float *delta, Heads<T> dq, float *slope_rows, float *partial)
 {
     constexpr int KD = kBlocks32<KDX>;
-    typedef Tile64<T, KD, KDX == 0> TL;
-    __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
-    __shared__ int red[4], key_documents[2][kTileRows];
+    typedef Streamed<T, KD, KDX == 0> TL;
+    constexpr int kRows = TL::kRows, kBuffers = kHalves<T, KD>;
+    __shared__ __attribute__((aligned(16))) typename TL::elem lds[2 * kBuffers * TL::kSize];
+    __shared__ int red[4], key_documents[kBuffers][kRows];
     const AttnBlock at(a);
     if (!at.any) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
@@ -42,6 +44,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     const Masks masks(a, at.batch);
     const float mul = MOD ? 1.f : a.scale * kLog2e;
     const Modified modified(a);
+    const SplitConst sc = split_const();
 
     Frag<T> qf[QB][KD], df[QB][KD];
     int limit[QB], position[QB], document[QB];
@@ -53,8 +56,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         const T *const p = q.at(at.particle, at.batch, h) + i * q.token, *const d = d_o.at(at.particle, at.batch, h) + i * d_o.token;
 #pragma unroll
         for (int s = 0; s < KD; ++s) {
-            qf[b][s] = load_frag(p + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
-            df[b][s] = load_frag(d + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+            qf[b][s] = load_frag(p + 32 * s + 8 * g, a.dim - 32 * s - 8 * g, sc);
+            df[b][s] = load_frag(d + 32 * s + 8 * g, a.dim - 32 * s - 8 * g, sc);
         }
         position[b] = masks.start + i;
         limit[b] = masks.end(a, position[b]);
@@ -66,9 +69,9 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         float del = 0.f;
 #pragma unroll
         for (int s = 0; s < KD; ++s) {
-            const Frag<T> f = load_frag(op + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+            const Frag<T> f = load_frag(op + 32 * s + 8 * g, a.dim - 32 * s - 8 * g, sc);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) del += (float)f[e] * (float)df[b][s][e];
+            for (int e = 0; e < 8; ++e) del += value_of<T>(f, e) * value_of<T>(df[b][s], e);
         }
         del = sum_over_rows(del);
         less[b] = f32x4{-del, -del, -del, -del};
@@ -79,7 +82,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     int lo = 0, hi = masks.documents ? (p1 < 0 || p0 >= a.s ? 0 : masks.end(a, min(p1, a.s - 1))) : masks.end(a, p1);
     const int free_keys = masks.documents ? 0 : masks.end(a, p0);
     if (masks.documents) narrow(masks.documents, p0, p1, a.s, red, lo, hi);
-    int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
+    int begin = lo / kRows, end = (hi + kRows - 1) / kRows;
     part_of(a, at.part, begin, end);
     const int wave_row = min(own + 16 * QB, a.rows) - 1;
     const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
@@ -87,7 +90,6 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     f32x4 acc[2 * KD][QB];
     float sum_dz[QB], sum_dz_far[QB], sum_far[QB]; // of dz, dz distance and P distance
     BlockScale bs;
-    const SplitConst sc = split_const();
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         sum_dz[b] = sum_dz_far[b] = sum_far[b] = 0.f;
@@ -101,15 +103,15 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     TL::offsets(v_at, a.dim, [&](int i) { return (uint32_t)i * (uint32_t)v.token; });
     int next_document = 0;
     const auto fetch = [&](int tile_of) {
-        const int key = tile_of * kTileRows, last = min(hi - key, kTileRows) - 1;
+        const int key = tile_of * kRows, last = min(hi - key, kRows) - 1;
         kt.load(ks + key * k.token, k_at, (uint32_t)k.token, last, a.dim);
         vt.load(vs + key * v.token, v_at, (uint32_t)v.token, last, a.dim);
-        if (masks.documents && threadIdx.x < kTileRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
+        if (masks.documents && threadIdx.x < kRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
     };
     const auto stage = [&](int half, int tile_of) {
-        kt.store(lds + half * 2 * TL::kSize, hi - tile_of * kTileRows, a.dim);
-        vt.store(lds + (half * 2 + 1) * TL::kSize, hi - tile_of * kTileRows, a.dim);
-        if (masks.documents && threadIdx.x < kTileRows) key_documents[half][threadIdx.x] = next_document;
+        kt.store(lds + half * 2 * TL::kSize, hi - tile_of * kRows, a.dim, sc);
+        vt.store(lds + (half * 2 + 1) * TL::kSize, hi - tile_of * kRows, a.dim, sc);
+        if (masks.documents && threadIdx.x < kRows) key_documents[half][threadIdx.x] = next_document;
     };
     if (begin < end) {
         fetch(begin);
@@ -120,11 +122,11 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     int half = 0;
     for (int n = begin; n < end; ++n) {
         if (n + 1 < end) fetch(n + 1);
-        const int key0 = n * kTileRows;
+        const int key0 = n * kRows;
         if (key0 < wave_limit) {
-            const T *const kl = lds + half * 2 * TL::kSize, *const vl = kl + TL::kSize;
+            const typename TL::elem *const kl = lds + half * 2 * TL::kSize, *const vl = kl + TL::kSize;
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
+            for (int m = 0; m < kRows / 32; ++m) {
                 const int key = key0 + 32 * m;
                 f32x4 s[2][QB], dp[2][QB];
 #pragma unroll
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                             }
                         }
                 };
-                if (key0 + kTileRows > free_keys) gradients(std::true_type{});
+                if (key0 + kRows > free_keys) gradients(std::true_type{});
                 else gradients(std::false_type{});
                 if constexpr (std::is_same<T, f16_t>::value) {
                     const float factor = bs.take(largest);
@@ -201,7 +203,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                 }
             }
         }
-        half ^= 1;
+        if constexpr (kBuffers == 2) half ^= 1;
+        else __syncthreads(); // (the tile has been read)
         if (n + 1 < end) stage(half, n + 1);
         __syncthreads();
     }
@@ -248,19 +251,20 @@ struct __attribute__((aligned(16))) RowInfo {
 };
 
 template <class T, int KDX, int KB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
                                                                                                            const float *lse, const float *delta, Heads<T> dk, Heads<T> dv, float *partial)
 {
     constexpr int KD = kBlocks32<KDX>;
-    typedef Tile64<T, KD, KDX == 0> TL;
+    typedef Streamed<T, KD, KDX == 0> TL;
+    constexpr int kRows = TL::kRows, kBuffers = kHalves<T, KD>;
     // Two waves to a SIMD hide little of what a wave waits for: operands are asked for well before their products, where the compiler, short of registers, asks for a few at a time and waits for each (4 x 2 x 4,096
     // x 16 heads of 64 bf16 causal 915 us, so 875; with one block of keys, three waves, the registers are worth more: 8 x 8 x 197 x 6 heads of 64 35 us, so 43).
     constexpr bool kDeep = sizeof(T) == 2 && (KB == 2 || KD > 2);
     constexpr int kEarly = kDeep ? (KD <= 2 ? 2 * KD : 4) : 0; // transposed operands that are asked for before the exponentials
     constexpr bool kHalf = std::is_same<T, f16_t>::value;
     constexpr float kExponent = kHalf ? 14.f : 0.f; // of probabilities as operands
-    __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
-    __shared__ RowInfo infos[2];
+    __shared__ __attribute__((aligned(16))) typename TL::elem lds[2 * kBuffers * TL::kSize];
+    __shared__ RowInfo infos[kBuffers];
     __shared__ int red[4];
     const AttnBlock at(a);
     if (!at.any) return;
@@ -269,6 +273,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     const Masks masks(a, at.batch);
     const float mul = MOD ? 1.f : a.scale * kLog2e;
     const Modified modified(a);
+    const SplitConst sc = split_const();
 
     Frag<T> kf[KB][KD], vf[KB][KD];
     int key[KB], document[KB];
@@ -280,8 +285,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 #pragma unroll
         for (int s = 0; s < KD; ++s) {
             const int left = there ? a.dim - 32 * s - 8 * g : 0;
-            kf[b][s] = load_frag(kp + 32 * s + 8 * g, left);
-            vf[b][s] = load_frag(vp + 32 * s + 8 * g, left);
+            kf[b][s] = load_frag(kp + 32 * s + 8 * g, left, sc);
+            vf[b][s] = load_frag(vp + 32 * s + 8 * g, left, sc);
         }
         document[b] = masks.documents && there ? masks.documents[key[b]] : 0;
     }
@@ -295,7 +300,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         row_lo = hi > lo ? max(row_lo, (lo - masks.start) * a.group) : 0;
         row_hi = hi > lo ? min(a.rows, (hi - masks.start) * a.group) : 0;
     }
-    int begin = row_lo / kTileRows, end = row_hi > row_lo ? (row_hi + kTileRows - 1) / kTileRows : begin;
+    int begin = row_lo / kRows, end = row_hi > row_lo ? (row_hi + kRows - 1) / kRows : begin;
     part_of(a, at.part, begin, end);
     // tiles from this row on need no mask
     const int wave_last = own + 16 * KB - 1;
@@ -305,14 +310,13 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 
     f32x4 acc_k[2 * KD][KB], acc_v[2 * KD][KB];
     BlockScale bs;
-    const SplitConst sc = split_const();
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int d = 0; d < 2 * KD; ++d) acc_k[d][b] = acc_v[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     TL qt, dt;
     // (tiles begin with a token's first head where the heads of a group divide 64: then the rows of all tiles lie alike)
-    const bool steady = kTileRows % a.group == 0;
+    const bool steady = kRows % a.group == 0;
     uint32_t q_at[TL::N], d_at[TL::N];
     const auto place = [&](int j, int64_t token, int64_t head) {
         const int i = a.query(j);
@@ -323,10 +327,10 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     float next_log = 0.f, next_delta = 0.f, next_slope = 0.f;
     int next_limit = 0, next_position = 0, next_document = 0;
     const auto fetch = [&](int tile_of) {
-        const int row = tile_of * kTileRows;
-        const int i0 = a.query(row), h0 = row - i0 * a.group, last = min(a.rows - row, kTileRows) - 1;
+        const int row = tile_of * kRows;
+        const int i0 = a.query(row), h0 = row - i0 * a.group, last = min(a.rows - row, kRows) - 1;
         const T *const qs = q.at(at.particle, at.batch, at.head * a.group) + i0 * q.token, *const ds = d_o.at(at.particle, at.batch, at.head * a.group) + i0 * d_o.token;
-        if (steady && last == kTileRows - 1) {
+        if (steady && last == kRows - 1) {
             qt.load(qs, q_at, a.dim);
             dt.load(ds, d_at, a.dim);
         } else {
@@ -340,7 +344,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
             TL::offsets(to, a.dim, [&](int j) { return row_at(j, d_o.token, d_o.head); });
             dt.load(ds, to, a.dim);
         }
-        if (threadIdx.x < kTileRows) {
+        if (threadIdx.x < kRows) {
             const int r = row + (int)threadIdx.x;
             next_log = INFINITY;
             next_delta = next_slope = 0.f;
@@ -358,9 +362,9 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         }
     };
     const auto stage = [&](int half, int tile_of) {
-        qt.store(lds + half * 2 * TL::kSize, a.rows - tile_of * kTileRows, a.dim);
-        dt.store(lds + (half * 2 + 1) * TL::kSize, a.rows - tile_of * kTileRows, a.dim);
-        if (threadIdx.x < kTileRows) {
+        qt.store(lds + half * 2 * TL::kSize, a.rows - tile_of * kRows, a.dim, sc);
+        dt.store(lds + (half * 2 + 1) * TL::kSize, a.rows - tile_of * kRows, a.dim, sc);
+        if (threadIdx.x < kRows) {
             RowInfo &info = infos[half];
             info.log[threadIdx.x] = next_log;
             info.less[threadIdx.x] = -next_delta;
@@ -379,12 +383,12 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     int half = 0;
     for (int n = begin; n < end; ++n) {
         if (n + 1 < end) fetch(n + 1);
-        const T *const ql = lds + half * 2 * TL::kSize, *const dl = ql + TL::kSize;
+        const typename TL::elem *const ql = lds + half * 2 * TL::kSize, *const dl = ql + TL::kSize;
         const RowInfo &info = infos[half];
-        const bool masked = n * kTileRows < free_row;
+        const bool masked = n * kRows < free_row;
         if (own < masks.length)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
+            for (int m = 0; m < kRows / 32; ++m) {
                 f32x4 s[2][KB], dp[2][KB];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
@@ -461,7 +465,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                 Frag<T> p[KB], z[KB][kZParts<T>];
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
-                    p[b] = as_operand<T>(s[0][b], s[1][b]);
+                    p[b] = as_operand<T>(s[0][b], s[1][b], sc);
                     as_parts<T>(dp[0][b], dp[1][b], sc, z[b]);
                 }
                 constexpr int kAtOnce = !kDeep ? 1 : KD <= 2 ? 2 * KD : KD; // operands
@@ -486,7 +490,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                             for (int b = 0; b < KB; ++b) acc_k[d0 + d][b] = mma(e[d], z[b][part], acc_k[d0 + d][b]);
                 }
             }
-        half ^= 1;
+        if constexpr (kBuffers == 2) half ^= 1;
+        else __syncthreads(); // (the tile has been read)
         if (n + 1 < end) stage(half, n + 1);
         __syncthreads();
     }

@@ -66,58 +66,68 @@ struct AttnBlock {
 // ---------------------------------------------------------------------------------------------
 // operands
 // ---------------------------------------------------------------------------------------------
+// Eight values of k of one row, lane l: row l % 16, group l / 16 of k.  16-bit values are as they are; fp32 ones three bf16 parts whose sum is the value exactly (split3): the products of parts that are not below 2^-24 of the
+// whole, six, take 96 cycles of a matrix core for 32 values of k, where the fp32 matrix instructions take 256.
 template <class T> struct FragOf {
     typedef T type __attribute__((ext_vector_type(8)));
 };
-template <class T> using Frag = typename FragOf<T>::type; // eight values of k of one row, lane l: row l % 16, group l / 16 of k
+template <> struct FragOf<float> {
+    typedef Split3 type;
+};
+template <class T> using Frag = typename FragOf<T>::type;
+template <class T> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
 
 __device__ __forceinline__ f32x4 mma(Frag<bf16_t> a, Frag<bf16_t> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma(Frag<f16_t> a, Frag<f16_t> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 mma(Frag<float> a, Frag<float> b, f32x4 c)
+__device__ __forceinline__ f32x4 mma(const Split3 &a, const Split3 &b, f32x4 c)
 {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
-    return c;
+    c = mma(a.l, b.h, c);
+    c = mma(a.m, b.m, c);
+    c = mma(a.h, b.l, c);
+    c = mma(a.m, b.h, c);
+    c = mma(a.h, b.m, c);
+    return mma(a.h, b.h, c);
 }
 
-// Heads of less than 16 bytes have kernels of their own, numbered 0: blocks of 32 values, loaded one by one.
+template <class T> __device__ __forceinline__ float value_of(const Frag<T> &f, int e)
+{
+    if constexpr (sizeof(T) == 4) return (float)f.h[e] + ((float)f.m[e] + (float)f.l[e]);
+    else return (float)f[e];
+}
+
+// Heads of less than eight values have kernels of their own, numbered 0: blocks of 32 values, loaded one by one.
 template <int KDX> constexpr int kBlocks32 = KDX ? KDX : 1;
 
 // Eight values from memory, those from `left` on 0 and not read.
-template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int left)
+template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int left, const SplitConst &sc)
 {
-    Frag<T> f;
-    constexpr int W = 16 / sizeof(T);
+    typename Pack<T, 8>::raw v;
     if (left >= 8) {
-#pragma unroll
-        for (int q = 0; q < 8; q += W) {
-            const typename Pack<T, W>::raw r = *reinterpret_cast<const typename Pack<T, W>::type *>(p + q);
-#pragma unroll
-            for (int e = 0; e < W; ++e) f[q + e] = r[e];
-        }
+        v = *reinterpret_cast<const typename Pack<T, 8>::type *>(p);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            f[e] = (T)0.f;
-            if (e < left) f[e] = p[e];
+            v[e] = (T)0.f;
+            if (e < left) v[e] = p[e];
         }
     }
-    return f;
+    if constexpr (sizeof(T) == 4) return split3(f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]}, sc);
+    else return v;
 }
 
-// Rows of up to 32 KD values in LDS, as they are in memory, 16 bytes at a time.  Which place of its row such a piece takes is permuted so that neither the same piece of 16 rows (`rows`) nor 32 bytes of
-// eight rows in succession (`columns`, what 32 lanes read at a time) meet in a bank, of which there are 64.  (fp32 heads of up to 32 or of 65 to 96 values: `columns` meet in pairs.)
-// TINY: heads of less than 16 bytes.
-// ROWS rows, brought by THREADS threads, neighbours in the workgroup.
+// ROWS rows of up to 32 KD values in LDS, eight values at a time, brought by THREADS threads, neighbours in the workgroup; of fp32 values three planes of parts, made on the way.  Which place of its row such a piece
+// takes is permuted so that neither the same piece of 16 rows (`rows`) nor 32 bytes of eight rows in succession (`columns`, what 32 lanes read at a time) meet in a bank, of which there are 64.
+// TINY: heads of less than eight values.
 template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
-    static constexpr int VEC = 16 / sizeof(T), kChunks = 32 * KD / VEC, kSize = ROWS * 32 * KD, N = ROWS * kChunks / THREADS;
+    typedef typename std::conditional<sizeof(T) == 4, bf16_t, T>::type elem; // in LDS
+    static constexpr int VEC = 8, kRows = ROWS, kChunks = 32 * KD / VEC, kPlane = ROWS * 32 * KD, kSize = kPlanes<T> * kPlane, N = ROWS * kChunks / THREADS;
+    static_assert(N * THREADS == ROWS * kChunks, "every thread has as many pieces");
     typedef typename Pack<T, VEC>::raw raw;
     raw v[N];
-    static __device__ __forceinline__ int place(int row, int chunk) // in 16 bytes; moves with the row by 16
+    static __device__ __forceinline__ int place(int row, int chunk) // in eight values; moves with the row by 16
     {
         int f;
-        if constexpr (sizeof(T) == 4) f = KD % 2 ? (row >> 1) & 7 : row & 15;
-        else if constexpr (KD == 4) f = ((row & 7) << 1) | ((row >> 3) & 1);
+        if constexpr (KD == 4) f = ((row & 7) << 1) | ((row >> 3) & 1);
         else if constexpr (KD == 2) f = (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
         else f = (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
         return row * kChunks + (chunk ^ f);
@@ -166,7 +176,7 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
         }
     }
     // What is not there becomes 0 on its way.
-    __device__ __forceinline__ void store(T *lds, int count, int dim)
+    __device__ __forceinline__ void store(elem *lds, int count, int dim, const SplitConst &sc)
     {
         if (!TINY && dim % VEC) {
             const int by = VEC - dim % VEC;
@@ -190,48 +200,51 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
                     if (row_of(u) >= count || chunk_of(u) * VEC + e >= dim) v[u][e] = (T)0.f;
         }
 #pragma unroll
-        for (int u = 0; u < N; ++u) reinterpret_cast<raw *>(lds)[place(row_of(u), chunk_of(u))] = v[u];
+        for (int u = 0; u < N; ++u) {
+            Frag<elem> *const to = reinterpret_cast<Frag<elem> *>(lds) + place(row_of(u), chunk_of(u));
+            if constexpr (sizeof(T) == 4) {
+                const Split3 x = split3(f32x4{v[u][0], v[u][1], v[u][2], v[u][3]}, f32x4{v[u][4], v[u][5], v[u][6], v[u][7]}, sc);
+                to[0] = x.h;
+                to[kPlane / 8] = x.m;
+                to[2 * (kPlane / 8)] = x.l;
+            } else {
+                *to = v[u];
+            }
+        }
     }
     // operand of rows row .. row + 15, values col .. col + 31
-    static __device__ __forceinline__ Frag<T> rows(const T *lds, int row, int col)
+    static __device__ __forceinline__ Frag<T> rows(const elem *lds, int row, int col)
     {
         const int lane = threadIdx.x & 63;
-        const raw *const p = reinterpret_cast<const raw *>(lds) + row * kChunks;
-        Frag<T> f;
-#pragma unroll
-        for (int q = 0; q < 8; q += VEC) {
-            const raw r = p[place(lane & 15, (col + q) / VEC + (lane >> 4) * (8 / VEC))];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[q + e] = r[e];
-        }
-        return f;
+        const Frag<elem> *const p = reinterpret_cast<const Frag<elem> *>(lds) + row * kChunks + place(lane & 15, col / VEC + (lane >> 4));
+        if constexpr (sizeof(T) == 4) return {p[0], p[kPlane / 8], p[2 * (kPlane / 8)]};
+        else return *p;
     }
     // operand of values col .. col + 15 (its rows), rows row .. row + 31 (its k, ordered 4 g + 0 .. 3, 16 + 4 g + 0 .. 3)
-    static __device__ __forceinline__ Frag<T> columns(const T *lds, int row, int col)
+    static __device__ __forceinline__ Frag<T> columns(const elem *lds, int row, int col)
     {
         const int lane = threadIdx.x & 63, g = lane >> 4;
-        Frag<T> f;
-        if constexpr (sizeof(T) == 2) {
-            // (16 lanes read 4 rows of 16 values, a lane the four values of the rows' column lane % 16)
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) s16x4 lds16x4;
-            typedef T t4 __attribute__((ext_vector_type(4)));
-            const T *const p = lds + row * 32 * KD + place(4 * g + ((lane & 15) >> 2), col / VEC + ((lane & 3) >> 1)) * VEC + 4 * (lane & 1);
-            const t4 lo = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p));
-            const t4 hi = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * 32 * KD)));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f[e] = lo[e];
-                f[4 + e] = hi[e];
-            }
-        } else {
-            const T *const p = lds + row * 32 * KD + (lane & 3);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = p[place(4 * g + (e & 3), col / VEC + ((lane & 15) >> 2)) * VEC + (e >> 2) * 16 * 32 * KD];
-        }
-        return f;
+        // (16 lanes read 4 rows of 16 values, a lane the four values of the rows' column lane % 16)
+        const elem *const p = lds + row * 32 * KD + place(4 * g + ((lane & 15) >> 2), col / VEC + ((lane & 3) >> 1)) * VEC + 4 * (lane & 1);
+        if constexpr (sizeof(T) == 4) return {turned(p), turned(p + kPlane), turned(p + 2 * kPlane)};
+        else return turned(p);
+    }
+    static __device__ __forceinline__ Frag<elem> turned(const elem *p)
+    {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds16x4;
+        typedef elem t4 __attribute__((ext_vector_type(4)));
+        const t4 lo = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)p));
+        const t4 hi = __builtin_bit_cast(t4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16x4 *)(p + 16 * 32 * KD)));
+        return Frag<elem>{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     }
 };
+
+// Streamed tiles of a workgroup: 64 rows, in two halves of LDS, of which one is worked on while the other is filled.  fp32 ones take half as much more than the values: 32 rows, or one half alone, so that two or three
+// workgroups fit a CU.
+template <class T, int KD> constexpr int kStreamed = sizeof(T) == 4 && KD % 2 == 0 ? 32 : kTileRows;
+template <class T, int KD> constexpr int kHalves = sizeof(T) == 4 && KD > 2 ? 1 : 2;
+template <class T, int KD, bool TINY> using Streamed = Tile<T, KD, TINY, kStreamed<T, KD>, kAttnBlock>;
 
 // Waits for the loads so far.  Before the loop over tiles: the compiler, which cannot tell an operand loaded before it from a tile loaded in it, would wait for the next tile with every tile.
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }
@@ -247,31 +260,34 @@ __device__ __forceinline__ void part_of(const AttnArgs &a, int part, int &begin,
 template <class T, int KD, bool TINY> using Tile64 = Tile<T, KD, TINY, kTileRows, kAttnBlock>;
 
 // What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
-// (LDS leaves room for one workgroup on a CU where fp32 heads are wider than 64.)
-template <class T, int KD> constexpr int kWavesPerSimd = sizeof(T) == 4 && KD > 2 ? 1 : 2;
+constexpr int kWavesPerSimd = 2;
 
 // Whether a wave can have two blocks of 16 rows (or keys) of its own, which halves what it reads from LDS, without running out of registers.
-template <class T, int KDX, bool MOD> constexpr bool kTwoForward = !(sizeof(T) == 2 && KDX == 4 && MOD);
-template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = sizeof(T) == 4 ? KDX < 2 : KDX < 3;
+template <class T, int KDX, bool MOD> constexpr bool kTwoForward = sizeof(T) == 4 ? KDX < 3 && !MOD : !(KDX == 4 && MOD);
+template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = sizeof(T) == 4 ? KDX < 2 && !MOD : KDX < 3;
 
 // Two results of 16 streamed rows each as a B operand.
-template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 b)
+template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 b, const SplitConst &sc)
 {
-    Frag<T> f;
+    if constexpr (sizeof(T) == 4) {
+        return split3(a, b, sc);
+    } else {
+        Frag<T> f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        f[e] = (T)a[e];
-        f[4 + e] = (T)b[e];
+        for (int e = 0; e < 4; ++e) {
+            f[e] = (T)a[e];
+            f[4 + e] = (T)b[e];
+        }
+        return f;
     }
-    return f;
 }
 
-// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it; fp32 is one part.
+// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it; fp32 is one operand.
 template <class T> constexpr int kZParts = 2;
 template <> inline constexpr int kZParts<float> = 1;
 template <class T> __device__ __forceinline__ void as_parts(f32x4 a, f32x4 b, const SplitConst &sc, Frag<T> (&out)[kZParts<T>])
 {
-    out[0] = as_operand<T>(a, b);
+    out[0] = as_operand<T>(a, b, sc);
     if constexpr (std::is_same<T, bf16_t>::value) { // (what is left of a pair: one dot product each, see split3)
         const bf16x2 neg_lo = __builtin_bit_cast(bf16x2, sc.neg_lo), neg_hi = __builtin_bit_cast(bf16x2, sc.neg_hi);
 #pragma unroll
@@ -282,14 +298,14 @@ template <class T> __device__ __forceinline__ void as_parts(f32x4 a, f32x4 b, co
             b[k] = __builtin_amdgcn_fdot2_f32_bf16(q, neg_lo, b[k], false);
             b[k + 1] = __builtin_amdgcn_fdot2_f32_bf16(q, neg_hi, b[k + 1], false);
         }
-        out[1] = as_operand<T>(a, b);
+        out[1] = as_operand<T>(a, b, sc);
     } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             a[e] -= (float)out[0][e];
             b[e] -= (float)out[0][4 + e];
         }
-        out[1] = as_operand<T>(a, b);
+        out[1] = as_operand<T>(a, b, sc);
     }
 }
 

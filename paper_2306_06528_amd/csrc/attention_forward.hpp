@@ -25,7 +25,7 @@ template <class T, int KD, int QB> struct Running {
         }
     }
     // Probabilities, relative to the maximum, of NB blocks of 16 keys from their scores, which times mul are exponents of 2.
-    template <int NB> __device__ __forceinline__ void probabilities(f32x4 (&s)[NB][QB], float mul, Frag<T> (&p)[NB / 2][QB])
+    template <int NB> __device__ __forceinline__ void probabilities(f32x4 (&s)[NB][QB], float mul, Frag<T> (&p)[NB / 2][QB], const SplitConst &sc)
     {
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
@@ -52,19 +52,20 @@ template <class T, int KD, int QB> struct Running {
                     total[b] += s[j][b][e];
                 }
 #pragma unroll
-            for (int j = 0; j < NB / 2; ++j) p[j][b] = as_operand<T>(s[2 * j][b], s[2 * j + 1][b]);
+            for (int j = 0; j < NB / 2; ++j) p[j][b] = as_operand<T>(s[2 * j][b], s[2 * j + 1][b], sc);
         }
     }
 };
 
 template <class T, int KDX, int QB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<T, KDX>))) void attention_forward_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o,
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void attention_forward_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<T> o,
                                                                                                               float *lse, float *partial, float *partial_lse)
 {
     constexpr int KD = kBlocks32<KDX>;
-    typedef Tile64<T, KD, KDX == 0> TL;
-    __shared__ __attribute__((aligned(16))) T lds[4 * TL::kSize];
-    __shared__ int red[4], key_documents[2][kTileRows];
+    typedef Streamed<T, KD, KDX == 0> TL;
+    constexpr int kRows = TL::kRows, kBuffers = kHalves<T, KD>;
+    __shared__ __attribute__((aligned(16))) typename TL::elem lds[2 * kBuffers * TL::kSize];
+    __shared__ int red[4], key_documents[kBuffers][kRows];
     const AttnBlock at(a);
     if (!at.any) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
@@ -73,6 +74,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     const Masks masks(a, at.batch);
     const float mul = MOD ? 1.f : a.scale * kLog2e; // scores times this are exponents of 2
     const Modified modified(a);
+    const SplitConst sc = split_const();
 
     Frag<T> qf[QB][KD];
     int limit[QB], position[QB], document[QB];
@@ -82,7 +84,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         const int r = min(own + 16 * b + (lane & 15), a.rows - 1), i = a.query(r), h = r - i * a.group;
         const T *const p = q.at(at.particle, at.batch, at.head * a.group + h) + i * q.token;
 #pragma unroll
-        for (int s = 0; s < KD; ++s) qf[b][s] = load_frag(p + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+        for (int s = 0; s < KD; ++s) qf[b][s] = load_frag(p + 32 * s + 8 * g, a.dim - 32 * s - 8 * g, sc);
         position[b] = masks.start + i;
         limit[b] = masks.end(a, position[b]);
         document[b] = masks.document(a, position[b]);
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     int lo = 0, hi = masks.documents ? (p1 < 0 || p0 >= a.s ? 0 : masks.end(a, min(p1, a.s - 1))) : masks.end(a, p1);
     const int free_keys = masks.documents ? 0 : masks.end(a, p0); // (positions rise with the rows)
     if (masks.documents) narrow(masks.documents, p0, p1, a.s, red, lo, hi);
-    int begin = lo / kTileRows, end = (hi + kTileRows - 1) / kTileRows;
+    int begin = lo / kRows, end = (hi + kRows - 1) / kRows;
     part_of(a, at.part, begin, end);
     const int wave_row = min(own + 16 * QB, a.rows) - 1;
     const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
@@ -107,15 +109,15 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     TL::offsets(v_at, a.dim, [&](int i) { return (uint32_t)i * (uint32_t)v.token; });
     int next_document = 0;
     const auto fetch = [&](int tile_of) {
-        const int key = tile_of * kTileRows, last = min(hi - key, kTileRows) - 1;
+        const int key = tile_of * kRows, last = min(hi - key, kRows) - 1;
         kt.load(ks + key * k.token, k_at, (uint32_t)k.token, last, a.dim);
         vt.load(vs + key * v.token, v_at, (uint32_t)v.token, last, a.dim);
-        if (masks.documents && threadIdx.x < kTileRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
+        if (masks.documents && threadIdx.x < kRows) next_document = key + (int)threadIdx.x < a.s ? masks.documents[key + threadIdx.x] : 0;
     };
     const auto stage = [&](int half, int tile_of) {
-        kt.store(lds + half * 2 * TL::kSize, hi - tile_of * kTileRows, a.dim);
-        vt.store(lds + (half * 2 + 1) * TL::kSize, hi - tile_of * kTileRows, a.dim);
-        if (masks.documents && threadIdx.x < kTileRows) key_documents[half][threadIdx.x] = next_document;
+        kt.store(lds + half * 2 * TL::kSize, hi - tile_of * kRows, a.dim, sc);
+        vt.store(lds + (half * 2 + 1) * TL::kSize, hi - tile_of * kRows, a.dim, sc);
+        if (masks.documents && threadIdx.x < kRows) key_documents[half][threadIdx.x] = next_document;
     };
     if (begin < end) {
         fetch(begin);
@@ -126,12 +128,12 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     int half = 0;
     for (int n = begin; n < end; ++n) {
         if (n + 1 < end) fetch(n + 1);
-        const int key = n * kTileRows;
+        const int key = n * kRows;
         if (key < wave_limit) {
-            const T *const kl = lds + half * 2 * TL::kSize, *const vl = kl + TL::kSize;
-            f32x4 s[4][QB];
+            const typename TL::elem *const kl = lds + half * 2 * TL::kSize, *const vl = kl + TL::kSize;
+            f32x4 s[kRows / 16][QB];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kRows / 16; ++j) {
 #pragma unroll
                 for (int b = 0; b < QB; ++b) s[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -144,15 +146,15 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
             if constexpr (MOD) {
                 modified.template apply<T>(s);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < kRows / 16; ++j)
 #pragma unroll
                     for (int b = 0; b < QB; ++b)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[j][b][e] = modified.exponent(s[j][b][e], slope[b], fabsf((float)(position[b] - (key + 16 * j + 4 * g + e))));
             }
-            if (key + kTileRows > free_keys) {
+            if (key + kRows > free_keys) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < kRows / 16; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int at_key = key + 16 * j + 4 * g + e;
@@ -162,10 +164,10 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                             if (at_key >= limit[b] || doc != document[b]) s[j][b][e] = -INFINITY;
                     }
             }
-            Frag<T> p[2][QB];
-            run.probabilities(s, mul, p);
+            Frag<T> p[kRows / 32][QB];
+            run.probabilities(s, mul, p, sc);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kRows / 32; ++j)
 #pragma unroll
                 for (int d = 0; d < 2 * KD; ++d) {
                     const Frag<T> f = TL::columns(vl, 32 * j, 16 * d);
@@ -173,7 +175,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                     for (int b = 0; b < QB; ++b) run.acc[d][b] = mma(f, p[j][b], run.acc[d][b]);
                 }
         }
-        half ^= 1;
+        if constexpr (kBuffers == 2) half ^= 1;
+        else __syncthreads(); // (the tile has been read)
         if (n + 1 < end) stage(half, n + 1);
         __syncthreads();
     }
@@ -216,7 +219,8 @@ __global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, H
     constexpr int KD = kBlocks32<KDX>;
     typedef Tile<T, KD, KDX == 0, kFewKeys, 64> TL;
     constexpr int kJoin = 16 * (32 * KD + 4); // floats of a wave's sums: rows four floats apart from what would be one bank
-    constexpr int kPart = 2 * TL::kSize * (int)sizeof(T) > kJoin * 4 ? 2 * TL::kSize * (int)sizeof(T) : kJoin * 4;
+    constexpr bool kOne = sizeof(T) == 4 && KD > 2; // values where the keys were, once these are read: both do not fit
+    constexpr int kTiles = (kOne ? 1 : 2) * TL::kSize * 2, kPart = kTiles > kJoin * 4 ? kTiles : kJoin * 4;
     __shared__ __attribute__((aligned(16))) char lds[kAttnWaves][kPart];
     __shared__ float tops[kAttnWaves][16], totals[kAttnWaves][16];
     const AttnBlock at(a);
@@ -225,11 +229,12 @@ __global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, H
     const Masks masks(a, at.batch);
     const float mul = MOD ? 1.f : a.scale * kLog2e;
     const Modified modified(a);
+    const SplitConst sc = split_const();
     const int r = min(lane & 15, a.rows - 1), i = a.query(r), h = at.head * a.group + r - i * a.group;
     const T *const qp = q.at(at.particle, at.batch, h) + i * q.token;
     Frag<T> qf[1][KD];
 #pragma unroll
-    for (int s = 0; s < KD; ++s) qf[0][s] = load_frag(qp + 32 * s + 8 * g, a.dim - 32 * s - 8 * g);
+    for (int s = 0; s < KD; ++s) qf[0][s] = load_frag(qp + 32 * s + 8 * g, a.dim - 32 * s - 8 * g, sc);
     const int position = masks.start + i, limit = masks.end(a, position), document = masks.document(a, position);
     const float slope = MOD && a.slopes ? a.slopes[at.particle * a.slopes_stride + h] * kLog2e : 0.f;
     const int p0 = masks.start, p1 = masks.start + a.t - 1;
@@ -240,7 +245,7 @@ __global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, H
 
     Running<T, KD, 1> run;
     const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
-    T *const kl = reinterpret_cast<T *>(lds[wave]), *const vl = kl + TL::kSize;
+    typename TL::elem *const kl = reinterpret_cast<typename TL::elem *>(lds[wave]), *const vl = kOne ? kl : kl + TL::kSize;
     TL kt, vt;
     uint32_t k_at[TL::N], v_at[TL::N];
     TL::offsets(k_at, a.dim, [&](int j) { return (uint32_t)j * (uint32_t)k.token; });
@@ -255,16 +260,23 @@ __global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, H
     for (int n = begin + wave; n < end; n += kAttnWaves) {
         const int key = n * kFewKeys;
         wave_sync(); // (the tile before has been read)
-        kt.store(kl, hi - key, a.dim);
-        vt.store(vl, hi - key, a.dim);
+        kt.store(kl, hi - key, a.dim, sc);
+        if constexpr (!kOne) vt.store(vl, hi - key, a.dim, sc);
         wave_sync();
-        if (n + kAttnWaves < end) fetch(n + kAttnWaves);
+        if constexpr (!kOne)
+            if (n + kAttnWaves < end) fetch(n + kAttnWaves);
         f32x4 s[2][1];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             s[j][0] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < KD; ++c) s[j][0] = mma(TL::rows(kl, 16 * j, 32 * c), qf[0][c], s[j][0]);
+        }
+        if constexpr (kOne) {
+            wave_sync();
+            vt.store(vl, hi - key, a.dim, sc);
+            wave_sync();
+            if (n + kAttnWaves < end) fetch(n + kAttnWaves);
         }
         if constexpr (MOD) {
             modified.template apply<T>(s);
@@ -284,7 +296,7 @@ __global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, H
                 }
         }
         Frag<T> p[1][1];
-        run.probabilities(s, mul, p);
+        run.probabilities(s, mul, p, sc);
 #pragma unroll
         for (int d = 0; d < 2 * KD; ++d) run.acc[d][0] = mma(TL::columns(vl, 0, 16 * d), p[0][0], run.acc[d][0]);
     }

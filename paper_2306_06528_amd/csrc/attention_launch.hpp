@@ -69,7 +69,7 @@ inline int padded_dim(const AttnArgs &a) { return (a.dim + 31) / 32 * 32; }
 template <class T, class F> int with_dim(int dim, F f)
 {
     using std::integral_constant;
-    if (dim * (int)sizeof(T) < 16) return f(integral_constant<int, 0>{});
+    if (dim < 8) return f(integral_constant<int, 0>{});
     if (dim <= 32) return f(integral_constant<int, 1>{});
     if (dim <= 64) return f(integral_constant<int, 2>{});
     if (dim <= 96) return f(integral_constant<int, 3>{});
