@@ -11,7 +11,7 @@
  *   - n particles x `batch` sequences x `length` tokens x `heads` heads x `dim` values, described by svgd_heads: value c of head h of
  *     token t of sequence b of particle i is element i * particle_stride + b * batch_stride + t * token_stride + h * head_stride + c of
  *     `data`.  Inputs may have any strides from 0 on, a view into the results of one linear map among them; outputs' heads must not
- *     overlap.  Gradients of q, k and v may lie side by side in the same rows (one tensor of all three, with the same strides).
+ *     overlap.
  */
 #ifndef SVGD_ATTENTION_H
 #define SVGD_ATTENTION_H
@@ -43,7 +43,7 @@ typedef struct svgd_heads {
  *     z = weight x + bias,  y = act(z) + residual         for every row x
  * weight: out x width, bias: out values per particle; bias and residual.data may be NULL.  z (DEVICE, 16-byte aligned, svgd_linear_saved
  * bytes) receives z for the backward pass, which needs it unless the activation is none; may be NULL.  scratch (DEVICE, 16-byte aligned):
- * svgd_linear_forward_scratch bytes, may be NULL if these are 0.  y may be the residual itself (same pointer and strides).
+ * svgd_linear_forward_scratch bytes, may be NULL if these are 0.
  * Of non-finite and of very small factors the same holds as of svgd_gated_ffn_*.
  */
 size_t svgd_linear_saved(int n, int64_t rows, int64_t out);

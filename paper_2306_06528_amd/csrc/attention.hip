@@ -178,18 +178,13 @@ int svgd_attention_backward(int dtype, const svgd_attention *p, svgd_heads d_o, 
                                dslopes ? extent(dslopes, dslopes_stride, p->n, p->heads) : Extent{0, 0}};
     const Extent read[6] = {extent(q, dtype, qs), extent(k, dtype, ks), extent(v, dtype, ks), extent(d_o, dtype, qs), extent(o, dtype, qs), extent(lse, stats)};
     const MaskExtents masks(*p);
-    const svgd_heads *const heads[3] = {&dq, &dk, &dv};
-    const int64_t counts[3] = {p->heads, p->kv_heads, p->kv_heads};
     for (int i = 0; i < 5; ++i) {
         for (const Extent &r : read)
             if (written[i].meets(r)) return SVGD_ERR_INVALID_ARG;
         for (int m = 0; m < (i < 4 ? 5 : 4); ++m) // (the slopes' gradients may lie between the slopes, in the same rows: looked at above)
             if (masks.e[m].meets(written[i])) return SVGD_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j) {
-            if (!written[i].meets(written[j])) continue;
-            const bool views = i < 3 && (counts[i] == counts[j] || p->length == p->keys) && side_by_side(*heads[j], counts[j], *heads[i], counts[i], dtype, j == 0 ? qs : ks);
-            if (!views) return SVGD_ERR_INVALID_ARG;
-        }
+        for (int j = 0; j < i; ++j)
+            if (written[i].meets(written[j])) return SVGD_ERR_INVALID_ARG;
     }
     AttnCall c{};
     c.a = args_of(*p);

@@ -46,20 +46,4 @@ inline bool valid_heads_output(const svgd_heads &h, int dtype, const HeadSizes &
     return true;
 }
 
-// Whether two tensors of the same sizes lie side by side in the same rows, as views into the results of one linear map do: then their extents meet, they do not.
-// (Same strides, and the second one's heads and values within the gap that the first one's leave in every token.)
-inline bool side_by_side(const svgd_heads &a, int64_t a_heads, const svgd_heads &b, int64_t b_heads, int dtype, const HeadSizes &s)
-{
-    if (a.particle_stride != b.particle_stride || a.batch_stride != b.batch_stride || a.token_stride != b.token_stride || !a.data || !b.data) return false;
-    const int64_t size = (int64_t)dtype_size(dtype), apart = ((intptr_t)b.data - (intptr_t)a.data);
-    if (apart % size) return false;
-    const int64_t d = apart / size, a_end = (a_heads - 1) * a.head_stride + s.dim, b_end = (b_heads - 1) * b.head_stride + s.dim;
-    const int64_t lo = d < 0 ? -d : d, first_end = d < 0 ? b_end : a_end, second_end = d < 0 ? a_end : b_end; // the one that comes first begins at 0
-    int64_t least = INT64_MAX;
-    if (s.n > 1) least = std::min(least, a.particle_stride);
-    if (s.batch > 1) least = std::min(least, a.batch_stride);
-    if (s.tokens > 1) least = std::min(least, a.token_stride);
-    return lo >= first_end && lo + second_end <= least;
-}
-
 } // namespace svgd

@@ -56,10 +56,9 @@ int svgd_linear_forward(int dtype, int activation, int n, int64_t rows, int64_t 
     const Extent written[3] = {extent(y, dtype, n, rows, out), extent(z, z_need), extent(scratch, need)};
     const Extent read[4] = {extent(x, dtype, n, rows, width), extent(weight, weight_stride, n, size), bias ? extent(bias, bias_stride, n, out) : Extent{0, 0},
                             residual.data ? extent(residual, dtype, n, rows, out) : Extent{0, 0}};
-    const bool in_place = residual.data && residual.data == y.data && (n == 1 || residual.particle_stride == y.particle_stride) && (rows == 1 || residual.row_stride == y.row_stride);
     for (int i = 0; i < 3; ++i) {
         for (int r = 0; r < 4; ++r)
-            if (written[i].meets(read[r]) && !(i == 0 && r == 3 && in_place)) return SVGD_ERR_INVALID_ARG;
+            if (written[i].meets(read[r])) return SVGD_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
             if (written[i].meets(written[j])) return SVGD_ERR_INVALID_ARG;
     }

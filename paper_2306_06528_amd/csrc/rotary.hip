@@ -83,17 +83,6 @@ struct Reads { // besides the activations
     }
 };
 
-bool same(const svgd_heads &a, const svgd_heads &b)
-{
-    return a.data == b.data && a.particle_stride == b.particle_stride && a.batch_stride == b.batch_stride && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
-}
-
-// Whether an output may lie where an input or another output lies: apart, or side by side in the same rows.
-bool apart(const svgd_heads &a, const HeadSizes &as, const svgd_heads &b, const HeadSizes &bs, int dtype)
-{
-    return !extent(a, dtype, as).meets(extent(b, dtype, bs)) || side_by_side(a, as.heads, b, bs.heads, dtype, as);
-}
-
 } // namespace
 
 extern "C" {
@@ -105,13 +94,14 @@ int svgd_qk_norm_rotary_forward(int dtype, const svgd_rotary *p, svgd_heads q, s
     if (!valid_heads(q, dtype, qs) || !valid_heads(k, dtype, ks) || !valid_heads_output(q_out, dtype, qs) || !valid_heads_output(k_out, dtype, ks)) return SVGD_ERR_INVALID_ARG;
     if (qs.none() && ks.none()) return SVGD_OK;
     const Reads reads(*p);
-    for (const Extent &w : {extent(q_out, dtype, qs), extent(k_out, dtype, ks)})
+    const Extent written[2] = {extent(q_out, dtype, qs), extent(k_out, dtype, ks)}, inputs[2] = {extent(q, dtype, qs), extent(k, dtype, ks)};
+    for (const Extent &w : written) {
         for (const Extent &r : reads.e)
             if (w.meets(r)) return SVGD_ERR_INVALID_ARG;
-    // (in place is fine: a head is read before it is written, by the same lanes)
-    if ((!same(q, q_out) && !apart(q, qs, q_out, qs, dtype)) || (!same(k, k_out) && !apart(k, ks, k_out, ks, dtype)) || !apart(k, ks, q_out, qs, dtype) || !apart(q, qs, k_out, ks, dtype) ||
-        !apart(q_out, qs, k_out, ks, dtype))
-        return SVGD_ERR_INVALID_ARG;
+        for (const Extent &r : inputs)
+            if (w.meets(r)) return SVGD_ERR_INVALID_ARG;
+    }
+    if (written[0].meets(written[1])) return SVGD_ERR_INVALID_ARG;
     const RotaryArgs a = args_of(*p, kForwardBlocks);
     return for_type(dtype, [&](auto t) {
         using T = decltype(t);
@@ -161,10 +151,9 @@ int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_
             const HeadSizes &s = i % 2 ? ks : qs;
             const Extent e = extent(*acts[i], dtype, s);
             if (work.meets(e) || grads[0].meets(e) || grads[1].meets(e)) return SVGD_ERR_INVALID_ARG;
-            if (dq.data && !(i == 0 && same(dq, dq_out)) && !apart(*acts[i], s, dq, qs, dtype)) return SVGD_ERR_INVALID_ARG;
-            if (dk.data && !(i == 1 && same(dk, dk_out)) && !apart(*acts[i], s, dk, ks, dtype)) return SVGD_ERR_INVALID_ARG;
+            if (written[0].meets(e) || written[1].meets(e)) return SVGD_ERR_INVALID_ARG;
         }
-        if (dq.data && dk.data && !apart(dq, qs, dk, ks, dtype)) return SVGD_ERR_INVALID_ARG;
+        if (written[0].meets(written[1])) return SVGD_ERR_INVALID_ARG;
         for (const Extent &x : written) {
             if (work.meets(x) || grads[0].meets(x) || grads[1].meets(x)) return SVGD_ERR_INVALID_ARG;
             for (const Extent &r : reads.e)

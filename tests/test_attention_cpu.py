@@ -81,7 +81,7 @@ def linear_forward(lib, dtype=0, act=4, n=2, rows=40, width=4, out=6, x=X, xs=(1
     (dict(rows=(1 << 30) + 1), TOO_LARGE), (dict(width=0), INVALID), (dict(width=(1 << 20) + 1), TOO_LARGE), (dict(out=0), INVALID), (dict(out=(1 << 20) + 1), TOO_LARGE),
     (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(w=None), INVALID), (dict(x=X + 2), INVALID), (dict(w=W + 2), INVALID), (dict(b=V + 1), INVALID), (dict(z=B + 8), INVALID),
     (dict(zn=8), INVALID), (dict(xs=(-160, 4)), INVALID), (dict(ys=(240, 5)), INVALID), (dict(ys=(100, 6)), INVALID), (dict(y=X), INVALID), (dict(y=W), INVALID), (dict(y=V), INVALID),
-    (dict(z=Y), INVALID), (dict(z=X), INVALID), (dict(res=Y + 4), INVALID), (dict(res=R + 1), INVALID), (dict(res=B), INVALID),
+    (dict(z=Y), INVALID), (dict(z=X), INVALID), (dict(res=Y + 4), INVALID), (dict(res=Y), INVALID), (dict(res=R + 1), INVALID), (dict(res=B), INVALID),
     (dict(rows=300, xs=(1 << 20, 2000), ys=(1 << 20, 6), width=2000, scratch=None), INVALID), (dict(rows=300, xs=(1 << 20, 2000), ys=(1 << 20, 6), width=2000, sn=16), INVALID)])
 def test_linear_forward_refuses(lib, bad, status):
     assert linear_forward(lib, **bad) == status
@@ -118,7 +118,7 @@ def rotary_forward(lib, dtype=0, q=Q, k=K, qo=O, ko=L, qs=QS, ks=KS, qos=QS, kos
     (dict(pairs=5), INVALID), (dict(pairs=-1), INVALID), (dict(batch=-1), INVALID), (dict(length=-1), INVALID), (dict(length=(1 << 24) + 1), TOO_LARGE), (dict(batch=1 << 20, length=1 << 20), TOO_LARGE),
     (dict(frequencies=None), INVALID), (dict(positions=None), INVALID), (dict(frequencies=M + 4), INVALID), (dict(positions=N + 4), INVALID), (dict(positions_stride=-1), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(eps=-1.0), INVALID), (dict(q_weight=None), INVALID), (dict(k_weight=None), INVALID), (dict(q_weight=W + 2), INVALID), (dict(q=None), INVALID),
-    (dict(ko=None), INVALID), (dict(q=Q + 2), INVALID), (dict(qs=(96, 48, -16, 8)), INVALID), (dict(qos=(96, 48, 16, 7)), INVALID), (dict(qos=(96, 40, 16, 8)), INVALID), (dict(qo=Q + 4), INVALID),
+    (dict(ko=None), INVALID), (dict(q=Q + 2), INVALID), (dict(qs=(96, 48, -16, 8)), INVALID), (dict(qos=(96, 48, 16, 7)), INVALID), (dict(qos=(96, 40, 16, 8)), INVALID), (dict(qo=Q + 4), INVALID), (dict(qo=Q), INVALID),
     (dict(qo=K), INVALID), (dict(ko=O), INVALID), (dict(qo=M), INVALID), (dict(qo=N), INVALID), (dict(ko=W), INVALID)])
 def test_rotary_forward_refuses(lib, bad, status):
     assert rotary_forward(lib, **bad) == status
@@ -131,7 +131,7 @@ def rotary_backward(lib, dtype=0, dqo=O, dko=L, q=Q, k=K, dq=X, dk=Y, dqs=QS, dk
 
 @pytest.mark.parametrize("bad,status", [
     (dict(dtype=-1), INVALID), (dict(n=65), TOO_LARGE), (dict(dqo=None), INVALID), (dict(q=None), INVALID), (dict(k=K + 1), INVALID), (dict(scratch=None), INVALID), (dict(scratch=S + 4), INVALID),
-    (dict(sn=32), INVALID), (dict(stride=7), INVALID), (dict(dqw=W), INVALID), (dict(dkw=V + 16), INVALID), (dict(dq=Q), INVALID), (dict(dq=O + 4), INVALID), (dict(dk=X), INVALID), (dict(dk=K), INVALID),
+    (dict(sn=32), INVALID), (dict(stride=7), INVALID), (dict(dqw=W), INVALID), (dict(dkw=V + 16), INVALID), (dict(dq=Q), INVALID), (dict(dq=O + 4), INVALID), (dict(dq=O), INVALID), (dict(dk=X), INVALID), (dict(dk=K), INVALID),
     (dict(scratch=X), INVALID), (dict(scratch=O), INVALID), (dict(dqw=X), INVALID), (dict(dqw=Q), INVALID), (dict(dqw=S), INVALID), (dict(q_weight=None, k_weight=None), INVALID), (dict(dqs=(96, 48, 16, 4)), INVALID)])
 def test_rotary_backward_refuses(lib, bad, status):
     assert rotary_backward(lib, **bad) == status
