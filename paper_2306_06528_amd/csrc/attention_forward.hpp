@@ -255,8 +255,8 @@ __global__ __launch_bounds__(kAttnBlock) void attention_few_kernel(AttnArgs a, H
         kt.load(ks + key * k.token, k_at, (uint32_t)k.token, last, a.dim);
         vt.load(vs + key * v.token, v_at, (uint32_t)v.token, last, a.dim);
     };
-    if (begin + wave < end) fetch(begin + wave);
     loads_done();
+    if (begin + wave < end) fetch(begin + wave);
     for (int n = begin + wave; n < end; n += kAttnWaves) {
         const int key = n * kFewKeys;
         wave_sync(); // (the tile before has been read)
