@@ -27,10 +27,11 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
     if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
 }
 
-template <class T, int KDX, int QB, bool MOD>
+template <class T, int KDX, bool MOD>
 __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
                                                                                                               Heads<const T> o, const float *lse, float *delta, Heads<T> dq, float *slope_rows, float *partial)
 {
+    constexpr int QB = 1; // blocks of 16 rows of a wave's own (attention_launch.hpp)
     constexpr int KD = kBlocks32<KDX>;
     typedef Streamed<T, KD, KDX == 0> TL;
     constexpr int kRows = TL::kRows, kBuffers = kHalves<T, KD>;

@@ -40,20 +40,23 @@ struct AttnArgs {
 };
 
 // Which particle, sequence, key head, tile and part a workgroup has.  Workgroups go round the eight dies in turn; a die gets ones that follow one another.  Four heads, whose keys meet in its L2, take turns
-// tile by tile, so that of causal ones the longest of four heads come first and the shortest last: head after head the last head's longest would be left over at the end.
+// tile by tile, so that of causal ones the longest of four heads come first and the shortest last: head after head the last head's longest would be left over at the end.  Where a die has less than four heads
+// of its own, all heads take turns: otherwise one die would get a head's long tiles and another its short ones (4 x 2 x 2,000 x 8 heads over 2 of 64 fp16, causal, with documents: forward 89 us, so 68; 2 x 2,048 x 8
+// heads of 64 bf16, causal, queries in two parts 38.5, so 32.4).
 struct AttnBlock {
     static constexpr int kHeads = 4;
     int particle, batch, head, tile, part;
     bool any;
     __device__ __forceinline__ AttnBlock(const AttnArgs &a)
     {
-        const int id = (int)(blockIdx.x & 7) * a.per_die + (int)(blockIdx.x >> 3);
-        any = id < a.total;
         const int each = a.tiles * a.splits, heads = a.n * a.batch * a.kv;
-        const int four = id / (kHeads * each), left = id - four * (kHeads * each);
-        const int of = min(kHeads, heads - four * kHeads); // (the last heads may be fewer; beyond the last one it does not matter)
-        const int turn = left / max(of, 1);
-        int h = four * kHeads + left - turn * of;
+        const bool few = heads < 8 * kHeads;
+        const int id = few ? (int)blockIdx.x : (int)(blockIdx.x & 7) * a.per_die + (int)(blockIdx.x >> 3);
+        any = id < a.total;
+        const int in_turn = few ? heads : kHeads, group = id / (in_turn * each), left = id - group * (in_turn * each);
+        const int of = max(min(in_turn, heads - group * in_turn), 1); // (the last heads may be fewer; beyond the last one it does not matter)
+        const int turn = left / of;
+        int h = group * in_turn + left - turn * of;
         tile = turn / a.splits;
         part = turn - tile * a.splits;
         head = h % a.kv;

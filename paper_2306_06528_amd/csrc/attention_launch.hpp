@@ -25,16 +25,27 @@ inline int64_t small_blocks(const AttnArgs &a, int64_t size) { return (int64_t)a
 // 21 / 18 and 457 / 392, keys 34.7 / 40 and 999 / 915; with queries of their own, which two blocks cost more registers, 27.9 / 30.3 and 671 / 684, so always one.
 constexpr int64_t kManyForward = 1024, kManyKeys = 4096;
 
-// Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards: as many as make the shortest way of a workgroup's tiles, the time until its first one
-// is there (one tile's) and, with parts, the sums' own launch, times the rounds of kAtATime workgroups.  (3 x 2 x 333 x 6 heads of 40 fp32, 192 workgroups of 6 tiles: 3 parts, which make two rounds, 20 us, 2 parts 15.)
+// Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards.  In units of a tile's time a workgroup takes its tiles and one for the time until the
+// first is there, and all of them take rounds of kAtATime.  Masks leave some of the workgroups less, how much on an average is `share`; the card then works on until the longest is done, and as fast as kAtOnce
+// workgroups that wait for nothing.  Parts' sums cost a launch.  (us of the keys' kernel in 1 / 2 / 3 / 4 parts, and of the sums: 4 x 2 x 2,000 x 8 heads over 2 of 64 fp16, causal, capped, 7 documents 226 / 129 / 113 / 122 and
+// 11; 4 x 2 x 1,000 x 8 over 4 of 64 bf16 causal 63 / 42 / 45 / 48 and 11; 3 x 1,500 x 8 over 4 of 64 fp32 causal 235 / 133 / 104 / 106 and 8; 8 x 2 x 512 x 4 of 64 bf16 causal 22.6 / 21.8 / 23 / 28 and 11.)
 constexpr int64_t kAtATime = 512;
+constexpr double kAtOnce = 341;
 inline int parts_for(const AttnArgs &a, int64_t own, int64_t streamed)
 {
     const int64_t blocks = small_blocks(a, own), tiles = ceil_div(streamed, kTileRows);
-    if (blocks == 0 || blocks >= kAtATime) return 1;
-    int64_t best = 1, least = tiles + 1;
-    for (int64_t parts = 2; parts <= 64 && 2 * parts <= tiles; ++parts) {
-        const int64_t cost = ceil_div(blocks * parts, kAtATime) * (ceil_div(tiles, parts) + 1) + 1;
+    const bool even = !a.causal && !a.documents;
+    if (blocks == 0 || blocks >= (even ? 1 : 2) * kAtATime) return 1;
+    const double share = a.documents ? 0.5 : 1 - 0.5 * (a.t < a.s ? a.t : a.s) / a.s;
+    int64_t best = 1;
+    double least = 1e30;
+    for (int64_t parts = 1; parts == 1 || (parts <= 64 && 2 * parts <= tiles); ++parts) {
+        const double longest = (double)(ceil_div(tiles, parts) + 1);
+        double cost = ceil_div(blocks * parts, kAtATime) * longest + (parts > 1 ? 1 : 0);
+        if (!even) {
+            const double all = (double)(blocks * parts) * (share * tiles / parts + 1) / kAtOnce;
+            cost = (all > longest ? all : longest) + (parts > 1 ? 2 : 0);
+        }
         if (cost < least) {
             least = cost;
             best = parts;

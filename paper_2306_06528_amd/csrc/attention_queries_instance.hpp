@@ -18,7 +18,7 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
             constexpr bool MOD = decltype(mod)::value;
             set_grid(a, a.rows, 16 * kAttnWaves, query_splits(a));
             const int grid = a.per_die * 8;
-            attention_queries_kernel<T, KD, 1, MOD>
+            attention_queries_kernel<T, KD, MOD>
                 <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), in<T>(c.o), c.lse, delta, out<T>(c.dq), c.slope_rows, c.partial);
             return launched_ok();
         });
