@@ -104,7 +104,7 @@ int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_
  * all of that head's results.  starts beyond +-2^28 count as that.
  * slopes: `heads` values per particle.  lse (DEVICE, n x batch x heads x length floats): log of the sum of exp z, for the backward pass; may be NULL.  scratch (DEVICE,
  * 16-byte aligned): svgd_attention_forward_scratch bytes of this same struct, may be NULL if these are 0.
- * fp32 factors go through products of three bf16 parts: an infinity there may come out as NaN, and factors below 2^-102 or so lose digits.
+ * Of non-finite and of very small fp32 factors the same holds as of svgd_gated_ffn_*.
  */
 typedef struct svgd_attention {
     int n, heads, kv_heads, dim;

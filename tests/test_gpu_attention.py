@@ -221,7 +221,7 @@ def test_rotary_parts_and_accumulate(att):
 # ---------------------------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------------------------
-def run_attention(att, q, k, v, do, poison=True, **how):
+def run_attention(att, q, k, v, do, **how):
     """Forward and backward against the definitions."""
     n, heads = q.shape[0], q.shape[3]
     slopes, ds = how.get("slopes"), None
@@ -357,6 +357,18 @@ def test_attention_parts(att):
     assert some[0] is None and torch.equal(some[1], all_of[1]) and torch.equal(some[2], all_of[2])
     some = att.attention_backward(do, q, k, v, o, lse, causal=True, slopes=slopes, dslopes=ds, accumulate=True, want_dkv=False)
     assert some[1] is None and some[2] is None and torch.equal(some[0], all_of[0]) and torch.equal(ds, 2 * once)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("kind", ["causal", "documents", "prefix"])
+@pytest.mark.parametrize("n,batch,t,s,heads,kv,d", [(2, 5, 1_100, 1_100, 3, 3, 24), (1, 5, 540, 700, 4, 2, 40), (5, 7, 330, 330, 2, 1, 72), (3, 4, 200, 1_000, 3, 3, 100)])
+def test_attention_uneven_workgroups(att, n, batch, t, s, heads, kv, d, kind, dtype):
+    """Workgroups whose masks leave them unlike numbers of tiles: streamed rows in parts, up to 682 workgroups; heads that all take turns (up to 31 key heads) or four at a time."""
+    g = gen(n, t, s, heads, kind)
+    how = {"causal": True} if kind == "causal" else masks_of(kind, g, batch, t, s) | {"causal": True}
+    q, do = (normal(g, n, batch, t, heads, d, dtype=dtype) for _ in range(2))
+    k, v = (normal(g, n, batch, s, kv, d, dtype=dtype) for _ in range(2))
+    run_attention(att, q, k, v, do, **how)
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
