@@ -4,11 +4,15 @@
 //     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
 // P is rounded to the activations' type for the product with do: half a step of each, with signs as random as those of the gradients' own rounding.  dz goes into the products with k and q in two
 // such parts (BlockScale: fp16): rounded to one, its roundings and those of o, from which delta comes, would together put dq and dk of short sequences off by 1.7 times what rounding the results does,
-// with two parts by 1.35.
+// with two parts by 1.35; with delta as `exact_delta` says by 1.00 up to 64 keys, and beyond by 1.25 at most.
 #pragma once
 #include "attention_common.hpp"
 
 namespace svgd {
+
+// o as it was stored leaves delta off by its roundings, which of few keys are not small beside dz's own and do not cancel.  Where all keys are in one tile, the queries' kernel makes delta from P and dP instead (another two
+// products of that tile); 16-bit activations.
+template <class T> __host__ __device__ inline bool exact_delta(const AttnArgs &a) { return sizeof(T) == 2 && a.s <= kTileRows; }
 
 // delta of every row, 16 lanes each, where the kernel that has queries of its own, which makes it otherwise, is not wanted.
 template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel(AttnArgs a, Heads<const T> o, Heads<const T> d_o, float *delta)
@@ -77,7 +81,6 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         }
         del = sum_over_rows(del);
         less[b] = f32x4{-del, -del, -del, -del};
-        if (g == 0 && at.part == 0 && own + 16 * b + (lane & 15) < a.rows) delta[line] = del;
     }
     const int last_row = min(first + 16 * QB * kAttnWaves, a.rows) - 1;
     const int p0 = masks.start + a.query(first), p1 = masks.start + a.query(last_row);
@@ -121,6 +124,53 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     }
     loads_done();
     __syncthreads();
+    if (exact_delta<T>(a)) {
+        float sum[QB], total[QB]; // of P dP and of P
+#pragma unroll
+        for (int b = 0; b < QB; ++b) sum[b] = total[b] = 0.f;
+        if (begin < end && 0 < wave_limit)
+#pragma unroll 1
+            for (int key = 0; key < kRows; key += 16) {
+                f32x4 s[1][QB], dp[QB];
+#pragma unroll
+                for (int b = 0; b < QB; ++b) s[0][b] = dp[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < KD; ++c) {
+                    const Frag<T> f = TL::rows(lds, key, 32 * c), e = TL::rows(lds + TL::kSize, key, 32 * c);
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) {
+                        s[0][b] = mma(f, qf[b][c], s[0][b]);
+                        dp[b] = mma(e, df[b][c], dp[b]);
+                    }
+                }
+                if constexpr (MOD) modified.template apply<T>(s);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at_key = key + 4 * g + e;
+                    const int doc = masks.documents ? key_documents[0][at_key] : 0;
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) {
+                        float x = s[0][b][e];
+                        if constexpr (MOD) x = modified.exponent(x, slope[b], fabsf((float)(position[b] - at_key)));
+                        if (at_key >= limit[b] || doc != document[b]) x = -INFINITY;
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
+                        sum[b] += p * dp[b][e];
+                        total[b] += p;
+                    }
+                }
+            }
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            const float all = sum_over_rows(total[b]), del = all > 0.f ? sum_over_rows(sum[b]) / all : 0.f;
+            less[b] = f32x4{-del, -del, -del, -del};
+        }
+    }
+    if (g == 0 && at.part == 0)
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            const int r = own + 16 * b + lane, i = a.query(min(r, a.rows - 1));
+            if (r < a.rows) delta[a.line(at.particle, at.batch, at.head * a.group + r - i * a.group, i)] = -less[b][0];
+        }
     int half = 0;
     for (int n = begin; n < end; ++n) {
         if (n + 1 < end) fetch(n + 1);

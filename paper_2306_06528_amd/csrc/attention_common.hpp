@@ -332,11 +332,18 @@ __device__ __forceinline__ float row_max(float v)
     return __builtin_elementwise_maximum(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false)));
 }
 
-// tanh: for 16-bit activations from one exponential, off by 2^-23 or so of 1; for fp32 the library's.
-template <class T> __device__ __forceinline__ float tanh_of(float x)
+// tanh, for 16-bit activations: up to 1/2 x times a polynomial in x^2 (through its values at the nodes of Chebyshev; off by 1.4e-8, rounded by 1.2e-7 of itself), beyond from one exponential, off by 2^-23 or so of 1, which
+// of a small one would be too much: the cap times that is the error of an exponent.  For fp32 the library's.
+constexpr float kTanhSmall = 0.5f;
+__device__ __forceinline__ float tanh_small(float x)
 {
-    if constexpr (sizeof(T) == 4) return tanhf(x);
-    else return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+    const float u = x * x;
+    return x * __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.01714132f, -0.05298924f), 0.13324828f), -0.33333072f), 1.f);
+}
+__device__ __forceinline__ float tanh_any(float x)
+{
+    const float large = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+    return fabsf(x) <= kTanhSmall ? tanh_small(x) : large;
 }
 
 // Scores that are capped, or less a slope times the distance: z = out t - slope distance in exponents of 2, where t = tanh(scale s / cap) and out = cap, or t = scale s and out = 1; d z / d (scale s) is
@@ -352,12 +359,32 @@ struct Modified {
 #pragma unroll
             for (int b = 0; b < B; ++b) s[j][b] *= in;
         if (on == 0.f) return;
+        bool small = sizeof(T) == 2;
+        if constexpr (sizeof(T) == 2) {
+            float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int b = 0; b < B; ++b)
+                for (int b = 0; b < B; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[j][b][e] = tanh_of<T>(s[j][b][e]);
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(s[j][b][e]));
+            small = __ballot(most > kTanhSmall) == 0; // (mostly)
+        }
+        if (small) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int b = 0; b < B; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[j][b][e] = tanh_small(s[j][b][e]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int b = 0; b < B; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[j][b][e] = sizeof(T) == 4 ? tanhf(s[j][b][e]) : tanh_any(s[j][b][e]);
+        }
     }
     __device__ __forceinline__ float exponent(float t, float slope, float distance) const { return __builtin_fmaf(t, out, -slope * distance); } // slope: times log2 e
     __device__ __forceinline__ float damp(float t) const { return __builtin_fmaf(-on * t, t, 1.f); }

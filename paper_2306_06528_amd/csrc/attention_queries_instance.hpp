@@ -8,7 +8,7 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
     AttnArgs &a = c.a;
     const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t;
     float *const delta = const_cast<float *>(c.delta);
-    if (!c.dq.data && !c.slope_rows) {
+    if (!c.dq.data && !c.slope_rows && !exact_delta<T>(a)) {
         attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), delta);
         return launched_ok();
     }
