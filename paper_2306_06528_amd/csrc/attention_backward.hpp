@@ -14,6 +14,13 @@ namespace svgd {
 // products of that tile); 16-bit activations.
 template <class T> __host__ __device__ inline bool exact_delta(const AttnArgs &a) { return sizeof(T) == 2 && a.s <= kTileRows; }
 
+// One of two forms of a loop, the same for the whole wave.
+template <class F> __device__ __forceinline__ void with_mask(bool masked, F f)
+{
+    if (masked) f(std::true_type{});
+    else f(std::false_type{});
+}
+
 // delta of every row, 16 lanes each, where the kernel that has queries of its own, which makes it otherwise, is not wanted.
 template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel(AttnArgs a, Heads<const T> o, Heads<const T> d_o, float *delta)
 {
@@ -200,7 +207,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                 }
                 if constexpr (MOD) modified.template apply<T>(s);
                 float largest = 0.f;
-                const auto gradients = [&](auto masked) {
+                const auto gradients = [&](auto masked, auto biased) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -211,23 +218,24 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                             for (int b = 0; b < QB; ++b) {
                                 float x = s[j][b][e];
                                 [[maybe_unused]] const float far = fabsf((float)(position[b] - at_key)), t = x;
-                                if constexpr (MOD) x = modified.exponent(t, slope[b], far);
+                                if constexpr (MOD) x = biased ? modified.exponent(t, slope[b], far) : t * modified.out;
                                 if (masked && (at_key >= limit[b] || doc != document[b])) x = -INFINITY;
                                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
                                 float dz = p * dp[j][b][e];
-                                if constexpr (MOD) {
+                                if (biased) {
                                     sum_dz[b] += dz;
                                     sum_dz_far[b] += dz * far;
                                     sum_far[b] += p * far;
-                                    dz *= modified.damp(t);
                                 }
+                                if constexpr (MOD) dz *= modified.damp(t);
                                 s[j][b][e] = dz;
                                 if constexpr (std::is_same<T, f16_t>::value) largest = fmaxf(largest, fabsf(dz));
                             }
                         }
                 };
-                if (key0 + kRows > free_keys) gradients(std::true_type{});
-                else gradients(std::false_type{});
+                const bool some_hidden = key0 + kRows > free_keys;
+                if (MOD && a.slopes) with_mask(some_hidden, [&](auto masked) { gradients(masked, std::bool_constant<MOD>{}); });
+                else with_mask(some_hidden, [&](auto masked) { gradients(masked, std::false_type{}); });
                 if constexpr (std::is_same<T, f16_t>::value) {
                     const float factor = bs.take(largest);
                     if (factor != 1.f) {
@@ -472,7 +480,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                 if constexpr (kDeep) __builtin_amdgcn_sched_barrier(0);
                 if constexpr (MOD) modified.template apply<T>(s);
                 float largest = 0.f;
-                const auto gradients = [&](auto hidden) {
+                const auto gradients = [&](auto hidden, auto biased) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int r = 32 * m + 16 * j + 4 * g;
@@ -486,7 +494,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                             for (int b = 0; b < KB; ++b) {
                                 float x = s[j][b][e];
                                 [[maybe_unused]] const float t = x;
-                                if constexpr (MOD) x = modified.exponent(t, slope[e], fabsf((float)(position[e] - key[b])));
+                                if constexpr (MOD) x = biased ? modified.exponent(t, slope[e], fabsf((float)(position[e] - key[b]))) : t * modified.out;
                                 if (hidden && (key[b] >= limit[e] || document[b] != documents[e])) x = -INFINITY;
                                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, kExponent - log[e]));
                                 float dz = p * dp[j][b][e];
@@ -498,8 +506,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                         }
                     }
                 };
-                if (masked) gradients(std::true_type{});
-                else gradients(std::false_type{});
+                if (MOD && a.slopes) with_mask(masked, [&](auto hidden) { gradients(hidden, std::bool_constant<MOD>{}); });
+                else with_mask(masked, [&](auto hidden) { gradients(hidden, std::false_type{}); });
                 if constexpr (kHalf) {
                     const float factor = bs.take(largest);
                     if (factor != 1.f) {

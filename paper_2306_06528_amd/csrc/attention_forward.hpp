@@ -147,12 +147,19 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
             }
             if constexpr (MOD) {
                 modified.template apply<T>(s);
+                if (a.slopes) {
 #pragma unroll
-                for (int j = 0; j < kRows / 16; ++j)
+                    for (int j = 0; j < kRows / 16; ++j)
 #pragma unroll
-                    for (int b = 0; b < QB; ++b)
+                        for (int b = 0; b < QB; ++b)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[j][b][e] = modified.exponent(s[j][b][e], slope[b], fabsf((float)(position[b] - (key + 16 * j + 4 * g + e))));
+                            for (int e = 0; e < 4; ++e) s[j][b][e] = modified.exponent(s[j][b][e], slope[b], fabsf((float)(position[b] - (key + 16 * j + 4 * g + e))));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kRows / 16; ++j)
+#pragma unroll
+                        for (int b = 0; b < QB; ++b) s[j][b] *= modified.out;
+                }
             }
             if (key + kRows > free_keys) {
 #pragma unroll
