@@ -265,9 +265,10 @@ template <class T, int KD, bool TINY> using Tile64 = Tile<T, KD, TINY, kTileRows
 // What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
 constexpr int kWavesPerSimd = 2;
 
-// Whether a wave can have two blocks of 16 rows (or keys) of its own, which halves what it reads from LDS, without running out of registers.
-template <class T, int KDX, bool MOD> constexpr bool kTwoForward = sizeof(T) == 4 ? KDX < 3 && !MOD : !(KDX == 4 && MOD);
-template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = sizeof(T) == 4 ? KDX < 2 && !MOD : KDX < 3;
+// Whether a wave can have two blocks of 16 rows (or keys) of its own, which halves what it reads from LDS, without running out of registers.  (Capped scores of 16 bits could, but the waves that one block leaves room
+// for are worth more: 4 x 2 x 2,000 x 8 heads over 2 of 64 fp16 forward 71 us with two, 62 with one; keys, 4 x 4 x 4,096 x 8 heads of 64 bf16, causal, 1,071 and 1,012.)
+template <class T, int KDX, bool MOD> constexpr bool kTwoForward = !MOD && (sizeof(T) == 2 || KDX < 3);
+template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = !MOD && KDX < (sizeof(T) == 2 ? 3 : 2);
 
 // Two results of 16 streamed rows each as a B operand.
 template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 b, const SplitConst &sc)

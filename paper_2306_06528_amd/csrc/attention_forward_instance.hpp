@@ -15,7 +15,7 @@ template <> int svgd::attention_forward<SVGD_ATTENTION_TYPE>(AttnCall &c)
                 attention_few_kernel<T, KD, MOD><<<a.per_die * 8, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
                 return launched_ok();
             }
-            const bool two = kTwoForward<T, KD, MOD> && small_blocks(a, a.rows) >= kManyForward;
+            const bool two = kTwoForward<T, KD, MOD> && many_forward(a);
             set_grid(a, a.rows, 16 * kAttnWaves * (two ? 2 : 1), forward_splits(a));
             const int grid = a.per_die * 8;
             if constexpr (kTwoForward<T, KD, MOD>)

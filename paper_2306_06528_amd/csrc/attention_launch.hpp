@@ -22,8 +22,14 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Workgroups with one block of 16 rows (or keys) for every wave.
 inline int64_t small_blocks(const AttnArgs &a, int64_t size) { return (int64_t)a.n * a.batch * a.kv * ceil_div(size, 16 * kAttnWaves); }
 // Two blocks to a wave where the workgroups are many all the same.  us with one and with two, 8 x 8 x 197 x 6 heads of 64 bf16 (1,536 small workgroups) and 4 x 2 x 4,096 x 16 heads of 64 causal (8,192): forward
-// 21 / 18 and 457 / 392, keys 34.7 / 40 and 999 / 915; with queries of their own, which two blocks cost more registers, 27.9 / 30.3 and 671 / 684, so always one.
-constexpr int64_t kManyForward = 1024, kManyKeys = 4096;
+// 21 / 18 and 457 / 392, keys 34.7 / 40 and 999 / 915; with queries of their own, which two blocks cost more registers, 27.9 / 30.3 and 671 / 684, so always one.  Masked calls, whose workgroups differ, are better off with
+// twice as many while these are few or short (64 bf16, causal: 1,024 of 2,048 keys 38 / 45, 1,536 of 1,024 keys 34 / 43 and of 4,096 99 / 91, 2,048 of 1,024 keys 42 / 45 and of 4,096 107 / 93, 4,096 of 1,024 keys 69 / 69).
+constexpr int64_t kManyKeys = 4096;
+inline bool many_forward(const AttnArgs &a)
+{
+    const bool even = !a.causal && !a.documents;
+    return small_blocks(a, a.rows) >= (even ? 1024 : a.s >= 2048 ? 1536 : 4096);
+}
 
 // Where workgroups with rows (or keys) of their own are few, the streamed ones go in parts, whose sums are added up afterwards.  In units of a tile's time a workgroup takes its tiles and one for the time until the
 // first is there, and all of them take rounds of kAtATime.  Masks leave some of the workgroups less, how much on an average is `share`; the card then works on until the longest is done, and as fast as kAtOnce
