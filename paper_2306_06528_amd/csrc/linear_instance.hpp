@@ -44,11 +44,6 @@ template <class T, class TD> static int linear_gradients(const LinearCall &c, co
     if (c.dx.data && c.s.rows > 0 && plan.input_parts > 1) {
         const FfnShape s{c.s.n, c.s.rows, c.s.width, c.s.out, c.s.out_ld, c.s.width_ld};
         reduce_rows_kernel<T><<<(unsigned)tiles(c.s.n * c.s.rows * c.s.width_ld / 4, 256), 256, 0, c.stream>>>(s, dx_partial, plan.input_parts, out<T>(c.dx));
-        if ((rc = launched())) return rc;
-    }
-    if (c.dweight.p && plan.param_parts > 1) {
-        const int64_t size = c.s.width * c.s.out;
-        reduce_params_kernel<<<(unsigned)tiles(c.s.n * size, 256), 256, 0, c.stream>>>(c.s.n, size, 1, param_partial, plan.param_parts, c.dweight, c.dweight, c.accumulate);
         rc = launched();
     }
     return rc;
@@ -66,15 +61,18 @@ template <> int linear_backward<SVGD_LINEAR_TYPE>(const LinearCall &c, const Lin
         else linear_slope_kernel<T, false><<<blocks, 256, 0, c.stream>>>(c.s, plan.sum_rows, plan.sums, groups, in<T>(c.dy), nullptr, nullptr, sums, c.dbias, c.accumulate);
         if (const int rc = launched()) return rc;
     }
-    if (c.dbias.p && (plan.sums > 1 || (c.s.rows == 0 && !c.accumulate))) { // (the sum over no rows is 0)
-        reduce_params_kernel<<<(unsigned)tiles(c.s.n * c.s.out, 256), 256, 0, c.stream>>>(c.s.n, c.s.out, 1, sums, plan.sums, c.dbias, c.dbias, c.accumulate);
-        if (const int rc = launched()) return rc;
+    const bool all = products && !(c.s.rows == 0 && c.accumulate);
+    if (all) {
+        const Rows<const float> d = act ? Rows<const float>{dz, c.s.rows * c.s.out_ld, c.s.out_ld} : Rows<const float>{(const float *)c.dy.data, c.dy.particle_stride, c.dy.row_stride};
+        const int rc = act || std::is_same<T, float>::value ? linear_gradients<T, float>(c, plan, d, dx_partial, param_partial) : linear_gradients<T, T>(c, plan, in<T>(c.dy), dx_partial, param_partial);
+        if (rc) return rc;
     }
-    if (!products || (c.s.rows == 0 && c.accumulate)) return SVGD_OK;
-    if constexpr (!std::is_same<T, float>::value)
-        if (!act) return linear_gradients<T, T>(c, plan, in<T>(c.dy), dx_partial, param_partial);
-    const Rows<const float> d = act ? Rows<const float>{dz, c.s.rows * c.s.out_ld, c.s.out_ld} : Rows<const float>{(const float *)c.dy.data, c.dy.particle_stride, c.dy.row_stride};
-    return linear_gradients<T, float>(c, plan, d, dx_partial, param_partial);
+    PartSums weight{}, bias{};
+    if (all && c.dweight.p && plan.param_parts > 1) weight = {param_partial, plan.param_parts, c.s.width * c.s.out, c.dweight};
+    if (c.dbias.p && (plan.sums > 1 || (c.s.rows == 0 && !c.accumulate))) bias = {sums, plan.sums, c.s.out, c.dbias}; // (the sum over no rows is 0)
+    if (weight.blocks() + bias.blocks() == 0) return SVGD_OK;
+    linear_sums_kernel<<<dim3((unsigned)(weight.blocks() + bias.blocks()), c.s.n), 256, 0, c.stream>>>(weight, bias, c.accumulate);
+    return launched();
 }
 
 } // namespace svgd

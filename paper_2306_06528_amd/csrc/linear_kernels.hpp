@@ -231,6 +231,30 @@ __global__ __launch_bounds__(256) void linear_slope_kernel(LinearShape s, int64_
     }
 }
 
+// Parts' sums of a parameter's gradient, [part][particle][size].
+struct PartSums {
+    const float *partial;
+    int parts; // 0: the sum is 0
+    int64_t size;
+    Params out; // null: none
+    __host__ __device__ int64_t blocks() const { return out.p ? (size + 255) / 256 : 0; }
+};
+
+// Adds them up, in order, those of the weight and of the bias in one launch: a workgroup has 256 values of a particle.  (8 x 1,024 x 1,024 in two parts and 1,024 in 32: 29 us, 5 x 333 x 501 in two and 501 in 62: 7.0; in a launch for each, with the particle divided out in 64 bits, 31 + 5.2 and 5.2 + 5.3.)
+static __global__ __launch_bounds__(256) void linear_sums_kernel(PartSums weight, PartSums bias, bool accumulate)
+{
+    const bool second = blockIdx.x >= weight.blocks();
+    const int64_t size = second ? bias.size : weight.size, k = (blockIdx.x - (second ? weight.blocks() : 0)) * 256 + threadIdx.x, step = gridDim.y * size;
+    const float *const partial = (second ? bias.partial : weight.partial) + blockIdx.y * size;
+    float *const to = const_cast<float *>(second ? bias.out.p : weight.out.p) + blockIdx.y * (second ? bias.out.stride : weight.out.stride);
+    const int parts = second ? bias.parts : weight.parts;
+    if (k >= size) return;
+    float total = 0.f;
+#pragma unroll 8
+    for (int part = 0; part < parts; ++part) total += partial[part * step + k];
+    to[k] = accumulate ? total + to[k] : total;
+}
+
 // dz, of T or fp32 values, for both products.
 template <class TL, class T, class TD>
 SVGD_TILE_KERNEL void linear_gradients_kernel(LinearShape s, TileGrid input, Rows<const TD> dz, Params weight, Rows<T> dx, float *dx_partial, WeightGrad<T, TD> grad, bool accumulate)
