@@ -41,8 +41,8 @@ struct AttnArgs {
 
 // Which particle, sequence, key head, tile and part a workgroup has.  Workgroups go round the eight dies in turn; a die gets ones that follow one another.  Four heads, whose keys meet in its L2, take turns
 // tile by tile, so that of causal ones the longest of four heads come first and the shortest last: head after head the last head's longest would be left over at the end.  Where a die has less than four heads
-// of its own, all heads take turns: otherwise one die would get a head's long tiles and another its short ones (4 x 2 x 2,000 x 8 heads over 2 of 64 fp16, causal, with documents: forward 89 us, so 68; 2 x 2,048 x 8
-// heads of 64 bf16, causal, queries in two parts 38.5, so 32.4).
+// of its own, all heads take turns: otherwise one die would get a head's long tiles and another its short ones (4 x 2 x 2,000 x 8 heads over 2 of 64 fp16, causal, with documents: forward 89 us, so 68, both with two blocks to
+// a wave; 2 x 2,048 x 8 heads of 64 bf16, causal, queries in two parts 38.5, so 32.4).
 struct AttnBlock {
     static constexpr int kHeads = 4;
     int particle, batch, head, tile, part;
