@@ -339,7 +339,7 @@ constexpr float kTanhSmall = 0.5f;
 __device__ __forceinline__ float tanh_small(float x)
 {
     const float u = x * x;
-    return x * __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.01714132f, -0.05298924f), 0.13324828f), -0.33333072f), 1.f);
+    return x * __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.01714132f, -0.05298924f), 0.13324828f), -0.3333307f), 1.f);
 }
 __device__ __forceinline__ float tanh_any(float x)
 {
