@@ -6,7 +6,8 @@
  * then the gated feed-forward half.
  *
  * Conventions: those of svgd_layers.h (activations of one svgd_dtype, parameters fp32 in the rows of X, their gradients in G, sums, products
- * and softmax statistics in fp32 or more, `accumulate`, `stream`, status, no synchronisation or allocation, the same inputs give the same
+ * and softmax statistics in fp32 or more - 16-bit attention's probabilities and gradients of scores, once they are operands of a product, in two
+ * parts of the activations' type, 2^-17 of bf16 ones and 2^-22 of fp16 ones -, `accumulate`, `stream`, status, no synchronisation or allocation, the same inputs give the same
  * bits), and for activations with heads
  *   - n particles x `batch` sequences x `length` tokens x `heads` heads x `dim` values, described by svgd_heads: value c of head h of
  *     token t of sequence b of particle i is element i * particle_stride + b * batch_stride + t * token_stride + h * head_stride + c of

@@ -2,8 +2,7 @@
 // streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse: four products and five for the forward pass's two.  4 x 2 x 4,096 x 16 heads of 64 bf16, causal:
 // 637 us (550 Gflop, 863 TFLOP/s) and 860 us (687 Gflop, 800 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197 x 6 heads of 64 bf16: 27.2 and 34.2, four tiles each.
 //     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
-// P is rounded to the activations' type for the product with do: half a step of each, with signs as random as those of the gradients' own rounding.  dz goes into the products with k and q in two
-// such parts (BlockScale: fp16): rounded to one, its roundings and those of o, from which delta comes, would together put dq and dk of short sequences off by 1.7 times what rounding the results does,
+// P goes into the product with do, and dz into those with k and q, in two parts of the activations' type (BlockScale: fp16).  P rounded to one would put dv off by 1.4 times what rounding it does; dz rounded to one, its roundings and those of o, from which delta comes, would together put dq and dk of short sequences off by 1.7 times what rounding the results does,
 // with two parts by 1.35; with delta as `exact_delta` says by 1.00 up to 64 keys, and beyond by 1.25 at most.
 #pragma once
 #include "attention_common.hpp"
@@ -250,14 +249,14 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                         s[1][b] *= bs.scale;
                     }
                 }
-                Frag<T> z[QB][kZParts<T>];
+                Frag<T> z[QB][kOperands<T>];
 #pragma unroll
                 for (int b = 0; b < QB; ++b) as_parts<T>(s[0][b], s[1][b], sc, z[b]);
 #pragma unroll
                 for (int d = 0; d < 2 * KD; ++d) {
                     const Frag<T> f = TL::columns(kl, 32 * m, 16 * d);
 #pragma unroll
-                    for (int part = 0; part < kZParts<T>; ++part)
+                    for (int part = 0; part < kOperands<T>; ++part)
 #pragma unroll
                         for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, z[b][part], acc[d][b]);
                 }
@@ -522,10 +521,10 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                         dp[1][b] *= bs.scale;
                     }
                 }
-                Frag<T> p[KB], z[KB][kZParts<T>];
+                Frag<T> p[KB][kOperands<T>], z[KB][kOperands<T>];
 #pragma unroll
                 for (int b = 0; b < KB; ++b) {
-                    p[b] = as_operand<T>(s[0][b], s[1][b], sc);
+                    as_parts<T>(s[0][b], s[1][b], sc, p[b]);
                     as_parts<T>(dp[0][b], dp[1][b], sc, z[b]);
                 }
                 constexpr int kAtOnce = !kDeep ? 1 : KD <= 2 ? 2 * KD : KD; // operands
@@ -541,11 +540,13 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
 #pragma unroll
                     for (int d = 0; d < kAtOnce; ++d)
 #pragma unroll
-                        for (int b = 0; b < KB; ++b) acc_v[d0 + d][b] = mma(f[d], p[b], acc_v[d0 + d][b]);
+                        for (int part = 0; part < kOperands<T>; ++part)
+#pragma unroll
+                            for (int b = 0; b < KB; ++b) acc_v[d0 + d][b] = mma(f[d], p[b][part], acc_v[d0 + d][b]);
 #pragma unroll
                     for (int d = 0; d < kAtOnce; ++d)
 #pragma unroll
-                        for (int part = 0; part < kZParts<T>; ++part)
+                        for (int part = 0; part < kOperands<T>; ++part)
 #pragma unroll
                             for (int b = 0; b < KB; ++b) acc_k[d0 + d][b] = mma(e[d], z[b][part], acc_k[d0 + d][b]);
                 }

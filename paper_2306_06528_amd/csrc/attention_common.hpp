@@ -286,10 +286,11 @@ template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 
     }
 }
 
-// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it; fp32 is one operand.
-template <class T> constexpr int kZParts = 2;
-template <> inline constexpr int kZParts<float> = 1;
-template <class T> __device__ __forceinline__ void as_parts(f32x4 a, f32x4 b, const SplitConst &sc, Frag<T> (&out)[kZParts<T>])
+// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it, which is little beside the 2^-9 or 2^-12 that an output's own rounding takes: how probabilities and the gradients of scores
+// become operands.  fp32 is one operand.
+template <class T> constexpr int kOperands = 2;
+template <> inline constexpr int kOperands<float> = 1;
+template <class T> __device__ __forceinline__ void as_parts(f32x4 a, f32x4 b, const SplitConst &sc, Frag<T> (&out)[kOperands<T>])
 {
     out[0] = as_operand<T>(a, b, sc);
     if constexpr (std::is_same<T, bf16_t>::value) { // (what is left of a pair: one dot product each, see split3)
