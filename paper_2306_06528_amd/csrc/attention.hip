@@ -98,17 +98,19 @@ template <class F> int for_type(int dtype, F f) { return dtype == SVGD_F32 ? f(f
 
 size_t rounded(size_t floats) { return (floats + 3) / 4 * 4; }
 
-// Scratch memory of the backward pass, in floats: delta, the slopes' rows (and their parts), parts' sums of dq or of dk and dv, which come after them.
+// Scratch memory of the backward pass, in floats: delta, the slopes' rows, where queries' rows are in parts these parts' sums of dz (and with slopes two more), parts' sums of dq (and of the keys' means, which 16 bits
+// need) or of dk and dv, which come after them.
 struct BackwardScratch {
-    size_t slopes, partial, total;
+    size_t slopes, sums, partial, total;
     explicit BackwardScratch(const svgd_attention &p)
     {
         const AttnArgs a = args_of(p);
         const size_t lines = lines_of(p), key_lines = (size_t)p.n * p.batch * p.kv_heads * p.keys;
         const size_t qs = query_splits(a), ks = key_splits(a), ld = padded_dim(a);
         slopes = rounded(lines);
-        partial = slopes + (p.slopes ? rounded(lines * (qs > 1 ? 1 + 3 * qs : 1)) : 0);
-        const size_t of_q = qs > 1 ? qs * lines * ld : 0, of_k = ks > 1 ? ks * key_lines * 2 * ld : 0;
+        sums = slopes + (p.slopes ? rounded(lines) : 0);
+        partial = sums + (qs > 1 ? rounded(lines * qs * (p.slopes ? 3 : 1)) : 0);
+        const size_t of_q = qs > 1 ? qs * lines * 2 * ld : 0, of_k = ks > 1 ? ks * key_lines * 2 * ld : 0;
         total = partial + (of_q > of_k ? of_q : of_k);
     }
 };
@@ -200,6 +202,7 @@ int svgd_attention_backward(int dtype, const svgd_attention *p, svgd_heads d_o, 
     c.delta = (const float *)scratch;
     const BackwardScratch parts(*p);
     c.slope_rows = dslopes ? (float *)scratch + parts.slopes : nullptr;
+    c.row_sums = (float *)scratch + parts.sums;
     c.partial = (float *)scratch + parts.partial;
     c.stream = (hipStream_t)stream;
     if (p->batch > 0 && p->length > 0) {

@@ -1,17 +1,20 @@
 // Attention, backward, without atomics: one kernel has rows of its own and streams keys and values past them (dq, and the slopes' gradients row by row), the other has keys of its own and
-// streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse: four products and five for the forward pass's two.  4 x 2 x 4,096 x 16 heads of 64 bf16, causal:
-// 637 us (550 Gflop, 863 TFLOP/s) and 860 us (687 Gflop, 800 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197 x 6 heads of 64 bf16: 27.2 and 34.2, four tiles each.
+// streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse: five products and six of 16-bit activations for the forward pass's three.  4 x 2 x 4,096 x 16 heads of 64 bf16, causal:
+// 755 us (687 Gflop, 910 TFLOP/s) and 905 us (825 Gflop, 911 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197 x 6 heads of 64 bf16: 30.2 and 36.9, four tiles each.
 //     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
-// P goes into the product with do, and dz into those with k and q, in two parts of the activations' type (BlockScale: fp16).  P rounded to one would put dv off by 1.4 times what rounding it does; dz rounded to one, its roundings and those of o, from which delta comes, would together put dq and dk of short sequences off by 1.7 times what rounding the results does,
-// with two parts by 1.35; with delta as `exact_delta` says by 1.00 up to 64 keys, and beyond by 1.25 at most.
+// P goes into the product with do, and dz into those with k and q, in two parts of the activations' type (BlockScale: fp16), and delta is made free of o's rounding (kRestore): dq, dk and dv are off by 1.00 times what
+// rounding them does, whether a row sees 3 keys or 4,096.  P in one part would make that 1.4 for dv, delta of o as it is stored 1.1 to 1.8 for dq and dk, the more the fewer keys count.
 #pragma once
 #include "attention_common.hpp"
 
 namespace svgd {
 
-// o as it was stored leaves delta off by its roundings, which of few keys are not small beside dz's own and do not cancel.  Where all keys are in one tile, the queries' kernel makes delta from P and dP instead (another two
-// products of that tile); 16-bit activations.
-template <class T> __host__ __device__ inline bool exact_delta(const AttnArgs &a) { return sizeof(T) == 2 && a.s <= kTileRows; }
+// o as it was stored leaves delta off by its roundings: by eps, which of rows that see few keys, or few that count, is not small beside dz and does not cancel.  The sum of a row's dz is 0, so made with the delta at hand it
+// is eps, and
+//     dz = dz0 - eps P,   dq = scale (sum dz0 damp k - eps sum P damp k)
+// The kernel that has queries of its own adds up the two sums beside dq's (a fifth product; P in one part does, eps being 2^-9 of delta), and leaves delta + eps for the kernel that has keys of its own.  Not for fp32, whose o
+// is rounded as every sum is.
+template <class T> constexpr bool kRestore = sizeof(T) == 2;
 
 // One of two forms of a loop, the same for the whole wave.
 template <class F> __device__ __forceinline__ void with_mask(bool masked, F f)
@@ -20,7 +23,7 @@ template <class F> __device__ __forceinline__ void with_mask(bool masked, F f)
     else f(std::false_type{});
 }
 
-// delta of every row, 16 lanes each, where the kernel that has queries of its own, which makes it otherwise, is not wanted.
+// delta of every row, 16 lanes each, where the kernel that has queries of its own, which makes it otherwise, is not wanted: fp32.
 template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel(AttnArgs a, Heads<const T> o, Heads<const T> d_o, float *delta)
 {
     const int64_t k = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), lines = (int64_t)a.n * a.batch * a.t * a.heads;
@@ -38,9 +41,12 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
     if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
 }
 
+// (Heads of 33 to 64 values, fp16, capped, take 170 registers left to themselves, two more than leave room for three waves: 4 x 2 x 2,000 x 8 heads over 2 of 64, causal, 7 documents 116 us, so 97.)
+template <int KDX> constexpr int kWavesOfQueries = KDX == 2 ? 3 : kWavesPerSimd;
+
 template <class T, int KDX, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
-                                                                                                              Heads<const T> o, const float *lse, float *delta, Heads<T> dq, float *slope_rows, float *partial)
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesOfQueries<KDX>))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+                                                                                                              Heads<const T> o, const float *lse, float *delta, Heads<T> dq, float *slope_rows, float *row_sums, float *partial)
 {
     constexpr int QB = 1; // blocks of 16 rows of a wave's own (attention_launch.hpp)
     constexpr int KD = kBlocks32<KDX>;
@@ -98,14 +104,17 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     const int wave_row = min(own + 16 * QB, a.rows) - 1;
     const int wave_limit = own >= a.rows ? 0 : masks.documents ? hi : masks.end(a, masks.start + a.query(wave_row));
 
-    f32x4 acc[2 * KD][QB];
+    f32x4 acc[2 * KD][QB], mean[kRestore<T> ? 2 * KD : 1][QB]; // of dz k and of P k
     float sum_dz[QB], sum_dz_far[QB], sum_far[QB]; // of dz, dz distance and P distance
     BlockScale bs;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         sum_dz[b] = sum_dz_far[b] = sum_far[b] = 0.f;
 #pragma unroll
-        for (int d = 0; d < 2 * KD; ++d) acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int d = 0; d < 2 * KD; ++d) {
+            acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (kRestore<T>) mean[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     }
     const T *const ks = k.at(at.particle, at.batch, at.head), *const vs = v.at(at.particle, at.batch, at.head);
     TL kt, vt;
@@ -130,53 +139,6 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     }
     loads_done();
     __syncthreads();
-    if (exact_delta<T>(a)) {
-        float sum[QB], total[QB]; // of P dP and of P
-#pragma unroll
-        for (int b = 0; b < QB; ++b) sum[b] = total[b] = 0.f;
-        if (begin < end && 0 < wave_limit)
-#pragma unroll 1
-            for (int key = 0; key < kRows; key += 16) {
-                f32x4 s[1][QB], dp[QB];
-#pragma unroll
-                for (int b = 0; b < QB; ++b) s[0][b] = dp[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < KD; ++c) {
-                    const Frag<T> f = TL::rows(lds, key, 32 * c), e = TL::rows(lds + TL::kSize, key, 32 * c);
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) {
-                        s[0][b] = mma(f, qf[b][c], s[0][b]);
-                        dp[b] = mma(e, df[b][c], dp[b]);
-                    }
-                }
-                if constexpr (MOD) modified.template apply<T>(s);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at_key = key + 4 * g + e;
-                    const int doc = masks.documents ? key_documents[0][at_key] : 0;
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) {
-                        float x = s[0][b][e];
-                        if constexpr (MOD) x = modified.exponent(x, slope[b], fabsf((float)(position[b] - at_key)));
-                        if (at_key >= limit[b] || doc != document[b]) x = -INFINITY;
-                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
-                        sum[b] += p * dp[b][e];
-                        total[b] += p;
-                    }
-                }
-            }
-#pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            const float all = sum_over_rows(total[b]), del = all > 0.f ? sum_over_rows(sum[b]) / all : 0.f;
-            less[b] = f32x4{-del, -del, -del, -del};
-        }
-    }
-    if (g == 0 && at.part == 0)
-#pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            const int r = own + 16 * b + lane, i = a.query(min(r, a.rows - 1));
-            if (r < a.rows) delta[a.line(at.particle, at.batch, at.head * a.group + r - i * a.group, i)] = -less[b][0];
-        }
     int half = 0;
     for (int n = begin; n < end; ++n) {
         if (n + 1 < end) fetch(n + 1);
@@ -219,15 +181,19 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                                 [[maybe_unused]] const float far = fabsf((float)(position[b] - at_key)), t = x;
                                 if constexpr (MOD) x = biased ? modified.exponent(t, slope[b], far) : t * modified.out;
                                 if (masked && (at_key >= limit[b] || doc != document[b])) x = -INFINITY;
-                                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b]));
-                                float dz = p * dp[j][b][e];
+                                float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, mul, -log[b])), dz = p * dp[j][b][e];
+                                if (biased || kRestore<T>) sum_dz[b] += dz;
                                 if (biased) {
-                                    sum_dz[b] += dz;
                                     sum_dz_far[b] += dz * far;
                                     sum_far[b] += p * far;
                                 }
-                                if constexpr (MOD) dz *= modified.damp(t);
+                                if constexpr (MOD) {
+                                    const float damp = modified.damp(t);
+                                    dz *= damp;
+                                    p *= damp;
+                                }
                                 s[j][b][e] = dz;
+                                dp[j][b][e] = p;
                                 if constexpr (std::is_same<T, f16_t>::value) largest = fmaxf(largest, fabsf(dz));
                             }
                         }
@@ -249,9 +215,12 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                         s[1][b] *= bs.scale;
                     }
                 }
-                Frag<T> z[QB][kOperands<T>];
+                Frag<T> z[QB][kOperands<T>], p[QB];
 #pragma unroll
-                for (int b = 0; b < QB; ++b) as_parts<T>(s[0][b], s[1][b], sc, z[b]);
+                for (int b = 0; b < QB; ++b) {
+                    as_parts<T>(s[0][b], s[1][b], sc, z[b]);
+                    if constexpr (kRestore<T>) p[b] = as_operand<T>(dp[0][b], dp[1][b], sc);
+                }
 #pragma unroll
                 for (int d = 0; d < 2 * KD; ++d) {
                     const Frag<T> f = TL::columns(kl, 32 * m, 16 * d);
@@ -259,6 +228,9 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
                     for (int part = 0; part < kOperands<T>; ++part)
 #pragma unroll
                         for (int b = 0; b < QB; ++b) acc[d][b] = mma(f, z[b][part], acc[d][b]);
+                    if constexpr (kRestore<T>)
+#pragma unroll
+                        for (int b = 0; b < QB; ++b) mean[d][b] = mma(f, p[b], mean[d][b]);
                 }
             }
         }
@@ -272,32 +244,46 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     for (int b = 0; b < QB; ++b) {
         const int r = own + 16 * b + (lane & 15);
         const int i = a.query(min(r, a.rows - 1)), h = at.head * a.group + min(r, a.rows - 1) - i * a.group;
+        const int64_t line = a.line(at.particle, at.batch, h, i), lines = (int64_t)a.n * a.batch * a.heads * a.t;
+        const float eps = kRestore<T> || MOD ? sum_over_rows(sum_dz[b]) : 0.f;
+        if (r < a.rows && g == 0) {
+            if (at.part == 0) delta[line] = kRestore<T> && a.splits == 1 ? eps - less[b][0] : -less[b][0];
+            if ((kRestore<T> || MOD) && a.splits > 1) row_sums[at.part * lines + line] = eps;
+        }
         if constexpr (MOD) {
-            // The sum of dz is 0 but for roundings, those of delta the largest: what they put on the sum with the distances is taken off (the probabilities add up to 1)
-            const float z = sum_over_rows(sum_dz[b]), zf = sum_over_rows(sum_dz_far[b]), f = sum_over_rows(sum_far[b]);
+            // What delta's error puts on the sum with the distances is taken off, in fp32 too (the probabilities add up to 1)
+            const float zf = sum_over_rows(sum_dz_far[b]), f = sum_over_rows(sum_far[b]);
             if (a.slopes && slope_rows && r < a.rows && g == 0) {
-                const int64_t line = a.line(at.particle, at.batch, h, i), lines = (int64_t)a.n * a.batch * a.heads * a.t;
                 if (a.splits > 1) {
-                    slope_rows[(1 + 3 * at.part) * lines + line] = z;
-                    slope_rows[(2 + 3 * at.part) * lines + line] = zf;
-                    slope_rows[(3 + 3 * at.part) * lines + line] = f;
+                    row_sums[(a.splits + 2 * at.part) * lines + line] = zf;
+                    row_sums[(a.splits + 2 * at.part + 1) * lines + line] = f;
                 } else {
-                    slope_rows[line] = z * f - zf;
+                    slope_rows[line] = eps * f - zf;
                 }
             }
         }
         if (r >= a.rows || !dq.p) continue;
         if (a.splits > 1) {
-            float *const out = partial + (at.part * ((int64_t)a.n * a.batch * a.heads * a.t) + a.line(at.particle, at.batch, h, i)) * (32 * KD);
+            constexpr int kEach = kRestore<T> ? 64 * KD : 32 * KD;
+            float *const out = partial + (at.part * lines + line) * kEach;
 #pragma unroll
-            for (int d = 0; d < 2 * KD; ++d) *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = acc[d][b] * factor;
+            for (int d = 0; d < 2 * KD; ++d) {
+                *reinterpret_cast<f32x4 *>(out + 16 * d + 4 * g) = acc[d][b] * factor;
+                if constexpr (kRestore<T>) *reinterpret_cast<f32x4 *>(out + 32 * KD + 16 * d + 4 * g) = mean[d][b] * a.scale;
+            }
             continue;
         }
+        const float off = eps * a.scale;
         T *const out = dq.at(at.particle, at.batch, h) + i * dq.token;
 #pragma unroll
         for (int d = 0; d < 2 * KD; ++d) {
             const int c = 16 * d + 4 * g;
-            const float x[4] = {acc[d][b][0] * factor, acc[d][b][1] * factor, acc[d][b][2] * factor, acc[d][b][3] * factor};
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = acc[d][b][e] * factor;
+                if constexpr (kRestore<T>) x[e] = __builtin_fmaf(-off, mean[d][b][e], x[e]);
+            }
             if (c < a.dim) store_pack<T, 4>(out + c, a.dim - c, x);
         }
     }
@@ -582,11 +568,57 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     }
 }
 
-// The parts' sums, in order, as T: a thread has four values of a line's `each` tensors of ld floats (dq; dk and dv), whose heads are `heads`, tokens `tokens`.
-template <class T> __global__ __launch_bounds__(256) void attention_sum_kernel(AttnArgs a, int heads, int tokens, int each, int ld, const float *partial, Heads<T> first, Heads<T> second)
+// dq from the parts' sums, in order, and what eps puts on delta: a thread has four values of a line's ld (dq null, not wanted: delta alone, a thread a line).
+template <class T> __global__ __launch_bounds__(256) void attention_query_sums_kernel(AttnArgs a, int ld, const float *partial, const float *row_sums, float *delta, Heads<T> dq)
 {
-    const int64_t lines = (int64_t)a.n * a.batch * heads * tokens;
-    const int quads = each * ld / 4;
+    const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t;
+    const int quads = dq.p ? ld / 4 : 1, each = kRestore<T> ? 2 * ld : ld;
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, line = k / quads;
+    const int c = (int)(k - line * quads) * 4;
+    if (line >= lines || c >= a.dim) return;
+    constexpr int U = kRestore<T> ? 4 : 8; // on their way together
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f}, mean = {0.f, 0.f, 0.f, 0.f};
+    float eps = 0.f;
+    for (int p0 = 0; p0 < a.splits; p0 += U) {
+        f32x4 x[U], y[U];
+        float z[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t p = min(p0 + u, a.splits - 1);
+            const float *const from = partial + (p * lines + line) * each + c;
+            if (dq.p) x[u] = *reinterpret_cast<const f32x4 *>(from);
+            if constexpr (kRestore<T>) {
+                if (dq.p) y[u] = *reinterpret_cast<const f32x4 *>(from + ld);
+                z[u] = row_sums[p * lines + line];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p0 + u >= a.splits) continue;
+            if (dq.p) sum += x[u];
+            if constexpr (kRestore<T>) {
+                if (dq.p) mean += y[u];
+                eps += z[u];
+            }
+        }
+    }
+    if constexpr (kRestore<T>) {
+        if (c == 0) delta[line] += eps;
+        sum -= eps * mean;
+    }
+    if (!dq.p) return;
+    const int i = (int)(line % a.t);
+    const int64_t head = line / a.t;
+    const int h = (int)(head % a.heads), b = (int)(head / a.heads % a.batch), particle = (int)(head / a.heads / a.batch);
+    const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
+    store_pack<T, 4>(dq.at(particle, b, h) + i * dq.token + c, a.dim - c, x);
+}
+
+// dk and dv from the parts' sums, in order: a thread has four values of a line's two times ld.
+template <class T> __global__ __launch_bounds__(256) void attention_key_sums_kernel(AttnArgs a, int ld, const float *partial, Heads<T> dk, Heads<T> dv)
+{
+    const int64_t lines = (int64_t)a.n * a.batch * a.kv * a.s;
+    const int quads = ld / 2;
     const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x, line = k / quads;
     const int at = (int)(k - line * quads) * 4, which = at / ld, c = at - which * ld;
     if (line >= lines || c >= a.dim) return;
@@ -595,30 +627,30 @@ template <class T> __global__ __launch_bounds__(256) void attention_sum_kernel(A
     for (int p0 = 0; p0 < a.splits; p0 += U) {
         f32x4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const f32x4 *>(partial + (min(p0 + u, a.splits - 1) * lines + line) * (each * ld) + at);
+        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const f32x4 *>(partial + (min(p0 + u, a.splits - 1) * lines + line) * (2 * ld) + at);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (p0 + u < a.splits) sum += x[u];
     }
-    const Heads<T> &to = which ? second : first;
+    const Heads<T> &to = which ? dv : dk;
     if (!to.p) return;
-    const int i = (int)(line % tokens);
-    const int64_t head = line / tokens;
-    const int h = (int)(head % heads), b = (int)(head / heads % a.batch), particle = (int)(head / heads / a.batch);
+    const int i = (int)(line % a.s);
+    const int64_t head = line / a.s;
+    const int h = (int)(head % a.kv), b = (int)(head / a.kv % a.batch), particle = (int)(head / a.kv / a.batch);
     const float x[4] = {sum[0], sum[1], sum[2], sum[3]};
     store_pack<T, 4>(to.at(particle, b, h) + i * to.token + c, a.dim - c, x);
 }
 
-// The rows' terms of the slopes' gradients from the parts'.
-static __global__ __launch_bounds__(256) void attention_slope_rows_kernel(AttnArgs a, float *slope_rows)
+// The rows' terms of the slopes' gradients from the parts': the sums of dz, and by turns those of dz and of P with the distances.
+static __global__ __launch_bounds__(256) void attention_slope_rows_kernel(AttnArgs a, const float *row_sums, float *slope_rows)
 {
     const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t, line = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (line >= lines) return;
     float z = 0.f, zf = 0.f, f = 0.f;
     for (int p = 0; p < a.splits; ++p) {
-        z += slope_rows[(1 + 3 * p) * lines + line];
-        zf += slope_rows[(2 + 3 * p) * lines + line];
-        f += slope_rows[(3 + 3 * p) * lines + line];
+        z += row_sums[p * lines + line];
+        zf += row_sums[(a.splits + 2 * p) * lines + line];
+        f += row_sums[(a.splits + 2 * p + 1) * lines + line];
     }
     slope_rows[line] = z * f - zf;
 }

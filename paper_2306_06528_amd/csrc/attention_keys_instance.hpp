@@ -27,6 +27,6 @@ template <> int svgd::attention_keys<SVGD_ATTENTION_TYPE>(AttnCall &c)
     if (rc || a.splits == 1) return rc;
     const int ld = padded_dim(a);
     const int64_t lines = (int64_t)a.n * a.batch * a.kv * a.s;
-    attention_sum_kernel<T><<<(unsigned)ceil_div(lines * (ld / 2), 256), 256, 0, c.stream>>>(a, a.kv, a.s, 2, ld, c.partial, out<T>(c.dk), out<T>(c.dv));
+    attention_key_sums_kernel<T><<<(unsigned)ceil_div(lines * (ld / 2), 256), 256, 0, c.stream>>>(a, ld, c.partial, out<T>(c.dk), out<T>(c.dv));
     return launched_ok();
 }

@@ -8,7 +8,7 @@ struct AttnCall {
     AttnArgs a;
     svgd_heads q, k, v, o, d_o, dq, dk, dv;
     const float *lse, *delta;
-    float *lse_out, *partial, *partial_lse, *slope_rows;
+    float *lse_out, *partial, *partial_lse, *slope_rows, *row_sums;
     hipStream_t stream;
 };
 

@@ -8,10 +8,11 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
     AttnArgs &a = c.a;
     const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t;
     float *const delta = const_cast<float *>(c.delta);
-    if (!c.dq.data && !c.slope_rows && !exact_delta<T>(a)) {
-        attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), delta);
-        return launched_ok();
-    }
+    if constexpr (!kRestore<T>)
+        if (!c.dq.data && !c.slope_rows) {
+            attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), delta);
+            return launched_ok();
+        }
     int rc = with_dim<T>(a.dim, [&](auto kd) {
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
@@ -19,18 +20,19 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
             set_grid(a, a.rows, 16 * kAttnWaves, query_splits(a));
             const int grid = a.per_die * 8;
             attention_queries_kernel<T, KD, MOD>
-                <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), in<T>(c.o), c.lse, delta, out<T>(c.dq), c.slope_rows, c.partial);
+                <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), in<T>(c.o), c.lse, delta, out<T>(c.dq), c.slope_rows, c.row_sums,
+                                                                            c.partial);
             return launched_ok();
         });
     });
     if (rc || a.splits == 1) return rc;
-    if (c.dq.data) {
+    if (c.dq.data || kRestore<T>) {
         const int ld = padded_dim(a);
-        attention_sum_kernel<T><<<(unsigned)ceil_div(lines * (ld / 4), 256), 256, 0, c.stream>>>(a, a.heads, a.t, 1, ld, c.partial, out<T>(c.dq), Heads<T>{});
+        attention_query_sums_kernel<T><<<(unsigned)ceil_div(lines * (c.dq.data ? ld / 4 : 1), 256), 256, 0, c.stream>>>(a, ld, c.partial, c.row_sums, delta, out<T>(c.dq));
         if ((rc = launched_ok())) return rc;
     }
     if (c.slope_rows) {
-        attention_slope_rows_kernel<<<(unsigned)ceil_div(lines, 256), 256, 0, c.stream>>>(a, c.slope_rows);
+        attention_slope_rows_kernel<<<(unsigned)ceil_div(lines, 256), 256, 0, c.stream>>>(a, c.row_sums, c.slope_rows);
         rc = launched_ok();
     }
     return rc;

@@ -1,4 +1,4 @@
-"""Attention of 16-bit activations holds in fp32 what it sums up: o and dv are off from the exact result, in the root mean square, by what rounding that result does.
+"""Attention of 16-bit activations holds in fp32 what it sums up: o, dq, dk and dv are off from the exact result, in the root mean square, by what rounding that result does.
 
 How near to 1 the ratio has to be: what an output is rounded to is off by step / sqrt(12) where the value is in its binade, 2^-9.3 (bf16) or 2^-12.3 (fp16) of it on an average.  What comes before, the fp32 sums,
 exponents of at most 2^5 or so (2^-24 2^5 of a probability) and operands in two parts (2^-17 of bf16, 2^-22 of fp16), is below 2^-16.3 of the values, a sixteenth of that and mostly independent of it: the
@@ -82,3 +82,31 @@ def run(att, name, dtype):
 def test_sums_of_probabilities(att, name, dtype):
     off = run(att, name, dtype)
     assert off["o"] <= MOST and off["dv"] <= MOST, off
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("name", CASES)
+def test_gradients_of_scores(att, name, dtype):
+    """Rows that see few keys, or few that count: what o's rounding leaves delta off by is not in dq and dk."""
+    off = run(att, name, dtype)
+    assert off["dq"] <= MOST and off["dk"] <= MOST, off
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("documents_of", [7, 1])
+def test_keys_alone(att, documents_of, dtype):
+    """dk and dv are the same whether dq is wanted or not, with queries' rows in parts too.  A document of one token: its probability is 1 whatever its score, so dq and dk are 0 but for fp32's roundings of dP - delta,
+    (d + 8) 2^-24 of sum |do v|, times the other operand."""
+    n, batch, t, heads, kv, d = 1, 1, 1_700, 2, 1, 32
+    q, do = (normal(("alone", x), n, batch, t, heads, d, dtype=dtype) for x in "qd")
+    k, v = (normal(("alone", x), n, batch, t, kv, d, dtype=dtype) for x in "kv")
+    how = {"causal": True, "documents": documents(documents_of, batch, t)}
+    o, lse = att.attention_forward(q, k, v, **how)
+    dq, dk, dv = att.attention_backward(do, q, k, v, o, lse, **how)
+    none, dk2, dv2 = att.attention_backward(do, q, k, v, o, lse, want_dq=False, **how)
+    assert none is None and torch.equal(dk, dk2) and torch.equal(dv, dv2)
+    if documents_of == 1:
+        far = (d + 8) * 2.0 ** -24 * (do.float().abs() * v.float().abs()).sum(-1, keepdim=True) * d ** -0.5
+        small = 2.0 ** -25 if dtype == torch.float16 else 0.0  # (half of fp16's smallest step)
+        assert (dq.float().abs() <= 2 * far * k.float().abs() + small).all()
+        assert (dk.float().abs() <= 2 * (far * q.float().abs()).sum(3, keepdim=True) + small).all()
