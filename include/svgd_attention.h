@@ -12,7 +12,8 @@
  *   - n particles x `batch` sequences x `length` tokens x `heads` heads x `dim` values, described by svgd_heads: value c of head h of
  *     token t of sequence b of particle i is element i * particle_stride + b * batch_stride + t * token_stride + h * head_stride + c of
  *     `data`.  Inputs may have any strides from 0 on, a view into the results of one linear map among them; outputs' heads must not
- *     overlap.
+ *     overlap, nor any other argument's values.  Two tensors whose addresses go through each other pass if their outer dimensions are
+ *     the same and what is inside of these lies side by side: dq, dk and dv as the parts of one gradient of q, k and v together.
  */
 #ifndef SVGD_ATTENTION_H
 #define SVGD_ATTENTION_H

@@ -134,13 +134,13 @@ int svgd_attention_forward(int dtype, const svgd_attention *p, svgd_heads q, svg
     if (p->batch == 0 || p->length == 0) return SVGD_OK;
     const size_t need = svgd_attention_forward_scratch(p), stats = lines_of(*p) * 4;
     if (!valid_heads_output(o, dtype, query_sizes(*p)) || !aligned_to(lse, 4) || (need && (!scratch || !aligned_to(scratch, 16) || scratch_bytes < need))) return SVGD_ERR_INVALID_ARG;
-    const Extent written[3] = {extent(o, dtype, query_sizes(*p)), extent(lse, lse ? stats : 0), extent(scratch, need)};
-    const Extent read[3] = {extent(q, dtype, query_sizes(*p)), extent(k, dtype, key_sizes(*p)), extent(v, dtype, key_sizes(*p))};
+    const HeadSizes qs = query_sizes(*p), ks = key_sizes(*p);
+    const Region written[3] = {{o, dtype, qs}, extent(lse, lse ? stats : 0), extent(scratch, need)}, read[3] = {{q, dtype, qs}, {k, dtype, ks}, {v, dtype, ks}};
     const MaskExtents masks(*p);
     for (int i = 0; i < 3; ++i) {
-        for (const Extent &r : read)
+        for (const Region &r : read)
             if (written[i].meets(r)) return SVGD_ERR_INVALID_ARG;
-        if (masks.meet(written[i])) return SVGD_ERR_INVALID_ARG;
+        if (masks.meet(written[i].all)) return SVGD_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
             if (written[i].meets(written[j])) return SVGD_ERR_INVALID_ARG;
     }
@@ -176,15 +176,14 @@ int svgd_attention_backward(int dtype, const svgd_attention *p, svgd_heads d_o, 
         (dk.data && !valid_heads_output(dk, dtype, ks)) || (dv.data && !valid_heads_output(dv, dtype, ks)) ||
         (need && (!scratch || !aligned_to(scratch, 16) || scratch_bytes < need)))
         return SVGD_ERR_INVALID_ARG;
-    const Extent written[5] = {extent(dq, dtype, qs), extent(dk, dtype, ks), extent(dv, dtype, ks), extent(scratch, need),
-                               dslopes ? extent(dslopes, dslopes_stride, p->n, p->heads) : Extent{0, 0}};
-    const Extent read[6] = {extent(q, dtype, qs), extent(k, dtype, ks), extent(v, dtype, ks), extent(d_o, dtype, qs), extent(o, dtype, qs), extent(lse, stats)};
+    const Region written[5] = {{dq, dtype, qs}, {dk, dtype, ks}, {dv, dtype, ks}, extent(scratch, need), dslopes ? extent(dslopes, dslopes_stride, p->n, p->heads) : Extent{0, 0}};
+    const Region read[6] = {{q, dtype, qs}, {k, dtype, ks}, {v, dtype, ks}, {d_o, dtype, qs}, {o, dtype, qs}, extent(lse, stats)};
     const MaskExtents masks(*p);
     for (int i = 0; i < 5; ++i) {
-        for (const Extent &r : read)
+        for (const Region &r : read)
             if (written[i].meets(r)) return SVGD_ERR_INVALID_ARG;
         for (int m = 0; m < (i < 4 ? 5 : 4); ++m) // (the slopes' gradients may lie between the slopes, in the same rows: looked at above)
-            if (masks.e[m].meets(written[i])) return SVGD_ERR_INVALID_ARG;
+            if (masks.e[m].meets(written[i].all)) return SVGD_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
             if (written[i].meets(written[j])) return SVGD_ERR_INVALID_ARG;
     }

@@ -1,16 +1,9 @@
 // Checks of tensors with heads (include/svgd_attention.h).
 #pragma once
+#include "heads_rules.hpp"
 #include "layer_common.hpp"
-#include "../../include/svgd_attention.h"
-
-#include <algorithm>
 
 namespace svgd {
-
-struct HeadSizes {
-    int64_t n, batch, tokens, heads, dim;
-    bool none() const { return batch == 0 || tokens == 0 || heads == 0; }
-};
 
 inline Extent extent(const svgd_heads &h, int dtype, const HeadSizes &s)
 {
@@ -45,5 +38,19 @@ inline bool valid_heads_output(const svgd_heads &h, int dtype, const HeadSizes &
     }
     return true;
 }
+
+// What a call reads or writes: a tensor with heads, or a stretch of memory.
+struct Region {
+    Extent all;
+    const svgd_heads *heads = nullptr;
+    HeadSizes sizes{};
+    int dtype = 0;
+    Region(const Extent &e) : all(e) {}
+    Region(const svgd_heads &h, int type, const HeadSizes &s) : all(extent(h, type, s)), heads(&h), sizes(s), dtype(type) {}
+    bool meets(const Region &o) const
+    {
+        return all.meets(o.all) && !(heads && o.heads && heads_apart(*heads, sizes, *o.heads, o.sizes, (int64_t)dtype_size(dtype)));
+    }
+};
 
 } // namespace svgd

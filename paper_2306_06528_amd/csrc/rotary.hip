@@ -96,11 +96,11 @@ int svgd_qk_norm_rotary_forward(int dtype, const svgd_rotary *p, svgd_heads q, s
     if (!valid_heads(q, dtype, qs) || !valid_heads(k, dtype, ks) || !valid_heads_output(q_out, dtype, qs) || !valid_heads_output(k_out, dtype, ks)) return SVGD_ERR_INVALID_ARG;
     if (qs.none() && ks.none()) return SVGD_OK;
     const Reads reads(*p);
-    const Extent written[2] = {extent(q_out, dtype, qs), extent(k_out, dtype, ks)}, inputs[2] = {extent(q, dtype, qs), extent(k, dtype, ks)};
-    for (const Extent &w : written) {
+    const Region written[2] = {{q_out, dtype, qs}, {k_out, dtype, ks}}, inputs[2] = {{q, dtype, qs}, {k, dtype, ks}};
+    for (const Region &w : written) {
         for (const Extent &r : reads.e)
             if (w.meets(r)) return SVGD_ERR_INVALID_ARG;
-        for (const Extent &r : inputs)
+        for (const Region &r : inputs)
             if (w.meets(r)) return SVGD_ERR_INVALID_ARG;
     }
     if (written[0].meets(written[1])) return SVGD_ERR_INVALID_ARG;
@@ -145,19 +145,19 @@ int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_
     if (!none) {
         const Reads reads(*p);
         const Extent work = extent(scratch, need);
-        const Extent written[2] = {extent(dq, dtype, qs), extent(dk, dtype, ks)};
+        const Region written[2] = {{dq, dtype, qs}, {dk, dtype, ks}};
         Extent grads[2];
         for (int i = 0; i < 2; ++i) grads[i] = g[i].p ? extent(g[i].p, g[i].stride, p->n, p->dim) : Extent{0, 0};
         const svgd_heads *const acts[4] = {&dq_out, &dk_out, &q, &k};
         for (int i = 0; i < (norm ? 4 : 2); ++i) {
             const HeadSizes &s = i % 2 ? ks : qs;
-            const Extent e = extent(*acts[i], dtype, s);
-            if (work.meets(e) || grads[0].meets(e) || grads[1].meets(e)) return SVGD_ERR_INVALID_ARG;
+            const Region e(*acts[i], dtype, s);
+            if (work.meets(e.all) || grads[0].meets(e.all) || grads[1].meets(e.all)) return SVGD_ERR_INVALID_ARG;
             if (written[0].meets(e) || written[1].meets(e)) return SVGD_ERR_INVALID_ARG;
         }
         if (written[0].meets(written[1])) return SVGD_ERR_INVALID_ARG;
-        for (const Extent &x : written) {
-            if (work.meets(x) || grads[0].meets(x) || grads[1].meets(x)) return SVGD_ERR_INVALID_ARG;
+        for (const Region &x : written) {
+            if (work.meets(x.all) || grads[0].meets(x.all) || grads[1].meets(x.all)) return SVGD_ERR_INVALID_ARG;
             for (const Extent &r : reads.e)
                 if (x.meets(r)) return SVGD_ERR_INVALID_ARG;
         }
