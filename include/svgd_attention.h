@@ -112,7 +112,7 @@ typedef struct svgd_attention {
     int n, heads, kv_heads, dim;
     int64_t batch, length, keys;
     int causal;
-    double scale, cap; /* scale and cap at least 1e-30; cap 0: none */
+    double scale, cap; /* scale and cap from 1e-30 to 2e38, scale / cap from 2^-126 to 3e38; cap 0: none */
     const float *slopes;
     int64_t slopes_stride;
     const int32_t *starts, *lengths, *documents, *prefix; /* DEVICE: batch, batch, batch x keys, batch values */

@@ -86,6 +86,8 @@ int check(int dtype, const svgd_attention *a, const svgd_heads &q, const svgd_he
     if (const int rc = check_sizes_of(a)) return rc;
     const float scale = (float)a->scale, cap = (float)a->cap; // (what does not fit fp32 is refused)
     if (!std::isfinite(scale) || !(scale > 0.f) || !std::isfinite(cap) || !(a->cap >= 0.0) || (a->cap > 0.0 && cap < 1e-30f) || scale < 1e-30f) return SVGD_ERR_INVALID_ARG;
+    // what the kernels make of them (Modified): times log2 e, and their quotient, which as a subnormal would have few digits
+    if (!std::isfinite(scale * kLog2e) || !std::isfinite(cap * kLog2e) || (cap > 0.f && !std::isnormal(scale / cap))) return SVGD_ERR_INVALID_ARG;
     if (a->slopes && !valid_params({a->slopes, a->slopes_stride, a->heads}, a->n, false)) return SVGD_ERR_INVALID_ARG;
     if (!aligned_to(a->starts, 4) || !aligned_to(a->lengths, 4) || !aligned_to(a->documents, 4) || !aligned_to(a->prefix, 4)) return SVGD_ERR_INVALID_ARG;
     if (far(q, a->heads / a->kv_heads, a->length) || far(k, 1, a->keys) || far(v, 1, a->keys)) return SVGD_ERR_TOO_LARGE;
