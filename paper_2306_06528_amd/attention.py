@@ -156,9 +156,11 @@ def linear(x, weight, bias=None, activation: str = "none", residual=None):
 
 
 def qk_norm_rotary(q, k, q_weight=None, k_weight=None, frequencies=None, positions=None, layout: str = "half", eps: float = 1e-6):
-    """Norms and rotation as an autograd function of q, k and the weights."""
+    """Norms and rotation as an autograd function of q, k and the weights.  Frequencies have no gradient: ones that ask for it are refused."""
     if _no_derivatives():
         return qk_norm_rotary_forward(q, k, q_weight, k_weight, frequencies, positions, layout, eps)
+    if isinstance(frequencies, torch.Tensor) and frequencies.requires_grad and torch.is_grad_enabled():
+        raise ValueError("frequencies have no gradient: detach them")
     return _QkNormRotary.apply(q, k, q_weight, k_weight, frequencies, positions, layout, eps)
 
 
