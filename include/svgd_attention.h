@@ -58,7 +58,7 @@ int svgd_linear_forward(int dtype, int activation, int n, int64_t rows, int64_t 
  * Its backward pass:
  *     dz = dy act'(z),  dx = dz weight,  dweight = sum_t dz x^T,  dbias = sum_t dz
  * The residual's gradient is dy.  dx.data, dweight and dbias may be NULL: that gradient is not wanted then.  scratch (DEVICE, 16-byte
- * aligned): svgd_linear_scratch bytes.
+ * aligned): svgd_linear_scratch bytes; svgd_linear_saved bytes less without an activation, where dz is dy.
  */
 size_t svgd_linear_scratch(int n, int64_t rows, int64_t width, int64_t out);
 int svgd_linear_backward(int dtype, int activation, int n, int64_t rows, int64_t width, int64_t out, svgd_rows dy, svgd_rows x,

@@ -262,7 +262,8 @@ PyObject *linear_backward(PyObject *, PyObject *const *a, Py_ssize_t na)
         if (!current_stream(x, a, stream)) Py_RETURN_NONE;
         at::Tensor dx;
         if (want_dx) dx = new_like(x);
-        const size_t need = svgd_linear_scratch(x.particles(), x.rows(), x.width(), l.out);
+        const size_t all = svgd_linear_scratch(x.particles(), x.rows(), x.width(), l.out);
+        const size_t need = all && l.activation == SVGD_NO_ACTIVATION ? all - svgd_linear_saved(x.particles(), x.rows(), l.out) : all;
         const at::Tensor scratch = bytes(need, x);
         const int rc = unlocked([&] {
             return svgd_linear_backward(x.dtype(), l.activation, x.particles(), x.rows(), x.width(), l.out, dy.desc(), x.desc(), l.weight.p(), l.weight.stride,

@@ -92,9 +92,9 @@ int svgd_linear_backward(int dtype, int activation, int n, int64_t rows, int64_t
     for (const Params *g : {&c.dweight, &c.dbias})
         if (g->p && (!valid_params(*g, n, true) || params_meet(*g, c.weight, n))) return SVGD_ERR_INVALID_ARG;
     if (dweight && dbias && params_meet(c.dweight, c.dbias, n)) return SVGD_ERR_INVALID_ARG;
-    const LinearBackwardPlan plan(n, rows, width, out);
+    const bool act = activation != SVGD_NO_ACTIVATION;
+    const LinearBackwardPlan plan(n, rows, width, out, act);
     if (rows > 0) {
-        const bool act = activation != SVGD_NO_ACTIVATION;
         const size_t z_need = act ? svgd_linear_saved(n, rows, out) : 0, need = plan.scratch();
         if (!valid_input(dy, dtype, rows) || (act && (!z || !aligned_to(z, 16) || z_bytes < z_need)) || (dx.data && !valid_output(dx, dtype, n, rows, width)) || !scratch ||
             !aligned_to(scratch, 16) || scratch_bytes < need)

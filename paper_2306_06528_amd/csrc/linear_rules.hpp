@@ -23,13 +23,13 @@ struct LinearForwardPlan {
     size_t scratch(int n, int64_t rows, int64_t out) const { return tile.parts > 1 ? (size_t)tile.parts * n * rows * linear_ld(out) * 4 : 0; }
 };
 
-// dx and the weight's gradient: tiles of one kind, in one launch.  The bias's gradient: `sums` parts of the rows.
+// dx and the weight's gradient: tiles of one kind, in one launch.  The bias's gradient: `sums` parts of the rows.  Without an activation dz is dy and has no place in scratch memory.
 struct LinearBackwardPlan {
     TileKind kind = kLarge;
     int input_parts = 1, param_parts = 0, sums;
     int64_t sum_rows; // rows of each
     size_t dz_floats, input_floats, param_floats, sum_floats;
-    LinearBackwardPlan(int n, int64_t rows, int64_t width, int64_t out)
+    LinearBackwardPlan(int n, int64_t rows, int64_t width, int64_t out, bool activation = true)
     {
         double least = 1e30;
         for (int kd = 0; kd < kTileKinds; ++kd) {
@@ -55,7 +55,7 @@ struct LinearBackwardPlan {
         s = s < 1 ? 1 : s > 128 ? 128 : s;
         sum_rows = rows > 0 ? (rows + s - 1) / s : 1;
         sums = rows > 0 ? (int)((rows + sum_rows - 1) / sum_rows) : 0;
-        dz_floats = (size_t)n * rows * linear_ld(out);
+        dz_floats = activation ? (size_t)n * rows * linear_ld(out) : 0;
         input_floats = input_parts > 1 ? (size_t)input_parts * n * rows * linear_ld(width) : 0;
         param_floats = param_parts > 1 ? (size_t)param_parts * n * width * out : 0;
         sum_floats = sums > 1 ? (size_t)sums * n * out : 0;
