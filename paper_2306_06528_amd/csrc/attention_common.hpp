@@ -6,6 +6,7 @@
 // make a step of 32 whose k are ordered as k_of says, in A as in B.
 #pragma once
 #include "../../include/svgd_attention.h"
+#include "attention_rules.hpp"
 #include "layer_common.hpp"
 
 namespace svgd {
@@ -13,8 +14,6 @@ namespace svgd {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-constexpr int kTileRows = 64; // streamed rows (or keys) in LDS at a time
-constexpr int kAttnWaves = 4, kAttnBlock = 64 * kAttnWaves;
 constexpr int kMaxStart = 1 << 28;
 constexpr int64_t kMaxTokenStride = SVGD_ATTENTION_MAX_STRIDE; // (offsets within a tile fit 32 bits)
 
@@ -260,15 +259,8 @@ __device__ __forceinline__ void part_of(const AttnArgs &a, int part, int &begin,
     end = first + (int)((int64_t)count * (part + 1) / a.splits);
 }
 
-template <class T, int KD, bool TINY> using Tile64 = Tile<T, KD, TINY, kTileRows, kAttnBlock>;
-
 // What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
 constexpr int kWavesPerSimd = 2;
-
-// Whether a wave can have two blocks of 16 rows (or keys) of its own, which halves what it reads from LDS, without running out of registers.  (Capped scores of 16 bits could, but the waves that one block leaves room
-// for are worth more: 4 x 2 x 2,000 x 8 heads over 2 of 64 fp16 forward 71 us with two, 62 with one; keys, 4 x 4 x 4,096 x 8 heads of 64 bf16, causal, 1,071 and 1,012.)
-template <class T, int KDX, bool MOD> constexpr bool kTwoForward = !MOD && (sizeof(T) == 2 || KDX < 3);
-template <class T, int KDX, bool MOD> constexpr bool kTwoKeys = !MOD && KDX < (sizeof(T) == 2 ? 3 : 2);
 
 // Two results of 16 streamed rows each as a B operand.
 template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 b, const SplitConst &sc)

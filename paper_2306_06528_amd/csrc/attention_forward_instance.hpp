@@ -6,7 +6,7 @@ template <> int svgd::attention_forward<SVGD_ATTENTION_TYPE>(AttnCall &c)
 {
     typedef SVGD_ATTENTION_TYPE T;
     AttnArgs &a = c.a;
-    const int rc = with_dim<T>(a.dim, [&](auto kd) {
+    const int rc = with_dim(a.dim, [&](auto kd) {
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
@@ -15,10 +15,11 @@ template <> int svgd::attention_forward<SVGD_ATTENTION_TYPE>(AttnCall &c)
                 attention_few_kernel<T, KD, MOD><<<a.per_die * 8, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
                 return launched_ok();
             }
-            const bool two = kTwoForward<T, KD, MOD> && many_forward(a);
+            constexpr bool kTwo = two_forward(sizeof(T), KD, MOD);
+            const bool two = kTwo && many_forward(a);
             set_grid(a, a.rows, 16 * kAttnWaves * (two ? 2 : 1), forward_splits(a));
             const int grid = a.per_die * 8;
-            if constexpr (kTwoForward<T, KD, MOD>)
+            if constexpr (kTwo)
                 if (two) {
                     attention_forward_kernel<T, KD, 2, MOD><<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), out<T>(c.o), c.lse_out, c.partial, c.partial_lse);
                     return launched_ok();

@@ -6,14 +6,15 @@ template <> int svgd::attention_keys<SVGD_ATTENTION_TYPE>(AttnCall &c)
 {
     typedef SVGD_ATTENTION_TYPE T;
     AttnArgs &a = c.a;
-    const int rc = with_dim<T>(a.dim, [&](auto kd) {
+    const int rc = with_dim(a.dim, [&](auto kd) {
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
-            const bool two = kTwoKeys<T, KD, MOD> && small_blocks(a, a.s) >= kManyKeys;
+            constexpr bool kTwo = two_keys(sizeof(T), KD, MOD);
+            const bool two = kTwo && many_keys(a);
             set_grid(a, a.s, 16 * kAttnWaves * (two ? 2 : 1), key_splits(a));
             const int grid = a.per_die * 8;
-            if constexpr (kTwoKeys<T, KD, MOD>)
+            if constexpr (kTwo)
                 if (two) {
                     attention_keys_kernel<T, KD, 2, MOD>
                         <<<grid, kAttnBlock, 0, c.stream>>>(a, in<T>(c.q), in<T>(c.k), in<T>(c.v), in<T>(c.d_o), c.lse, c.delta, out<T>(c.dk), out<T>(c.dv), c.partial);

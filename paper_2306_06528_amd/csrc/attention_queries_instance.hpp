@@ -13,7 +13,7 @@ template <> int svgd::attention_queries<SVGD_ATTENTION_TYPE>(AttnCall &c)
             attention_delta_kernel<T><<<(unsigned)ceil_div(lines, 16), 256, 0, c.stream>>>(a, in<T>(c.o), in<T>(c.d_o), delta);
             return launched_ok();
         }
-    int rc = with_dim<T>(a.dim, [&](auto kd) {
+    int rc = with_dim(a.dim, [&](auto kd) {
         return with_truth(modified_scores(a), [&](auto mod) {
             constexpr int KD = decltype(kd)::value;
             constexpr bool MOD = decltype(mod)::value;
