@@ -187,7 +187,7 @@ template <class... Ps> __device__ __forceinline__ void next_head(HeadTurn &at, H
         ++at.t;
         ((ps.p += ps.carry), ...);
     }
-    while (at.t >= at.length) { // (mostly not once, kTokens times at most)
+    while (at.t >= at.length) { // (mostly not once; with a single head in sequences of one token as often as there are teams)
         at.t -= at.length;
         ((ps.p += ps.wrap), ...);
     }
