@@ -118,7 +118,9 @@ template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int 
 }
 
 // ROWS rows of up to 32 KD values in LDS, eight values at a time, brought by THREADS threads, neighbours in the workgroup; of fp32 values three planes of parts, made on the way.  Which place of its row such a piece
-// takes is permuted so that neither the same piece of 16 rows (`rows`) nor 32 bytes of eight rows in succession (`columns`, what 32 lanes read at a time) meet in a bank, of which there are 64.
+// takes is permuted so that what is read at a time meets in no bank, of which there are 64: 32 bytes of eight rows in succession (`columns`, by 32 lanes), and of `rows` not one piece of 16 rows but, since the lanes 0 .. 3,
+// 12 .. 15 and 20 .. 27 read 16 bytes each together and those between them, a piece of eight rows and the next one of the eight others (SQ_LDS_BANK_CONFLICT 0 for either and for the stores; as though
+// lanes 0 .. 15 read together, half the cycles of `rows`).
 // TINY: heads of less than eight values.
 template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
     typedef typename std::conditional<sizeof(T) == 4, bf16_t, T>::type elem; // in LDS
@@ -129,9 +131,9 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
     static __device__ __forceinline__ int place(int row, int chunk) // in eight values; moves with the row by 16
     {
         int f;
-        if constexpr (KD == 4) f = ((row & 7) << 1) | ((row >> 3) & 1);
-        else if constexpr (KD == 2) f = (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
-        else f = (((row >> 2) & 1) << 1) | ((row >> 3) & 1);
+        if constexpr (KD == 4) f = (row & 7) << 1;
+        else if constexpr (KD == 2) f = ((row >> 1) & 3) << 1;
+        else f = ((row >> 2) & 1) << 1;
         return row * kChunks + (chunk ^ f);
     }
     static __device__ __forceinline__ int row_of(int u) { return ((int)(threadIdx.x & (THREADS - 1)) + THREADS * u) / kChunks; }
