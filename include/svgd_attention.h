@@ -102,8 +102,8 @@ int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_
  * Query i is at position p = starts[b] + i (starts NULL: keys - length + i), key j at position j.  Query i sees key j where
  *     j < lengths[b] (NULL: keys), and not causal or j <= p or j < prefix[b] (NULL: 0), and documents[b, p] = documents[b, j] (NULL: all one)
  * A query whose position has no document (p < 0 or p >= keys) sees nothing if there are documents.  Where a query sees nothing o is 0 and lse -infinity, and
- * nothing flows back.  Keys and values from lengths[b] on are not read.  A non-finite key or value that some queries of a sequence see and others do not may make NaN of
- * all of that head's results.  starts beyond +-2^28 count as that.
+ * nothing flows back, whatever it and its d_o hold.  Keys and values from lengths[b] on are not read.  Those before it have to be finite, seen or not: a non-finite
+ * one may make NaN of all of that head's results.  starts beyond +-2^28 count as that.
  * slopes: `heads` values per particle.  lse (DEVICE, n x batch x heads x length floats): log of the sum of exp z, for the backward pass; may be NULL.  scratch (DEVICE,
  * 16-byte aligned): svgd_attention_forward_scratch bytes of this same struct, may be NULL if these are 0.
  * Of non-finite and of very small fp32 factors the same holds as of svgd_gated_ffn_*.

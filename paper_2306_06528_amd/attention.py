@@ -70,7 +70,8 @@ def attention_forward(q, k, v, causal: bool = False, cap: float = 0.0, slopes=No
 
     Key j is at position j, query i at starts[b] + i (None: the queries are the last tokens, keys - tokens + i).  All masks are int32 CUDA tensors: with `causal` a
     query sees no key behind its position, but the first prefix[b] in any case; lengths (batch,): how many keys there are (what lies behind is not read: a cache that was filled so
-    far); documents (batch, keys): a query sees only keys of its position's document.  A query that sees nothing has o = 0 and lse = -inf.
+    far; before that keys and values have to be finite, seen or not); documents (batch, keys): a query sees only keys of its position's document.  A query that sees nothing has o = 0 and lse = -inf,
+    and nothing flows back from it.
     lse, float32 (n, batch, heads, tokens), is for attention_backward.  One call serves training, prompts and single tokens over a cache."""
     return _call(_binding.attention_forward, stream, q, q, k, v, causal, cap, slopes, scale, starts, lengths, documents, prefix)
 

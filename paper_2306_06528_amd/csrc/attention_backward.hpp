@@ -41,11 +41,12 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
     if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
 }
 
-// (Heads of 33 to 64 values, fp16, capped, take 170 registers left to themselves, two more than leave room for three waves: 4 x 2 x 2,000 x 8 heads over 2 of 64, causal, 7 documents 116 us, so 97.)
-template <int KDX> constexpr int kWavesOfQueries = KDX == 2 ? 3 : kWavesPerSimd;
+// (Heads of 33 to 64 values, fp16, capped, take 169 and 170 registers left to themselves, one or two more than leave room for three waves: 4 x 2 x 2,000 x 8 heads over 2 of 64, causal, 7 documents, queries 116 us, so 95,
+// keys 124, so 114; fp32 would spill 47: keys of 3 x 2 x 333 x 6 heads over 2 of 40 29 us, so 23.)
+template <class T, int KDX, int B> constexpr int kWavesBackward = sizeof(T) == 2 && KDX == 2 && B == 1 ? 3 : kWavesPerSimd;
 
 template <class T, int KDX, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesOfQueries<KDX>))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesBackward<T, KDX, 1>))) void attention_queries_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
                                                                                                               Heads<const T> o, const float *lse, float *delta, Heads<T> dq, float *slope_rows, float *row_sums, float *partial)
 {
     constexpr int QB = 1; // blocks of 16 rows of a wave's own (attention_launch.hpp)
@@ -244,6 +245,15 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     for (int b = 0; b < QB; ++b) {
         const int r = own + 16 * b + (lane & 15);
         const int i = a.query(min(r, a.rows - 1)), h = at.head * a.group + min(r, a.rows - 1) - i * a.group;
+        if (log[b] == INFINITY) { // a row that sees nothing: 0, whatever it holds
+            sum_dz[b] = sum_dz_far[b] = sum_far[b] = 0.f;
+            less[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < 2 * KD; ++d) {
+                acc[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if constexpr (kRestore<T>) mean[d][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
         const int64_t line = a.line(at.particle, at.batch, h, i), lines = (int64_t)a.n * a.batch * a.heads * a.t;
         const float eps = kRestore<T> || MOD ? sum_over_rows(sum_dz[b]) : 0.f;
         if (r < a.rows && g == 0) {
@@ -296,7 +306,7 @@ struct __attribute__((aligned(16))) RowInfo {
 };
 
 template <class T, int KDX, int KB, bool MOD>
-__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesPerSimd))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
+__global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWavesBackward<T, KDX, KB>))) void attention_keys_kernel(AttnArgs a, Heads<const T> q, Heads<const T> k, Heads<const T> v, Heads<const T> d_o,
                                                                                                            const float *lse, const float *delta, Heads<T> dk, Heads<T> dv, float *partial)
 {
     constexpr int KD = kBlocks32<KDX>;
@@ -412,19 +422,27 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         if (threadIdx.x < kRows) {
             RowInfo &info = infos[half];
             info.log[threadIdx.x] = next_log;
-            info.less[threadIdx.x] = -next_delta;
+            info.less[threadIdx.x] = next_log == INFINITY ? 0.f : -next_delta; // (not where it is loaded, which would wait for it)
             info.slope[threadIdx.x] = next_slope;
             info.limit[threadIdx.x] = next_limit;
             info.position[threadIdx.x] = next_position;
             info.document[threadIdx.x] = next_document;
         }
     };
+    // Rows that see nothing are 0 in the products, whatever they hold.
+    const auto ready = [&](int half) {
+        __syncthreads();
+        if (!a.blind()) return;
+        TL::clear(lds + half * 2 * TL::kSize, infos[half].log);
+        TL::clear(lds + (half * 2 + 1) * TL::kSize, infos[half].log);
+        __syncthreads();
+    };
     if (begin < end) {
         fetch(begin);
         stage(0, begin);
     }
     loads_done();
-    __syncthreads();
+    ready(0);
     int half = 0;
     for (int n = begin; n < end; ++n) {
         if (n + 1 < end) fetch(n + 1);
@@ -540,7 +558,7 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
         if constexpr (kBuffers == 2) half ^= 1;
         else __syncthreads(); // (the tile has been read)
         if (n + 1 < end) stage(half, n + 1);
-        __syncthreads();
+        ready(half);
     }
     const float of_k = kHalf ? a.scale * 0x1p-14f / bs.scale : a.scale, of_v = kHalf ? 0x1p-14f : 1.f;
 #pragma unroll

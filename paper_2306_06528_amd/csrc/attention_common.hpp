@@ -35,6 +35,7 @@ struct AttnArgs {
     int tiles, splits; // tiles of a workgroup's own rows; parts of the streamed ones
     int per_die, total;           // workgroups
     __device__ __forceinline__ int query(int r) const { return group == 1 ? r : (int)__umulhi((uint32_t)r, group_mul); } // exact: r group < 2^32
+    __device__ __forceinline__ bool blind() const { return starts || lengths || t > s; } // there may be queries that see nothing
     __device__ __forceinline__ int64_t line(int i, int b, int h, int query) const { return ((int64_t)(i * batch + b) * heads + h) * t + query; }
 };
 
@@ -214,6 +215,20 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
             } else {
                 *to = v[u];
             }
+        }
+    }
+    // Rows whose log is infinite become 0 in LDS.  (The piece's number is hidden from the compiler, which would keep its places in registers all the time.)
+    static __device__ __forceinline__ void clear(elem *lds, const float *log)
+    {
+        int piece = threadIdx.x & (THREADS - 1);
+        asm volatile("" : "+v"(piece));
+#pragma unroll 1
+        for (; piece < ROWS * kChunks; piece += THREADS) {
+            const int row = piece / kChunks;
+            if (log[row] != INFINITY) continue;
+            Frag<elem> *const to = reinterpret_cast<Frag<elem> *>(lds) + place(row, piece - row * kChunks);
+#pragma unroll
+            for (int p = 0; p < kPlanes<T>; ++p) to[p * (kPlane / 8)] = Frag<elem>{};
         }
     }
     // operand of rows row .. row + 15, values col .. col + 31
