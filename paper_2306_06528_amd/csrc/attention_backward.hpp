@@ -1,6 +1,7 @@
 // Attention, backward, without atomics: one kernel has rows of its own and streams keys and values past them (dq, and the slopes' gradients row by row), the other has keys of its own and
 // streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse: five products and six of 16-bit activations for the forward pass's three.  4 x 2 x 4,096 x 16 heads of 64 bf16, causal:
-// 755 us (687 Gflop, 910 TFLOP/s) and 905 us (825 Gflop, 911 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197 x 6 heads of 64 bf16: 30.2 and 36.9, four tiles each.
+// 732 us (687 Gflop, 938 TFLOP/s) and 842 us (825 Gflop, 980 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197 x 6 heads of 64 bf16: 28.8 and 33.1, four tiles each.  (With P in one part and delta of o as it
+// is stored 621 and 763, 27.1 and 31.2.)
 //     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
 // P goes into the product with do, and dz into those with k and q, in two parts of the activations' type (BlockScale: fp16), and delta is made free of o's rounding (kRestore): dq, dk and dv are off by 1.00 times what
 // rounding them does, whether a row sees 3 keys or 4,096.  P in one part would make that 1.4 for dv, delta of o as it is stored 1.1 to 1.8 for dq and dk, the more the fewer keys count.

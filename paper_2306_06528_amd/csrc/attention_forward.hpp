@@ -1,14 +1,14 @@
 // Attention, forward.  A workgroup has 64 QB rows, a wave 16 QB of them; tiles of 64 keys and their values go through two halves of LDS, the next tile being on its way
 // from memory while one is worked on.  One pass with the running maximum and sum: sums are rescaled only where a maximum rises by more than 2^8.
-// 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 391 us, 703 TFLOP/s.  Exponentials, maxima and sums take as long as the products and run beside them only in part: a matrix instruction keeps the vector ALU of its SIMD for
-// some 40 % of its time.  8 x 8 x 197 x 6 heads of 64 bf16: 17.5 us, four tiles a workgroup.
+// 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 466 us, 885 TFLOP/s of the three products made (590 of the two of the formula).  Exponentials, maxima and sums take as long as the products and run beside them only in part: a matrix instruction keeps the vector ALU of its SIMD for
+// some 40 % of its time.  8 x 8 x 197 x 6 heads of 64 bf16: 20 us, four tiles a workgroup.
 #pragma once
 #include "attention_common.hpp"
 
 namespace svgd {
 
 // Probabilities, relative to the running maximum, go into their product with the values in two parts of the activations' type (as_parts): in one, half a step off each, with signs as random as those of o's own rounding,
-// they would put o off by 1.1 to 1.4 times what rounding it does.  The third product takes 4 x 2 x 4,096 x 16 heads of 64 bf16, causal, from 391 to 491 us, a cache's tokens nothing.  fp16 ones are held 2^6 times as large,
+// they would put o off by 1.1 to 1.4 times what rounding it does.  The third product takes 4 x 2 x 4,096 x 16 heads of 64 bf16, causal, from 360 to 466 us, a cache's tokens nothing.  fp16 ones are held 2^6 times as large,
 // so that those down to 2^-20 keep their digits.
 template <class T> constexpr float kProbExponent = 0.f;
 template <> inline constexpr float kProbExponent<f16_t> = 6.f;
