@@ -2,13 +2,13 @@
  * svgd_attention.h - C ABI of the attention half of the particles' layers: linear maps with bias, activation and residual, norms of
  * queries and keys with the rotation by their positions, and attention, forward and backward, for all n networks of an ensemble at once.
  *
- * With the calls of svgd_layers.h these make whole transformer blocks of n networks: s = s + linear(attention(rotary(linear(layer_norm(s))))),
- * then the gated feed-forward half.
+ * With the calls of svgd_layers.h these make whole transformer blocks of n networks: s = s +
+ * linear(attention(rotary(linear(layer_norm(s))))), then the gated feed-forward half.
  *
- * Conventions: those of svgd_layers.h (activations of one svgd_dtype, parameters fp32 in the rows of X, their gradients in G, sums, products
- * and softmax statistics in fp32 or more - 16-bit attention's probabilities and gradients of scores, once they are operands of a product, in two
- * parts of the activations' type, 2^-17 of bf16 ones and 2^-22 of fp16 ones -, `accumulate`, `stream`, status, no synchronisation or allocation, the same inputs give the same
- * bits), and for activations with heads
+ * Conventions: those of svgd_layers.h (activations of one svgd_dtype, parameters fp32 in the rows of X, their gradients in G, sums,
+ * products and softmax statistics in fp32 or more - 16-bit attention's probabilities and gradients of scores, once they are operands of a
+ * product, in two parts of the activations' type, 2^-17 of bf16 ones and 2^-22 of fp16 ones -, `accumulate`, `stream`, status, no
+ * synchronisation or allocation, the same inputs give the same bits), and for activations with heads
  *   - n particles x `batch` sequences x `length` tokens x `heads` heads x `dim` values, described by svgd_heads: value c of head h of
  *     token t of sequence b of particle i is element i * particle_stride + b * batch_stride + t * token_stride + h * head_stride + c of
  *     `data`.  Inputs may have any strides from 0 on, a view into the results of one linear map among them; outputs' heads must not
@@ -70,9 +70,9 @@ int svgd_linear_backward(int dtype, int activation, int n, int64_t rows, int64_t
  * Norms of queries and keys, head by head, and the rotation by position, in one pass:
  *     y_c = x_c weight_c / sqrt(avg_c x_c^2 + eps),  pairs j of the first 2 `pairs` values of y turned by the angle position frequency_j
  * Pair j is the values j and j + pairs (interleaved = 0) or 2 j and 2 j + 1.  weights: `dim` values per particle, of queries and of keys;
- * either both or neither is NULL: no norm then.  frequencies (DEVICE, `pairs` doubles) and positions (DEVICE, int64 each; sequence b's token t
- * has positions[b * positions_stride + t], a stride of 0: all sequences the same) may be NULL if pairs is 0.  Angles are formed and reduced in
- * 64 bits.  heads or kv_heads may be 0 (q or k is not there).
+ * either both or neither is NULL: no norm then.  frequencies (DEVICE, `pairs` doubles) and positions (DEVICE, int64 each; sequence b's
+ * token t has positions[b * positions_stride + t], a stride of 0: all sequences the same) may be NULL if pairs is 0.  Angles are formed and
+ * reduced in 64 bits.  heads or kv_heads may be 0 (q or k is not there).
  */
 typedef struct svgd_rotary {
     int n, heads, kv_heads, dim, pairs, interleaved;
@@ -87,9 +87,11 @@ typedef struct svgd_rotary {
 int svgd_qk_norm_rotary_forward(int dtype, const svgd_rotary *p, svgd_heads q, svgd_heads k, svgd_heads q_out, svgd_heads k_out, void *stream);
 
 /*
- * Its backward pass, from q and k as the forward call got them (without a norm they are not read and may be NULL): with g = dy turned back, xhat = x rstd and a = g weight,
+ * Its backward pass, from q and k as the forward call got them (without a norm they are not read and may be NULL): with g = dy turned back,
+ * xhat = x rstd and a = g weight,
  *     dx = rstd (a - xhat avg_c(a xhat)),  dweight = sum over sequences, tokens and heads of g xhat
- * dweights may be NULL, each for itself.  scratch (DEVICE, 16-byte aligned): svgd_qk_norm_rotary_scratch bytes; may be NULL if no dweight is wanted.
+ * dweights may be NULL, each for itself.  scratch (DEVICE, 16-byte aligned): svgd_qk_norm_rotary_scratch bytes; may be NULL if no dweight
+ * is wanted.
  */
 size_t svgd_qk_norm_rotary_scratch(const svgd_rotary *p);
 int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_out, svgd_heads dk_out, svgd_heads q, svgd_heads k, svgd_heads dq,
@@ -101,11 +103,11 @@ int svgd_qk_norm_rotary_backward(int dtype, const svgd_rotary *p, svgd_heads dq_
  *     z = scale q k;  z = cap tanh(z / cap) if cap > 0;  z -= slope |p - j| if slopes;  P = softmax of z over the keys that are seen;  o = P v
  * Query i is at position p = starts[b] + i (starts NULL: keys - length + i), key j at position j.  Query i sees key j where
  *     j < lengths[b] (NULL: keys), and not causal or j <= p or j < prefix[b] (NULL: 0), and documents[b, p] = documents[b, j] (NULL: all one)
- * A query whose position has no document (p < 0 or p >= keys) sees nothing if there are documents.  Where a query sees nothing o is 0 and lse -infinity, and
- * nothing flows back, whatever it and its d_o hold.  Keys and values from lengths[b] on are not read.  Those before it have to be finite, seen or not: a non-finite
- * one may make NaN of all of that head's results.  starts beyond +-2^28 count as that.
- * slopes: `heads` values per particle.  lse (DEVICE, n x batch x heads x length floats): log of the sum of exp z, for the backward pass; may be NULL.  scratch (DEVICE,
- * 16-byte aligned): svgd_attention_forward_scratch bytes of this same struct, may be NULL if these are 0.
+ * A query whose position has no document (p < 0 or p >= keys) sees nothing if there are documents.  Where a query sees nothing o is 0 and
+ * lse -infinity, and nothing flows back, whatever it and its d_o hold.  Keys and values from lengths[b] on are not read.  Those before it
+ * have to be finite, seen or not: a non-finite one may make NaN of all of that head's results.  starts beyond +-2^28 count as that.
+ * slopes: `heads` values per particle.  lse (DEVICE, n x batch x heads x length floats): log of the sum of exp z, for the backward pass;
+ * may be NULL.  scratch (DEVICE, 16-byte aligned): svgd_attention_forward_scratch bytes of this same struct, may be NULL if these are 0.
  * Of non-finite and of very small fp32 factors the same holds as of svgd_gated_ffn_*.
  */
 typedef struct svgd_attention {
@@ -124,8 +126,8 @@ int svgd_attention_forward(int dtype, const svgd_attention *a, svgd_heads q, svg
 /*
  * Its backward pass, o and lse being the forward call's: with dP = do v and dz = P (dP - sum_c do_c o_c),
  *     dslope = -sum dz |p - j|,  dz *= 1 - tanh^2,  dq = scale dz k,  dk = scale sum dz q,  dv = sum P do
- * dslopes (`heads` values per particle) may be NULL; with `accumulate` it is added to.  Gradients of keys that no query sees are 0.  scratch (DEVICE, 16-byte aligned):
- * svgd_attention_scratch bytes.
+ * dslopes (`heads` values per particle) may be NULL; with `accumulate` it is added to.  Gradients of keys that no query sees are 0.
+ * scratch (DEVICE, 16-byte aligned): svgd_attention_scratch bytes.
  */
 size_t svgd_attention_scratch(const svgd_attention *a);
 int svgd_attention_backward(int dtype, const svgd_attention *a, svgd_heads d_o, svgd_heads q, svgd_heads k, svgd_heads v, svgd_heads o, const float *lse,

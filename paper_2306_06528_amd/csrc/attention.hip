@@ -100,8 +100,8 @@ template <class F> int for_type(int dtype, F f) { return dtype == SVGD_F32 ? f(f
 
 size_t rounded(size_t floats) { return (floats + 3) / 4 * 4; }
 
-// Scratch memory of the backward pass, in floats: delta, the slopes' rows, where queries' rows are in parts these parts' sums of dz (and with slopes two more), parts' sums of dq (and of the keys' means, which 16 bits
-// need) or of dk and dv, which come after them.
+// Scratch memory of the backward pass, in floats: delta, the slopes' rows, where queries' rows are in parts these parts' sums of dz (and
+// with slopes two more), parts' sums of dq (and of the keys' means, which 16 bits need) or of dk and dv, which come after them.
 struct BackwardScratch {
     size_t slopes, sums, partial, total;
     explicit BackwardScratch(const svgd_attention &p)

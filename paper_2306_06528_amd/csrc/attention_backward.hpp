@@ -1,20 +1,22 @@
-// Attention, backward, without atomics: one kernel has rows of its own and streams keys and values past them (dq, and the slopes' gradients row by row), the other has keys of its own and
-// streams rows past them (dk and dv, summed over the heads that share them).  Both make the probabilities again from lse: five products and six of 16-bit activations for the forward pass's three.  4 x 2 x 4,096 x 16 heads of 64 bf16, causal:
-// 732 us (687 Gflop, 938 TFLOP/s) and 842 us (825 Gflop, 980 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197 x 6 heads of 64 bf16: 28.8 and 33.1, four tiles each.  (With P in one part and delta of o as it
-// is stored 621 and 763, 27.1 and 31.2.)
+// Attention, backward, without atomics: one kernel has rows of its own and streams keys and values past them (dq, and the slopes' gradients
+// row by row), the other has keys of its own and streams rows past them (dk and dv, summed over the heads that share them).  Both make the
+// probabilities again from lse: five products and six of 16-bit activations for the forward pass's three.  4 x 2 x 4,096 x 16 heads of 64
+// bf16, causal: 732 us (687 Gflop, 938 TFLOP/s) and 842 us (825 Gflop, 980 TFLOP/s), matrix cores and vector ALU taking turns; 8 x 8 x 197
+// x 6 heads of 64 bf16: 28.8 and 33.1, four tiles each.  (With P in one part and delta of o as it is stored 621 and 763, 27.1 and 31.2.)
 //     P = exp(z - lse),  dP = do v,  dz = P (dP - delta),  delta = sum_c do_c o_c
-// P goes into the product with do, and dz into those with k and q, in two parts of the activations' type (BlockScale: fp16), and delta is made free of o's rounding (kRestore): dq, dk and dv are off by 1.00 times what
-// rounding them does, whether a row sees 3 keys or 4,096.  P in one part would make that 1.4 for dv, delta of o as it is stored 1.1 to 1.8 for dq and dk, the more the fewer keys count.
+// P goes into the product with do, and dz into those with k and q, in two parts of the activations' type (BlockScale: fp16), and delta is
+// made free of o's rounding (kRestore): dq, dk and dv are off by 1.00 times what rounding them does, whether a row sees 3 keys or 4,096.  P
+// in one part would make that 1.4 for dv, delta of o as it is stored 1.1 to 1.8 for dq and dk, the more the fewer keys count.
 #pragma once
 #include "attention_common.hpp"
 
 namespace svgd {
 
-// o as it was stored leaves delta off by its roundings: by eps, which of rows that see few keys, or few that count, is not small beside dz and does not cancel.  The sum of a row's dz is 0, so made with the delta at hand it
-// is eps, and
+// o as it was stored leaves delta off by its roundings: by eps, which of rows that see few keys, or few that count, is not small beside dz
+// and does not cancel.  The sum of a row's dz is 0, so made with the delta at hand it is eps, and
 //     dz = dz0 - eps P,   dq = scale (sum dz0 damp k - eps sum P damp k)
-// The kernel that has queries of its own adds up the two sums beside dq's (a fifth product; P in one part does, eps being 2^-9 of delta), and leaves delta + eps for the kernel that has keys of its own.  Not for fp32, whose o
-// is rounded as every sum is.
+// The kernel that has queries of its own adds up the two sums beside dq's (a fifth product; P in one part does, eps being 2^-9 of delta),
+// and leaves delta + eps for the kernel that has keys of its own.  Not for fp32, whose o is rounded as every sum is.
 template <class T> constexpr bool kRestore = sizeof(T) == 2;
 
 // One of two forms of a loop, the same for the whole wave.
@@ -42,8 +44,9 @@ template <class T> __global__ __launch_bounds__(256) void attention_delta_kernel
     if ((threadIdx.x & 15) == 0) delta[a.line(particle, b, h, i)] = sum;
 }
 
-// (Heads of 33 to 64 values, fp16, capped, take 169 and 170 registers left to themselves, one or two more than leave room for three waves: 4 x 2 x 2,000 x 8 heads over 2 of 64, causal, 7 documents, queries 116 us, so 95,
-// keys 124, so 114; fp32 would spill 47: keys of 3 x 2 x 333 x 6 heads over 2 of 40 29 us, so 23.)
+// (Heads of 33 to 64 values, fp16, capped, take 169 and 170 registers left to themselves, one or two more than leave room for three waves:
+// 4 x 2 x 2,000 x 8 heads over 2 of 64, causal, 7 documents, queries 116 us, so 95, keys 124, so 114; fp32 would spill 47: keys of 3 x 2 x
+// 333 x 6 heads over 2 of 40 29 us, so 23.)
 template <class T, int KDX, int B> constexpr int kWavesBackward = sizeof(T) == 2 && KDX == 2 && B == 1 ? 3 : kWavesPerSimd;
 
 template <class T, int KDX, bool MOD>
@@ -313,8 +316,9 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     constexpr int KD = kBlocks32<KDX>;
     typedef Streamed<T, KD, KDX == 0> TL;
     constexpr int kRows = TL::kRows, kBuffers = kHalves<T, KD>;
-    // Two waves to a SIMD hide little of what a wave waits for: operands are asked for well before their products, where the compiler, short of registers, asks for a few at a time and waits for each (4 x 2 x 4,096
-    // x 16 heads of 64 bf16 causal 915 us, so 875; with one block of keys, three waves, the registers are worth more: 8 x 8 x 197 x 6 heads of 64 35 us, so 43).
+    // Two waves to a SIMD hide little of what a wave waits for: operands are asked for well before their products, where the compiler,
+    // short of registers, asks for a few at a time and waits for each (4 x 2 x 4,096 x 16 heads of 64 bf16 causal 915 us, so 875; with one
+    // block of keys, three waves, the registers are worth more: 8 x 8 x 197 x 6 heads of 64 35 us, so 43).
     constexpr bool kDeep = sizeof(T) == 2 && (KB == 2 || KD > 2);
     constexpr int kEarly = kDeep ? (KD <= 2 ? 2 * KD : 4) : 0; // transposed operands that are asked for before the exponentials
     constexpr bool kHalf = std::is_same<T, f16_t>::value;
@@ -587,7 +591,8 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     }
 }
 
-// dq from the parts' sums, in order, and what eps puts on delta: a thread has four values of a line's ld (dq null, not wanted: delta alone, a thread a line).
+// dq from the parts' sums, in order, and what eps puts on delta: a thread has four values of a line's ld (dq null, not wanted: delta alone,
+// a thread a line).
 template <class T> __global__ __launch_bounds__(256) void attention_query_sums_kernel(AttnArgs a, int ld, const float *partial, const float *row_sums, float *delta, Heads<T> dq)
 {
     const int64_t lines = (int64_t)a.n * a.batch * a.heads * a.t;

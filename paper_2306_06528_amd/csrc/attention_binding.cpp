@@ -289,7 +289,8 @@ PyObject *qk_norm_rotary_forward(PyObject *, PyObject *const *a, Py_ssize_t na)
     });
 }
 
-// qk_norm_rotary_backward(current_device, stream_of, dq_out, dk_out, q, k, q_weight, k_weight, frequencies, positions, layout, eps, dq_weight, dk_weight, accumulate) -> (dq, dk)
+// qk_norm_rotary_backward(current_device, stream_of, dq_out, dk_out, q, k, q_weight, k_weight, frequencies, positions, layout, eps,
+// dq_weight, dk_weight, accumulate) -> (dq, dk)
 PyObject *qk_norm_rotary_backward(PyObject *, PyObject *const *a, Py_ssize_t na)
 {
     return guarded(na, 15, [&]() -> PyObject * {
@@ -337,7 +338,8 @@ PyObject *attention_forward(PyObject *, PyObject *const *a, Py_ssize_t na)
     });
 }
 
-// attention_backward(current_device, stream_of, do, q, k, v, o, lse, causal, cap, slopes, scale, starts, lengths, documents, prefix, dslopes, accumulate, want_dq, want_dkv) -> (dq, dk, dv)
+// attention_backward(current_device, stream_of, do, q, k, v, o, lse, causal, cap, slopes, scale, starts, lengths, documents, prefix,
+// dslopes, accumulate, want_dq, want_dkv) -> (dq, dk, dv)
 PyObject *attention_backward(PyObject *, PyObject *const *a, Py_ssize_t na)
 {
     return guarded(na, 20, [&]() -> PyObject * {

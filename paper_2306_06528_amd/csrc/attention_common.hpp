@@ -1,9 +1,10 @@
 // What the attention kernels share: arguments, tiles of keys or rows in LDS, operands of the matrix instructions, masks.
 //
-// Queries of the heads that share a key head are one list of rows: row r is query r / group of head r % group of those.  A wave holds rows (or keys) of its own as the
-// B operand of the matrix instructions, 16 to a block, and streams the others past them as A: the results then have a row of the wave's own per lane (lane % 16), and of the streamed
-// ones 4 (lane / 16) + 0 .. 3 of every 16.  Softmax statistics are one register per lane, and probabilities are, as they come, the B operand of the next product: two blocks of 16
-// make a step of 32 whose k are ordered as k_of says, in A as in B.
+// Queries of the heads that share a key head are one list of rows: row r is query r / group of head r % group of those.  A wave holds rows
+// (or keys) of its own as the B operand of the matrix instructions, 16 to a block, and streams the others past them as A: the results then
+// have a row of the wave's own per lane (lane % 16), and of the streamed ones 4 (lane / 16) + 0 .. 3 of every 16.  Softmax statistics are
+// one register per lane, and probabilities are, as they come, the B operand of the next product: two blocks of 16 make a step of 32 whose k
+// are ordered as k_of says, in A as in B.
 #pragma once
 #include "../../include/svgd_attention.h"
 #include "attention_rules.hpp"
@@ -39,10 +40,12 @@ struct AttnArgs {
     __device__ __forceinline__ int64_t line(int i, int b, int h, int query) const { return ((int64_t)(i * batch + b) * heads + h) * t + query; }
 };
 
-// Which particle, sequence, key head, tile and part a workgroup has.  Workgroups go round the eight dies in turn; a die gets ones that follow one another.  Four heads, whose keys meet in its L2, take turns
-// tile by tile, so that of causal ones the longest of four heads come first and the shortest last: head after head the last head's longest would be left over at the end.  Where a die has less than four heads
-// of its own, all heads take turns: otherwise one die would get a head's long tiles and another its short ones (4 x 2 x 2,000 x 8 heads over 2 of 64 fp16, causal, with documents: forward 89 us, so 68, both with two blocks to
-// a wave; 2 x 2,048 x 8 heads of 64 bf16, causal, queries in two parts 38.5, so 32.4).
+// Which particle, sequence, key head, tile and part a workgroup has.  Workgroups go round the eight dies in turn; a die gets ones that
+// follow one another.  Four heads, whose keys meet in its L2, take turns tile by tile, so that of causal ones the longest of four heads
+// come first and the shortest last: head after head the last head's longest would be left over at the end.  Where a die has less than four
+// heads of its own, all heads take turns: otherwise one die would get a head's long tiles and another its short ones (4 x 2 x 2,000 x 8
+// heads over 2 of 64 fp16, causal, with documents: forward 89 us, so 68, both with two blocks to a wave; 2 x 2,048 x 8 heads of 64 bf16,
+// causal, queries in two parts 38.5, so 32.4).
 struct AttnBlock {
     static constexpr int kHeads = 4;
     int particle, batch, head, tile, part;
@@ -69,8 +72,9 @@ struct AttnBlock {
 // ---------------------------------------------------------------------------------------------
 // operands
 // ---------------------------------------------------------------------------------------------
-// Eight values of k of one row, lane l: row l % 16, group l / 16 of k.  16-bit values are as they are; fp32 ones three bf16 parts whose sum is the value exactly (split3): the products of parts that are not below 2^-24 of the
-// whole, six, take 96 cycles of a matrix core for 32 values of k, where the fp32 matrix instructions take 256.
+// Eight values of k of one row, lane l: row l % 16, group l / 16 of k.  16-bit values are as they are; fp32 ones three bf16 parts whose sum
+// is the value exactly (split3): the products of parts that are not below 2^-24 of the whole, six, take 96 cycles of a matrix core for 32
+// values of k, where the fp32 matrix instructions take 256.
 template <class T> struct FragOf {
     typedef T type __attribute__((ext_vector_type(8)));
 };
@@ -118,11 +122,12 @@ template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *p, int 
     else return v;
 }
 
-// ROWS rows of up to 32 KD values in LDS, eight values at a time, brought by THREADS threads, neighbours in the workgroup; of fp32 values three planes of parts, made on the way.  Which place of its row such a piece
-// takes is permuted so that what is read at a time meets in no bank, of which there are 64: 32 bytes of eight rows in succession (`columns`, by 32 lanes), and of `rows` not one piece of 16 rows but, since the lanes 0 .. 3,
-// 12 .. 15 and 20 .. 27 read 16 bytes each together and those between them, a piece of eight rows and the next one of the eight others (SQ_LDS_BANK_CONFLICT 0 for either and for the stores; as though
-// lanes 0 .. 15 read together, half the cycles of `rows`).
-// TINY: heads of less than eight values.
+// ROWS rows of up to 32 KD values in LDS, eight values at a time, brought by THREADS threads, neighbours in the workgroup; of fp32 values
+// three planes of parts, made on the way.  Which place of its row such a piece takes is permuted so that what is read at a time meets in no
+// bank, of which there are 64: 32 bytes of eight rows in succession (`columns`, by 32 lanes), and of `rows` not one piece of 16 rows but,
+// since the lanes 0 .. 3, 12 .. 15 and 20 .. 27 read 16 bytes each together and those between them, a piece of eight rows and the next one
+// of the eight others (SQ_LDS_BANK_CONFLICT 0 for either and for the stores; as though lanes 0 .. 15 read together, half the cycles of
+// `rows`).  TINY: heads of less than eight values.
 template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
     typedef typename std::conditional<sizeof(T) == 4, bf16_t, T>::type elem; // in LDS
     static constexpr int VEC = 8, kRows = ROWS, kChunks = 32 * KD / VEC, kPlane = ROWS * 32 * KD, kSize = kPlanes<T> * kPlane, N = ROWS * kChunks / THREADS;
@@ -139,8 +144,8 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
     }
     static __device__ __forceinline__ int row_of(int u) { return ((int)(threadIdx.x & (THREADS - 1)) + THREADS * u) / kChunks; }
     static __device__ __forceinline__ int chunk_of(int u) { return ((int)(threadIdx.x & (THREADS - 1)) + THREADS * u) % kChunks; }
-    // Where the thread's pieces lie, in bytes from the tile's first row; row(i): where row i starts, in elements.  A piece that ends beyond the head is loaded further left (and moved to its place by
-    // `store`).
+    // Where the thread's pieces lie, in bytes from the tile's first row; row(i): where row i starts, in elements.  A piece that ends beyond
+    // the head is loaded further left (and moved to its place by `store`).
     static __device__ __forceinline__ uint32_t column(int u, int dim)
     {
         const int c = chunk_of(u) * VEC;
@@ -174,7 +179,8 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) v[u][e] = p[c + e < dim ? c + e : dim - 1];
             } else {
-                // (a wave's own tiles are read once: 8 x 4 sequences of 4,096 to 8,192 keys, 4 heads of 128 bf16 80 us, so as what others read too 92)
+                // (a wave's own tiles are read once: 8 x 4 sequences of 4,096 to 8,192 keys, 4 heads of 128 bf16 80 us, so as what others
+                // read too 92)
                 if constexpr (THREADS == 64) v[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Pack<T, VEC>::type *>(from + at[u]));
                 else v[u] = *reinterpret_cast<const typename Pack<T, VEC>::type *>(from + at[u]);
             }
@@ -217,7 +223,8 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
             }
         }
     }
-    // Rows whose log is infinite become 0 in LDS.  (The piece's number is hidden from the compiler, which would keep its places in registers all the time.)
+    // Rows whose log is infinite become 0 in LDS.  (The piece's number is hidden from the compiler, which would keep its places in
+    // registers all the time.)
     static __device__ __forceinline__ void clear(elem *lds, const float *log)
     {
         int piece = threadIdx.x & (THREADS - 1);
@@ -259,13 +266,14 @@ template <class T, int KD, bool TINY, int ROWS, int THREADS> struct Tile {
     }
 };
 
-// Streamed tiles of a workgroup: 64 rows, in two halves of LDS, of which one is worked on while the other is filled.  fp32 ones take half as much more than the values: 32 rows, or one half alone, so that two or three
-// workgroups fit a CU.
+// Streamed tiles of a workgroup: 64 rows, in two halves of LDS, of which one is worked on while the other is filled.  fp32 ones take half
+// as much more than the values: 32 rows, or one half alone, so that two or three workgroups fit a CU.
 template <class T, int KD> constexpr int kStreamed = sizeof(T) == 4 && KD % 2 == 0 ? 32 : kTileRows;
 template <class T, int KD> constexpr int kHalves = sizeof(T) == 4 && KD > 2 ? 1 : 2;
 template <class T, int KD, bool TINY> using Streamed = Tile<T, KD, TINY, kStreamed<T, KD>, kAttnBlock>;
 
-// Waits for the loads so far.  Before the loop over tiles: the compiler, which cannot tell an operand loaded before it from a tile loaded in it, would wait for the next tile with every tile.
+// Waits for the loads so far.  Before the loop over tiles: the compiler, which cannot tell an operand loaded before it from a tile loaded
+// in it, would wait for the next tile with every tile.
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 // The part's share of the tiles begin .. end - 1.
@@ -276,7 +284,8 @@ __device__ __forceinline__ void part_of(const AttnArgs &a, int part, int &begin,
     end = first + (int)((int64_t)count * (part + 1) / a.splits);
 }
 
-// What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
+// What the kernels are built for; told so, the compiler keeps products out of the accumulation registers, which cost a move for every value
+// (forward, 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 604 us, so 468).
 constexpr int kWavesPerSimd = 2;
 
 // Two results of 16 streamed rows each as a B operand.
@@ -295,8 +304,8 @@ template <class T> __device__ __forceinline__ Frag<T> as_operand(f32x4 a, f32x4 
     }
 }
 
-// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it, which is little beside the 2^-9 or 2^-12 that an output's own rounding takes: how probabilities and the gradients of scores
-// become operands.  fp32 is one operand.
+// The same in two parts whose sum is the value but for 2^-17 (bf16) or 2^-22 (fp16) of it, which is little beside the 2^-9 or 2^-12 that an
+// output's own rounding takes: how probabilities and the gradients of scores become operands.  fp32 is one operand.
 template <class T> constexpr int kOperands = 2;
 template <> inline constexpr int kOperands<float> = 1;
 template <class T> __device__ __forceinline__ void as_parts(f32x4 a, f32x4 b, const SplitConst &sc, Frag<T> (&out)[kOperands<T>])
@@ -343,8 +352,9 @@ __device__ __forceinline__ float row_max(float v)
     return __builtin_elementwise_maximum(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false)));
 }
 
-// tanh, for 16-bit activations: up to 1/2 x times a polynomial in x^2 (through its values at the nodes of Chebyshev; off by 1.4e-8, rounded by 1.2e-7 of itself), beyond from one exponential, off by 2^-23 or so of 1, which
-// of a small one would be too much: the cap times that is the error of an exponent.  For fp32 the library's.
+// tanh, for 16-bit activations: up to 1/2 x times a polynomial in x^2 (through its values at the nodes of Chebyshev; off by 1.4e-8, rounded
+// by 1.2e-7 of itself), beyond from one exponential, off by 2^-23 or so of 1, which of a small one would be too much: the cap times that is
+// the error of an exponent.  For fp32 the library's.
 constexpr float kTanhSmall = 0.5f;
 __device__ __forceinline__ float tanh_small(float x)
 {
@@ -357,8 +367,8 @@ __device__ __forceinline__ float tanh_any(float x)
     return fabsf(x) <= kTanhSmall ? tanh_small(x) : large;
 }
 
-// Scores that are capped, or less a slope times the distance: z = out t - slope distance in exponents of 2, where t = tanh(scale s / cap) and out = cap, or t = scale s and out = 1; d z / d (scale s) is
-// 1 - on t^2, on = 1 or 0.
+// Scores that are capped, or less a slope times the distance: z = out t - slope distance in exponents of 2, where t = tanh(scale s / cap)
+// and out = cap, or t = scale s and out = 1; d z / d (scale s) is 1 - on t^2, on = 1 or 0.
 struct Modified {
     float in, out, on;
     __device__ __forceinline__ Modified(const AttnArgs &a) : in(a.cap > 0.f ? a.scale / a.cap : a.scale), out((a.cap > 0.f ? a.cap : 1.f) * kLog2e), on(a.cap > 0.f ? 1.f : 0.f) {}
@@ -422,7 +432,8 @@ struct Masks {
     __device__ __forceinline__ int document(const AttnArgs &a, int p) const { return documents && p >= 0 && p < a.s ? documents[p] : 0; }
 };
 
-// Narrows the streamed places [lo, hi) to those from the first to the last that may share a document with one of the places [first, last]: all threads of the workgroup call it.
+// Narrows the streamed places [lo, hi) to those from the first to the last that may share a document with one of the places [first, last]:
+// all threads of the workgroup call it.
 __device__ __forceinline__ void narrow(const int32_t *documents, int first, int last, int size, int *red, int &lo, int &hi)
 {
     first = max(first, 0);
@@ -455,7 +466,8 @@ __device__ __forceinline__ void narrow(const int32_t *documents, int first, int 
     if (lo == INT32_MAX) lo = hi = 0;
 }
 
-// fp16 operands made of sums' terms (dz): scaled by a power of two that keeps the largest so far below 2^15, by wave.  Without it gradients below 6e-5 would lose their digits and those beyond 65,504 be infinite.
+// fp16 operands made of sums' terms (dz): scaled by a power of two that keeps the largest so far below 2^15, by wave.  Without it gradients
+// below 6e-5 would lose their digits and those beyond 65,504 be infinite.
 struct BlockScale {
     float scale = 0x1p100f;
     // the factor by which what was summed up so far has to be multiplied (mostly 1), given the lane's largest new magnitude

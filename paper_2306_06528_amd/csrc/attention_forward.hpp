@@ -1,19 +1,22 @@
-// Attention, forward.  A workgroup has 64 QB rows, a wave 16 QB of them; tiles of 64 keys and their values go through two halves of LDS, the next tile being on its way
-// from memory while one is worked on.  One pass with the running maximum and sum: sums are rescaled only where a maximum rises by more than 2^8.
-// 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 466 us, 885 TFLOP/s of the three products made (590 of the two of the formula).  Exponentials, maxima and sums take as long as the products and run beside them only in part: a matrix instruction keeps the vector ALU of its SIMD for
-// some 40 % of its time.  8 x 8 x 197 x 6 heads of 64 bf16: 20 us, four tiles a workgroup.
+// Attention, forward.  A workgroup has 64 QB rows, a wave 16 QB of them; tiles of 64 keys and their values go through two halves of LDS,
+// the next tile being on its way from memory while one is worked on.  One pass with the running maximum and sum: sums are rescaled only
+// where a maximum rises by more than 2^8. 4 x 2 x 4,096 x 16 heads of 64 bf16, causal: 466 us, 885 TFLOP/s of the three products made (590
+// of the two of the formula).  Exponentials, maxima and sums take as long as the products and run beside them only in part: a matrix
+// instruction keeps the vector ALU of its SIMD for some 40 % of its time.  8 x 8 x 197 x 6 heads of 64 bf16: 20 us, four tiles a workgroup.
 #pragma once
 #include "attention_common.hpp"
 
 namespace svgd {
 
-// Probabilities, relative to the running maximum, go into their product with the values in two parts of the activations' type (as_parts): in one, half a step off each, with signs as random as those of o's own rounding,
-// they would put o off by 1.1 to 1.4 times what rounding it does.  The third product takes 4 x 2 x 4,096 x 16 heads of 64 bf16, causal, from 360 to 466 us, a cache's tokens nothing.  fp16 ones are held 2^6 times as large,
-// so that those down to 2^-20 keep their digits.
+// Probabilities, relative to the running maximum, go into their product with the values in two parts of the activations' type (as_parts):
+// in one, half a step off each, with signs as random as those of o's own rounding, they would put o off by 1.1 to 1.4 times what rounding
+// it does.  The third product takes 4 x 2 x 4,096 x 16 heads of 64 bf16, causal, from 360 to 466 us, a cache's tokens nothing.  fp16 ones
+// are held 2^6 times as large, so that those down to 2^-20 keep their digits.
 template <class T> constexpr float kProbExponent = 0.f;
 template <> inline constexpr float kProbExponent<f16_t> = 6.f;
 
-// Running maxima and sums of a wave's rows, and their sums of values, of which value 16 d + 4 (lane / 16) + e of row lane % 16 is acc[d][b][e].
+// Running maxima and sums of a wave's rows, and their sums of values, of which value 16 d + 4 (lane / 16) + e of row lane % 16 is
+// acc[d][b][e].
 template <class T, int KD, int QB> struct Running {
     f32x4 acc[2 * KD][QB];
     float top[QB], total[QB]; // total: of the lane's keys
@@ -222,8 +225,9 @@ __global__ __launch_bounds__(kAttnBlock) __attribute__((amdgpu_waves_per_eu(kWav
     }
 }
 
-// Up to 16 rows: single tokens, or a few, over a cache.  All four waves have the same rows; each takes every fourth tile of 32 keys through a part of LDS of its own, so that none waits for another before the
-// end, when their sums are joined.  Reading keys and values once bounds it: 8 x 4 x 1 over up to 8,192 x 4 heads of 128 bf16, 486 MB, 79 us, 6.1 TB/s, and the join of 8 parts 4.6; 16 x 1 over 200 x 4 heads of
+// Up to 16 rows: single tokens, or a few, over a cache.  All four waves have the same rows; each takes every fourth tile of 32 keys through
+// a part of LDS of its own, so that none waits for another before the end, when their sums are joined.  Reading keys and values once bounds
+// it: 8 x 4 x 1 over up to 8,192 x 4 heads of 128 bf16, 486 MB, 79 us, 6.1 TB/s, and the join of 8 parts 4.6; 16 x 1 over 200 x 4 heads of
 // 64 fp32 10 us, the chain of one load, two products and the join, twice.
 constexpr int kFewKeys = 32;
 template <class T, int KDX, bool MOD>

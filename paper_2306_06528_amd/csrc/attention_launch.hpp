@@ -1,4 +1,5 @@
-// What a call of attention launches, by sizes alone (attention_rules.hpp).  The kernels' instances are compiled type by type (attention_*_<type>.hip).
+// What a call of attention launches, by sizes alone (attention_rules.hpp).  The kernels' instances are compiled type by type
+// (attention_*_<type>.hip).
 #pragma once
 #include "attention_common.hpp"
 

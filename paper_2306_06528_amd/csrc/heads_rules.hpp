@@ -12,9 +12,10 @@ struct HeadSizes {
     bool none() const { return batch == 0 || tokens == 0 || heads == 0; }
 };
 
-// Whether no value of one is one of the other's (`size` bytes each), where their addresses go through each other: the queries', keys' and values' parts of one linear map's results, or of its gradient.  They lie
-// apart if their outer dimensions are the same, if what is inside of these (the values, and mostly the heads) are two stretches side by side, and if from one step of an outer dimension to the next it is as far as both
-// together and all that is nearer.  Every choice of outer dimensions is tried; strides are valid ones (valid_heads).
+// Whether no value of one is one of the other's (`size` bytes each), where their addresses go through each other: the queries', keys' and
+// values' parts of one linear map's results, or of its gradient.  They lie apart if their outer dimensions are the same, if what is inside
+// of these (the values, and mostly the heads) are two stretches side by side, and if from one step of an outer dimension to the next it is
+// as far as both together and all that is nearer.  Every choice of outer dimensions is tried; strides are valid ones (valid_heads).
 inline bool heads_apart(const svgd_heads &a, const HeadSizes &as, const svgd_heads &b, const HeadSizes &bs, int64_t size)
 {
     if (!a.data || !b.data || as.none() || bs.none()) return true;

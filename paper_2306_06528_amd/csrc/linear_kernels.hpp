@@ -1,11 +1,13 @@
-// Linear maps with bias, activation and residual, and their backward pass: the tile products of ffn_kernels.hpp with epilogues of their own.
+// Linear maps with bias, activation and residual, and their backward pass: the tile products of ffn_kernels.hpp with epilogues of their
+// own.
 //     z = x W^T + b, y = act(z) + residual          linear_forward_kernel, or thin_linear_kernel for few rows
 //     dz = dy act'(z), db = sum dz                  linear_slope_kernel (dz only where there is an activation: otherwise it is dy)
 //     dx = dz W, dW = dz^T x                        linear_gradients_kernel
-// x has one, two or three parts by its type and W three, so a product has fp32's accuracy; without an activation dW of 16-bit calls is a product of 16-bit operands, of one part each
-// for bf16: exact at a sixth of the cost.  The matrix cores bound the large products, reading the weights those of few rows.
-// 8 x 4,096 x 1,024 x 1,024 bf16: forward 256 to 266 us (206 Gflop of bf16 products, 780 TFLOP/s: two rounds of tiles, whose first loads and epilogues nothing covers), gradients 256 to 269 (275, 1,050 TFLOP/s), sums of
-// dy's columns 24 (67 MB); 5 x 1,003 x 333 x 501 fp32 tanh: forward 35, gradients 39; 16 x 1 x 256 x 768 fp32: 5.0.
+// x has one, two or three parts by its type and W three, so a product has fp32's accuracy; without an activation dW of 16-bit calls is a
+// product of 16-bit operands, of one part each for bf16: exact at a sixth of the cost.  The matrix cores bound the large products, reading
+// the weights those of few rows. 8 x 4,096 x 1,024 x 1,024 bf16: forward 256 to 266 us (206 Gflop of bf16 products, 780 TFLOP/s: two rounds
+// of tiles, whose first loads and epilogues nothing covers), gradients 256 to 269 (275, 1,050 TFLOP/s), sums of dy's columns 24 (67 MB); 5
+// x 1,003 x 333 x 501 fp32 tanh: forward 35, gradients 39; 16 x 1 x 256 x 768 fp32: 5.0.
 #pragma once
 #include "ffn_thin_kernels.hpp"
 #include "linear_rules.hpp"
@@ -176,8 +178,8 @@ template <class T, int JB> SVGD_THIN_KERNEL void thin_linear_kernel(LinearShape 
     });
 }
 
-// dz (null: not wanted) of some rows, and the sums of their columns (null: not wanted) to sums[part][particle][out], or where there is one part to the bias's gradient: 64 lanes have four columns
-// each, the four waves every fourth row.
+// dz (null: not wanted) of some rows, and the sums of their columns (null: not wanted) to sums[part][particle][out], or where there is one
+// part to the bias's gradient: 64 lanes have four columns each, the four waves every fourth row.
 template <class T, bool ACT>
 __global__ __launch_bounds__(256) void linear_slope_kernel(LinearShape s, int64_t per, int parts, int groups, Rows<const T> dy, const float *z, float *dz, float *sums, Params dbias,
                                                            bool accumulate)
@@ -240,7 +242,9 @@ struct PartSums {
     __host__ __device__ int64_t blocks() const { return out.p ? (size + 255) / 256 : 0; }
 };
 
-// Adds them up, in order, those of the weight and of the bias in one launch: a workgroup has 256 values of a particle.  (8 x 1,024 x 1,024 in two parts and 1,024 in 32: 29 us, 5 x 333 x 501 in two and 501 in 62: 7.0; in a launch for each, with the particle divided out in 64 bits, 31 + 5.2 and 5.2 + 5.3.)
+// Adds them up, in order, those of the weight and of the bias in one launch: a workgroup has 256 values of a particle.  (8 x 1,024 x 1,024
+// in two parts and 1,024 in 32: 29 us, 5 x 333 x 501 in two and 501 in 62: 7.0; in a launch for each, with the particle divided out in 64
+// bits, 31 + 5.2 and 5.2 + 5.3.)
 static __global__ __launch_bounds__(256) void linear_sums_kernel(PartSums weight, PartSums bias, bool accumulate)
 {
     const bool second = blockIdx.x >= weight.blocks();

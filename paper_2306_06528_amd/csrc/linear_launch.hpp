@@ -1,4 +1,5 @@
-// The launches of both passes, by the plan that linear_rules.hpp makes.  The kernels' instances are compiled type by type (linear_<type>.hip).
+// The launches of both passes, by the plan that linear_rules.hpp makes.  The kernels' instances are compiled type by type
+// (linear_<type>.hip).
 #pragma once
 #include "ffn_launch.hpp"
 #include "linear_kernels.hpp"

@@ -1,11 +1,14 @@
-// Which tiles a linear map takes, and into how many parts its columns go: plain numbers, no HIP.  Kinds, costs and limits are those of ffn_rules.hpp.
+// Which tiles a linear map takes, and into how many parts its columns go: plain numbers, no HIP.  Kinds, costs and limits are those of
+// ffn_rules.hpp.
 #pragma once
 #include "ffn_rules.hpp"
 
 namespace svgd {
 
-// What a launch takes (ffn_rules.hpp says in what): of the kinds and of one, two or four parts at 14 shapes (1 to 32 particles of 40 to 16,000 rows, 64 to 2,000 wide), fp32 and bf16, forward finds the fastest or one
-// within 8 % of it, backward one within 14 %.  (With the rates of the feed-forward block's products 5 x 1,003 x 333 x 501 fp32 forward took 39 us, so 29; 8 x 1,576 x 384 x 1,152 fp32 backward 202 and 172.)
+// What a launch takes (ffn_rules.hpp says in what): of the kinds and of one, two or four parts at 14 shapes (1 to 32 particles of 40 to
+// 16,000 rows, 64 to 2,000 wide), fp32 and bf16, forward finds the fastest or one within 8 % of it, backward one within 14 %.  (With the
+// rates of the feed-forward block's products 5 x 1,003 x 333 x 501 fp32 forward took 39 us, so 29; 8 x 1,576 x 384 x 1,152 fp32 backward
+// 202 and 172.)
 constexpr Rates kOfLinear = {{1.0, 0.61, 0.42}, 1.0, 8.8, 0.1, 3.7e6};
 constexpr Rates kOfLinearGradients = {{1.0, 0.73, 0.54}, 0.78, 6.2, 4.0, 12e6};
 
@@ -23,7 +26,8 @@ struct LinearForwardPlan {
     size_t scratch(int n, int64_t rows, int64_t out) const { return tile.parts > 1 ? (size_t)tile.parts * n * rows * linear_ld(out) * 4 : 0; }
 };
 
-// dx and the weight's gradient: tiles of one kind, in one launch.  The bias's gradient: `sums` parts of the rows.  Without an activation dz is dy and has no place in scratch memory.
+// dx and the weight's gradient: tiles of one kind, in one launch.  The bias's gradient: `sums` parts of the rows.  Without an activation dz
+// is dy and has no place in scratch memory.
 struct LinearBackwardPlan {
     TileKind kind = kLarge;
     int input_parts = 1, param_parts = 0, sums;

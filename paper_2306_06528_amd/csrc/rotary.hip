@@ -70,8 +70,8 @@ RotaryArgs args_of(const svgd_rotary &p, int64_t most)
     a.blocks = (int)((a.tokens + a.per - 1) / a.per);
     return a;
 }
-// (Forward, 8 x 8 x 197 x 12 heads of 64 bf16: 8,192 workgroups 30 us, 2,048 17, fewer angles being formed twice.  Backward, 8 x 2 x 4,096 x 20 heads of 128 bf16: 768, as many as are there at a time, 233 us, 1,024
-// 286, 2,048 243.)
+// (Forward, 8 x 8 x 197 x 12 heads of 64 bf16: 8,192 workgroups 30 us, 2,048 17, fewer angles being formed twice.  Backward, 8 x 2 x 4,096
+// x 20 heads of 128 bf16: 768, as many as are there at a time, 233 us, 1,024 286, 2,048 243.)
 constexpr int64_t kForwardBlocks = 2048, kBackwardBlocks = 768;
 
 struct Reads { // besides the activations

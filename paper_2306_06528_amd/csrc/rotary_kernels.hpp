@@ -1,8 +1,9 @@
-// Norms of queries and keys, head by head, with the rotation by position in the same pass, forward and backward.  A team of L lanes holds a head, 16 bytes a lane, from its one load to its
-// one store; memory bounds both passes.  A workgroup has some tokens of one particle: their angles are formed in 64 bits once for all heads (kTokens tokens at a time, to LDS), and the weights
-// and their gradients stay in registers.  In the half layout a value's partner is another lane's: the team's values change lanes in its part of LDS.
-// 8 x 2 x 4,096 x 20 heads of 128 bf16: forward 157 us (671 MB, 4.3 TB/s), backward 234 (1,007 MB, 4.3 TB/s); 8 x 8 x 197 x 12 heads of 64, in the memory-side cache: 16.7 and 26.5, bound by
-// the formation of angles, 64-bit, and by the latency of a team's loads, one head ahead.
+// Norms of queries and keys, head by head, with the rotation by position in the same pass, forward and backward.  A team of L lanes holds a
+// head, 16 bytes a lane, from its one load to its one store; memory bounds both passes.  A workgroup has some tokens of one particle: their
+// angles are formed in 64 bits once for all heads (kTokens tokens at a time, to LDS), and the weights and their gradients stay in
+// registers.  In the half layout a value's partner is another lane's: the team's values change lanes in its part of LDS. 8 x 2 x 4,096 x 20
+// heads of 128 bf16: forward 157 us (671 MB, 4.3 TB/s), backward 234 (1,007 MB, 4.3 TB/s); 8 x 8 x 197 x 12 heads of 64, in the memory-side
+// cache: 16.7 and 26.5, bound by the formation of angles, 64-bit, and by the latency of a team's loads, one head ahead.
 #pragma once
 #include "attention_common.hpp"
 
@@ -112,7 +113,8 @@ __device__ __forceinline__ void angles(const RotaryArgs &a, int64_t first, int64
     }
 }
 
-// What a pass reads and writes of queries (0) and of keys (1): read from the kernel's arguments by number, so that only one of them takes scalar registers at a time.
+// What a pass reads and writes of queries (0) and of keys (1): read from the kernel's arguments by number, so that only one of them takes
+// scalar registers at a time.
 template <class T> struct RotaryKind {
     Heads<const T> x, dy; // backward; forward x alone
     Heads<T> to;
@@ -147,8 +149,9 @@ template <class T, bool WHOLE> struct HeadPiece {
     }
 };
 
-// The heads of `count` tokens from token0 on, dealt to the teams one after the other.  From one of a team's to its next one it is `tokens` tokens and `more` heads, and at the end of a token's heads or of a
-// sequence a step back: pointers are moved on by sums (as products of 64 bits addresses took a third of the instructions).
+// The heads of `count` tokens from token0 on, dealt to the teams one after the other.  From one of a team's to its next one it is `tokens`
+// tokens and `more` heads, and at the end of a token's heads or of a sequence a step back: pointers are moved on by sums (as products of 64
+// bits addresses took a third of the instructions).
 struct HeadTurn {
     int items, heads, length, teams, item, tokens, more;
     int i, t, h; // the token's number among them, of its sequence; head
